@@ -464,6 +464,93 @@ int32_t gs_table_mult(void* table, int64_t num_nodes, int32_t dim, int32_t dtype
 int32_t gs_table_mult_add(void* dst, const void* src, int64_t num_nodes, int32_t dim, int32_t dtype,
                           float factor, void* stream);
 
+/* --------------------------------------------------------------------------
+ * gs_softmax_loss -- skip-gram's own objective, which negative sampling stands in
+ * for (Sec. 2.2): the softmax over every node, with the gradients of both tables.
+ *   w_in [num_in][dim], w_out [num_nodes][dim] of dtype GS_F32 | GS_BF16 | GS_F16.
+ *   For pair i: h = w_in[centers[i]], t = contexts[i], z_j = scale * <h, w_out[j]>
+ *   + bias[j]; loss_out[i] = log sum_j exp(z_j) - z_t.  With p_j = exp(z_j) / sum:
+ *     g_in[i]  = grad_scale * scale * (sum_j p_j w_out[j] - w_out[t])      per pair
+ *     g_out[j] = grad_scale * scale * sum_i (p_ij - [t_i = j]) h_i         every node
+ *   bias  float[num_nodes] or NULL: constants (log-frequency offsets); -infinity
+ *   masks a node: it is no answer, its row is not looked at and its gradient is 0.
+ *   loss_out float[num_pairs];  g_in [num_pairs][dim] or NULL;  g_out
+ *   [num_nodes][dim] or NULL, both of the tables' dtype and overwritten.
+ *   Sums, maxima and statistics are fp32 or fp64; 16-bit tables: the probabilities
+ *   are rounded to the tables' format before they are summed with rows (fp32 sums).
+ *   Same bits on every run.  The pairs x nodes matrix is never stored.
+ *   contexts[i] = -1 leaves the pair out (loss 0, no gradient).  A centre outside
+ *   [0, num_in), or another context outside [0, num_nodes), gives loss NaN and no
+ *   gradient; a masked context gives loss +infinity and no gradient.  Equal centres
+ *   are separate rows of g_in; num_pairs = 0 writes zeros to g_out.
+ *   dim a multiple of 4 (fp32) or 8 (16-bit) and at most 256; tables and gradients
+ *   16-byte aligned; scale > 0.  Errors: GS_EINVAL otherwise.  Workspace:
+ *   gs_softmax_loss_workspace_bytes (want_grad: whether g_in or g_out is given).
+ *
+ * gs_scores -- the same z, for answers: scores_out[i][j] = scale * <w_in[centers[i]],
+ *   w_out[j]> + bias[j], float[num_centers][num_nodes]; -infinity for masked nodes,
+ *   a row of NaN (but for masked nodes) for a centre that is no row.
+ * ------------------------------------------------------------------------ */
+size_t gs_softmax_loss_workspace_bytes(int64_t num_pairs, int64_t num_nodes, int32_t dim, int32_t dtype,
+                                       int32_t want_grad);
+int32_t gs_softmax_loss(const void* w_in, int64_t num_in, const void* w_out, int64_t num_nodes, int32_t dim,
+                        int32_t dtype, const int32_t* centers, const int32_t* contexts, int64_t num_pairs,
+                        const float* bias, float scale, float* loss_out, void* g_in, void* g_out,
+                        float grad_scale, void* ws, size_t ws_bytes, void* stream);
+size_t gs_scores_workspace_bytes(int64_t num_centers, int64_t num_nodes, int32_t dim, int32_t dtype);
+int32_t gs_scores(const void* w_in, int64_t num_in, const void* w_out, int64_t num_nodes, int32_t dim,
+                  int32_t dtype, const int32_t* centers, int64_t num_centers, const float* bias, float scale,
+                  float* scores_out, void* ws, size_t ws_bytes, void* stream);
+
+/* --------------------------------------------------------------------------
+ * gs_sample_scores -- one node per row of scores, by given random numbers.
+ *   scores [rows][n] of dtype GS_F32 | GS_BF16 | GS_F16, aligned to its element;
+ *   -infinity and NaN leave a node out.  uniforms float[rows] in [0, 1).
+ *   Each of temperature, top_k, top_p, min_p: one value per row, or NULL.  Nodes
+ *   are ordered by score, the lowest index first among equal scores, and
+ *     e_j = exp((s_j - max) / temperature)            (NULL: temperature 1)
+ *     top_k  keeps the first k nodes                  (k < 1: no such limit)
+ *     top_p  then keeps those of them before which less than top_p of their sum
+ *            lies, and always the first               (>= 1 or NaN: no limit)
+ *     min_p  then keeps e_j >= min_p                  (<= 0 or NaN: no limit; 1 at most)
+ *   ids_out[r] = the smallest index j with sum_{i <= j, kept} e_i > u * sum_{kept} e
+ *   (u >= 1 or NaN: the last that has any weight); probs_out[r], if not NULL, e_j
+ *   over that sum.  temperature 0 takes the first node of the order, probability 1.
+ *   A row of nothing but left-out nodes gives id -1 and probability 0; a negative
+ *   temperature or NaN gives id -1 and probability NaN.  All weights are fp64, so
+ *   that the answer is that of the definition unless u falls within about 1e-15 of
+ *   a border; same answer on every run.
+ *   ids_out int32[rows], probs_out float[rows]; 1 <= n < 2^31, rows < 2^22.
+ * ------------------------------------------------------------------------ */
+size_t gs_sample_scores_workspace_bytes(int64_t rows, int64_t n, int32_t dtype);
+int32_t gs_sample_scores(const void* scores, int64_t rows, int64_t n, int32_t dtype, const float* uniforms,
+                         const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                         int32_t* ids_out, float* probs_out, void* ws, size_t ws_bytes, void* stream);
+
+/* --------------------------------------------------------------------------
+ * gs_clip_grads -- the norm of many tensors taken together, and clipping to it.
+ *   list: HOST array (read during the call).  norm_out double[1] = square root of
+ *   the sum of all squares (summed in fp64; same bits on every run).  Where it is
+ *   above max_norm, every element becomes x * (max_norm / norm), rounded once.  A
+ *   norm that is infinite or NaN scales nothing.
+ *   A tensor with out == NULL (or out == data) is clipped in place, and not written
+ *   at all while the norm is not above max_norm; another one is written to `out`,
+ *   scaled or copied.  data and out need their element's alignment alone; no tensor
+ *   may overlap another's out.  max_norm = infinity with everything in place is the
+ *   norm alone.  Empty lists and empty tensors are fine (norm 0).
+ *   Errors: GS_EINVAL for max_norm < 0 or NaN, a dtype that is none, more than 2^40
+ *   elements.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  void* data;
+  void* out;           /* or NULL: in place                 */
+  int64_t count;       /* elements                          */
+  int32_t dtype;       /* GS_F32 | GS_BF16 | GS_F16         */
+} gs_tensor;
+size_t gs_clip_grads_workspace_bytes(int32_t num_tensors);
+int32_t gs_clip_grads(const gs_tensor* list, int32_t num_tensors, double max_norm, double* norm_out, void* ws,
+                      size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -34,6 +34,9 @@ EXPORTS = (
     "gs_line1_step_workspace_bytes", "gs_line1_step",
     "gs_unique_ids_workspace_bytes", "gs_unique_ids", "gs_get_rows", "gs_put_rows",
     "gs_table_mult", "gs_table_mult_add", "gs_sort_pairs_workspace_bytes", "gs_sort_pairs",
+    "gs_softmax_loss_workspace_bytes", "gs_softmax_loss", "gs_scores_workspace_bytes", "gs_scores",
+    "gs_sample_scores_workspace_bytes", "gs_sample_scores",
+    "gs_clip_grads_workspace_bytes", "gs_clip_grads",
 )
 
 
@@ -55,6 +58,10 @@ class CsrStruct(C.Structure):
 
 class AliasStruct(C.Structure):
     _fields_ = [("prob", C.c_void_p), ("alias", C.c_void_p), ("packed", C.c_void_p)]
+
+
+class TensorStruct(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("out", C.c_void_p), ("count", C.c_int64), ("dtype", C.c_int32)]
 
 
 _lib = None
@@ -550,3 +557,139 @@ def gs_sort_pairs(centers, contexts, num_nodes: int, centers_out=None, contexts_
                              _dev(contexts_out, torch.int32), _dev(ws), C.c_size_t(ws.numel()), _stream())
     _check(rc, "gs_sort_pairs")
     return centers_out, contexts_out
+
+
+def gs_softmax_loss_workspace_bytes(num_pairs: int, num_nodes: int, dim: int, dtype: int = GS_F32,
+                                    want_grad: bool = True) -> int:
+    return int(lib().gs_softmax_loss_workspace_bytes(C.c_int64(num_pairs), C.c_int64(num_nodes), C.c_int32(dim),
+                                                     C.c_int32(dtype), C.c_int32(bool(want_grad))))
+
+
+def _two_tables(w_in, w_out, bias):
+    if w_in.dim() != 2 or w_out.dim() != 2 or w_in.shape[1] != w_out.shape[1] or w_in.dtype != w_out.dtype:
+        raise TypeError("w_in and w_out must be [rows, dim] with the same dim and dtype")
+    if bias is not None and tuple(bias.shape) != (w_out.shape[0],):
+        raise ValueError("bias must have one value per row of w_out")
+    return _table_dtype(w_in)
+
+
+def _out(t, shape, dtype, device, name):
+    """A new output, or the caller's, checked."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{name} must have shape {tuple(shape)} and dtype {dtype}")
+    return t
+
+
+def gs_softmax_loss(w_in, w_out, centers, contexts, bias=None, scale: float = 1.0, grad_scale: float = 1.0,
+                    want_grad: bool = True, loss_out=None, g_in=None, g_out=None, ws=None):
+    """Softmax loss of every pair over all nodes; returns (loss [n] float32, g_in [n, dim], g_out [nodes, dim]),
+    the gradients None without want_grad (see gs.h)."""
+    dtype = _two_tables(w_in, w_out, bias)
+    (num_in, dim), num_nodes, n = w_in.shape, int(w_out.shape[0]), int(centers.numel())
+    if int(contexts.numel()) != n:
+        raise ValueError("centers and contexts must have the same length")
+    dev = w_in.device
+    loss_out = _out(loss_out, (n,), torch.float32, dev, "loss_out")
+    if want_grad:
+        g_in = _out(g_in, (n, dim), w_in.dtype, dev, "g_in")
+        g_out = _out(g_out, (num_nodes, dim), w_out.dtype, dev, "g_out")
+    else:
+        g_in = g_out = None
+    if ws is None:
+        ws = _workspace(gs_softmax_loss_workspace_bytes(n, num_nodes, dim, dtype, want_grad), dev)
+    rc = lib().gs_softmax_loss(
+        _dev(w_in, None, "w_in"), C.c_int64(num_in), _dev(w_out, None, "w_out"), C.c_int64(num_nodes), C.c_int32(dim),
+        C.c_int32(dtype), _dev(centers, torch.int32, "centers"), _dev(contexts, torch.int32, "contexts"), C.c_int64(n),
+        _dev(bias, torch.float32, "bias"), C.c_float(scale), _dev(loss_out, None, "loss_out"), _dev(g_in, None, "g_in"),
+        _dev(g_out, None, "g_out"), C.c_float(grad_scale), _dev(ws), C.c_size_t(ws.numel()), _stream())
+    _check(rc, "gs_softmax_loss")
+    return loss_out, g_in, g_out
+
+
+def gs_scores_workspace_bytes(num_centers: int, num_nodes: int, dim: int, dtype: int = GS_F32) -> int:
+    return int(lib().gs_scores_workspace_bytes(C.c_int64(num_centers), C.c_int64(num_nodes), C.c_int32(dim), C.c_int32(dtype)))
+
+
+def gs_scores(w_in, w_out, centers, bias=None, scale: float = 1.0, out=None, ws=None):
+    """float32 [n, nodes]: scale * <w_in[centers[i]], w_out[j]> + bias[j]."""
+    dtype = _two_tables(w_in, w_out, bias)
+    (num_in, dim), num_nodes, n = w_in.shape, int(w_out.shape[0]), int(centers.numel())
+    dev = w_in.device
+    out = _out(out, (n, num_nodes), torch.float32, dev, "out")
+    if ws is None:
+        ws = _workspace(gs_scores_workspace_bytes(n, num_nodes, dim, dtype), dev)
+    rc = lib().gs_scores(
+        _dev(w_in, None, "w_in"), C.c_int64(num_in), _dev(w_out, None, "w_out"), C.c_int64(num_nodes), C.c_int32(dim),
+        C.c_int32(dtype), _dev(centers, torch.int32, "centers"), C.c_int64(n), _dev(bias, torch.float32, "bias"),
+        C.c_float(scale), _dev(out, None, "out"), _dev(ws), C.c_size_t(ws.numel()), _stream())
+    _check(rc, "gs_scores")
+    return out
+
+
+def gs_sample_scores_workspace_bytes(rows: int, n: int, dtype: int = GS_F32) -> int:
+    return int(lib().gs_sample_scores_workspace_bytes(C.c_int64(rows), C.c_int64(n), C.c_int32(dtype)))
+
+
+def gs_sample_scores(scores, uniforms, temperature=None, top_k=None, top_p=None, min_p=None, ids_out=None,
+                     probs_out=None, ws=None):
+    """One node per row of scores [rows, n]; returns (ids int32 [rows], probs float32 [rows]).  The filters are
+    tensors with one value per row, or None (see gs.h)."""
+    if scores.dim() != 2:
+        raise ValueError("scores must be [rows, n]")
+    dtype = _table_dtype(scores)
+    rows, n = int(scores.shape[0]), int(scores.shape[1])
+    dev = scores.device
+    for name, t in (("uniforms", uniforms), ("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p)):
+        if t is not None and tuple(t.shape) != (rows,):
+            raise ValueError(f"{name} must have one value per row of scores")
+    ids_out = _out(ids_out, (rows,), torch.int32, dev, "ids_out")
+    probs_out = _out(probs_out, (rows,), torch.float32, dev, "probs_out")
+    if ws is None:
+        ws = _workspace(gs_sample_scores_workspace_bytes(rows, n, dtype), dev)
+    rc = lib().gs_sample_scores(
+        _dev(scores, None, "scores"), C.c_int64(rows), C.c_int64(n), C.c_int32(dtype),
+        _dev(uniforms, torch.float32, "uniforms"), _dev(temperature, torch.float32, "temperature"),
+        _dev(top_k, torch.int32, "top_k"), _dev(top_p, torch.float32, "top_p"), _dev(min_p, torch.float32, "min_p"),
+        _dev(ids_out), _dev(probs_out), _dev(ws), C.c_size_t(ws.numel()), _stream())
+    _check(rc, "gs_sample_scores")
+    return ids_out, probs_out
+
+
+class GradList:
+    """Gradients (and, where given, the tensors that receive them clipped) as the host array gs_clip_grads takes;
+    built once for tensors that stay where they are."""
+
+    def __init__(self, grads, outs=None):
+        self.grads, self.outs = list(grads), None if outs is None else list(outs)
+        if self.outs is not None and len(self.outs) != len(self.grads):
+            raise ValueError("one output per gradient")
+        if not self.grads:
+            raise ValueError("no gradients")
+        self.device = self.grads[0].device
+        self.array = (TensorStruct * len(self.grads))()
+        for i, g in enumerate(self.grads):
+            _dev(g, None, "gradient")
+            o = None if self.outs is None else self.outs[i]
+            if o is not None and (o.dtype != g.dtype or o.numel() != g.numel()):
+                raise TypeError("an output must have its gradient's size and dtype")
+            self.array[i] = TensorStruct(g.data_ptr(), None if o is None else _dev(o, None, "output").value, g.numel(), _table_dtype(g))
+
+
+def gs_clip_grads_workspace_bytes(num_tensors: int) -> int:
+    return int(lib().gs_clip_grads_workspace_bytes(C.c_int32(num_tensors)))
+
+
+def gs_clip_grads(grads, max_norm: float, norm_out=None, ws=None):
+    """Clips a GradList (or a list of tensors, in place) to the norm max_norm; returns the norm before, float64 [1]."""
+    if not isinstance(grads, GradList):
+        grads = GradList(grads)
+    n = len(grads.grads)
+    norm_out = _out(norm_out, (1,), torch.float64, grads.device, "norm_out")
+    if ws is None:
+        ws = _workspace(gs_clip_grads_workspace_bytes(n), grads.device)
+    rc = lib().gs_clip_grads(grads.array, C.c_int32(n), C.c_double(max_norm), _dev(norm_out), _dev(ws),
+                             C.c_size_t(ws.numel()), _stream())
+    _check(rc, "gs_clip_grads")
+    return norm_out

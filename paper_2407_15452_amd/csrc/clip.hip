@@ -1,0 +1,305 @@
+// gs_clip_grads: the norm of many tensors taken together, and all of them scaled down to a limit.
+//
+//   norm = sqrt(sum over tensors and elements of x^2);  x <- x * (max_norm / norm) where norm > max_norm
+//
+// Both passes run over the same pieces of work (32 KB of one tensor each), dealt to a fixed number of workgroups, and are
+// bound by memory.  The squares are summed in fp64 (fp32 would overflow from 1.8e19 on and lose small tensors next to large
+// ones); every workgroup leaves one partial sum and the second pass adds them in order, so the same tensors give the same
+// bits on every run.  The second pass runs backwards: what the first one read last is still in the caches.
+// Addresses and sizes travel in the kernel arguments (nothing is copied to the device), kPerLaunch tensors a launch.
+
+#include <cmath>
+
+#include "common.h"
+
+namespace gs {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPieces = 8;                     // 16-byte pieces per lane and unit: that many loads in flight
+constexpr int kUnit = kThreads * kPieces;      // pieces per unit: 32 KB
+constexpr int kMaxGroups = 1024;               // four workgroups per compute unit
+constexpr int kPerLaunch = 112;                // the arguments stay below 4 KB
+
+struct Item {
+  void* data;
+  void* out;
+  int64_t count;
+  uint32_t first_unit;                         // of this launch
+  int32_t dtype;
+};
+struct ClipArgs {
+  Item item[kPerLaunch];
+  int32_t items;
+  uint32_t units;
+  double* parts;                               // first pass: this launch's; second: all
+  int32_t num_parts;
+  double max_norm;
+  double* norm_out;                            // second pass: null but for one launch
+};
+static_assert(sizeof(ClipArgs) <= 4096, "kernel arguments");
+
+__device__ __forceinline__ int find_item(const ClipArgs& a, uint32_t unit) {
+  int lo = 0, hi = a.items - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.item[mid].first_unit <= unit) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+// elements in front of the first 16-byte boundary
+template <typename T>
+__device__ __forceinline__ int64_t head_of(const T* p, int64_t count) {
+  const int64_t h = (int64_t)((16 - ((uintptr_t)p & 15)) & 15) / (int64_t)sizeof(T);
+  return h < count ? h : count;
+}
+
+struct F32Value {
+  typedef float elem;
+  static __device__ __forceinline__ float get(float x) { return x; }
+  static __device__ __forceinline__ float put(float x) { return x; }
+};
+template <typename H>
+struct HalfValue {
+  typedef uint16_t elem;
+  static __device__ __forceinline__ float get(uint16_t x) { return H::lo(x); }
+  static __device__ __forceinline__ uint16_t put(float x) { return (uint16_t)H::round(x); }
+};
+
+template <typename V>
+__device__ __forceinline__ double piece_squares(uint4 w) {
+  constexpr int per = 16 / (int)sizeof(typename V::elem);
+  typename V::elem e[per];
+  __builtin_memcpy(e, &w, 16);
+  double s = 0.0;
+#pragma unroll
+  for (int k = 0; k < per; ++k) {
+    const double x = (double)V::get(e[k]);
+    s = fma(x, x, s);
+  }
+  return s;
+}
+template <typename V>
+__device__ __forceinline__ uint4 piece_scaled(uint4 w, float factor) {
+  constexpr int per = 16 / (int)sizeof(typename V::elem);
+  typename V::elem e[per];
+  __builtin_memcpy(e, &w, 16);
+#pragma unroll
+  for (int k = 0; k < per; ++k) e[k] = V::put(V::get(e[k]) * factor);
+  __builtin_memcpy(&w, e, 16);
+  return w;
+}
+
+template <typename V>
+__device__ double unit_squares(const Item& it, uint32_t unit) {
+  typedef typename V::elem elem;
+  constexpr int per = 16 / (int)sizeof(elem);
+  const elem* x = static_cast<const elem*>(it.data);
+  const int64_t head = head_of(x, it.count);
+  const int64_t pieces = (it.count - head) / per;
+  const uint4* body = reinterpret_cast<const uint4*>(x + head);
+  const int64_t first = (int64_t)unit * kUnit + threadIdx.x;
+  uint4 w[kPieces];
+#pragma unroll
+  for (int k = 0; k < kPieces; ++k) {
+    const int64_t p = first + (int64_t)k * kThreads;
+    w[k] = p < pieces ? body[p] : make_uint4(0, 0, 0, 0);
+  }
+  double s = 0.0;
+#pragma unroll
+  for (int k = 0; k < kPieces; ++k) s += piece_squares<V>(w[k]);
+  if (unit == 0) {                             // what lies in front of the first whole piece and after the last
+    const int64_t tail = head + pieces * per;
+    const int64_t rest = head + (it.count - tail);
+    if ((int64_t)threadIdx.x < rest) {
+      const int64_t at = (int64_t)threadIdx.x < head ? (int64_t)threadIdx.x : tail + ((int64_t)threadIdx.x - head);
+      const double v = (double)V::get(x[at]);
+      s = fma(v, v, s);
+    }
+  }
+  return s;
+}
+
+template <typename V>
+__device__ void unit_scaled(const Item& it, uint32_t unit, float factor, bool copy) {
+  typedef typename V::elem elem;
+  constexpr int per = 16 / (int)sizeof(elem);
+  const elem* x = static_cast<const elem*>(it.data);
+  elem* y = static_cast<elem*>(it.out);
+  const int64_t head = head_of(x, it.count);
+  const int64_t pieces = (it.count - head) / per;
+  const int64_t tail = head + pieces * per;
+  if ((((uintptr_t)x ^ (uintptr_t)y) & 15) == 0) {
+    const uint4* from = reinterpret_cast<const uint4*>(x + head);
+    uint4* to = reinterpret_cast<uint4*>(y + head);
+    const int64_t first = (int64_t)unit * kUnit + threadIdx.x;
+    uint4 w[kPieces];
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) {
+      const int64_t p = first + (int64_t)k * kThreads;
+      w[k] = p < pieces ? from[p] : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) {
+      const int64_t p = first + (int64_t)k * kThreads;
+      if (p < pieces) to[p] = copy ? w[k] : piece_scaled<V>(w[k], factor);
+    }
+  } else {                                     // the two lie differently: element by element
+    const int64_t from = head + (int64_t)unit * kUnit * per;
+    const int64_t end = min(from + (int64_t)kUnit * per, tail);
+    for (int64_t i = from + threadIdx.x; i < end; i += kThreads) y[i] = copy ? x[i] : V::put(V::get(x[i]) * factor);
+  }
+  if (unit == 0) {
+    const int64_t rest = head + (it.count - tail);
+    if ((int64_t)threadIdx.x < rest) {
+      const int64_t at = (int64_t)threadIdx.x < head ? (int64_t)threadIdx.x : tail + ((int64_t)threadIdx.x - head);
+      y[at] = copy ? x[at] : V::put(V::get(x[at]) * factor);
+    }
+  }
+}
+
+// sum over the workgroup, the same in every lane
+__device__ double group_sum(double s) {
+  __shared__ double wave_sum[kThreads / 64];
+#pragma unroll
+  for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d, 64);
+  if ((threadIdx.x & 63) == 0) wave_sum[threadIdx.x >> 6] = s;
+  __syncthreads();
+  s = 0.0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) s += wave_sum[w];
+  __syncthreads();
+  return s;
+}
+
+__global__ __launch_bounds__(kThreads) void squares_kernel(ClipArgs a) {
+  double s = 0.0;
+  for (uint32_t u = blockIdx.x; u < a.units; u += gridDim.x) {
+    const Item& it = a.item[find_item(a, u)];
+    const uint32_t unit = u - it.first_unit;
+    if (it.dtype == GS_F32) s += unit_squares<F32Value>(it, unit);
+    else if (it.dtype == GS_BF16) s += unit_squares<HalfValue<bf16_t>>(it, unit);
+    else s += unit_squares<HalfValue<f16_t>>(it, unit);
+  }
+  s = group_sum(s);
+  if (threadIdx.x == 0) a.parts[blockIdx.x] = s;
+}
+
+// many launches' parts into one
+__global__ __launch_bounds__(kThreads) void add_parts_kernel(const double* parts, int32_t num_parts, double* to) {
+  double s = 0.0;
+  for (int32_t k = threadIdx.x; k < num_parts; k += kThreads) s += parts[k];
+  s = group_sum(s);
+  if (threadIdx.x == 0) *to = s;
+}
+
+__global__ __launch_bounds__(kThreads) void clip_kernel(ClipArgs a) {
+  double s = 0.0;
+  for (int32_t k = threadIdx.x; k < a.num_parts; k += kThreads) s += a.parts[k];
+  const double norm = sqrt(group_sum(s));
+  if (a.norm_out != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *a.norm_out = norm;
+  // a norm that is no number, or infinite, says that some gradient is: nothing is scaled by it
+  const bool reached = norm > a.max_norm && norm < INFINITY;
+  const float factor = reached ? (float)(a.max_norm / norm) : 1.0f;
+  for (uint32_t v = blockIdx.x; v < a.units; v += gridDim.x) {
+    const uint32_t u = a.units - 1 - v;
+    const Item& it = a.item[find_item(a, u)];
+    if (!reached && it.out == it.data) continue;
+    const uint32_t unit = u - it.first_unit;
+    if (it.dtype == GS_F32) unit_scaled<F32Value>(it, unit, factor, !reached);
+    else if (it.dtype == GS_BF16) unit_scaled<HalfValue<bf16_t>>(it, unit, factor, !reached);
+    else unit_scaled<HalfValue<f16_t>>(it, unit, factor, !reached);
+  }
+}
+
+int64_t elem_bytes(int32_t dtype) { return dtype == GS_F32 ? 4 : 2; }
+int64_t launches_for(int64_t num_tensors) { return std::max<int64_t>(1, ceil_div(num_tensors, kPerLaunch)); }
+
+// the next launch's tensors from `at` on; returns where the one after it begins
+int32_t fill_args(const gs_tensor* list, int32_t num_tensors, int32_t at, ClipArgs& a) {
+  uint64_t units = 0;
+  a.items = 0;
+  while (at < num_tensors && a.items < kPerLaunch) {
+    const gs_tensor& t = list[at];
+    if (t.count > 0) {
+      const uint64_t more = (uint64_t)std::max<int64_t>(1, ceil_div(ceil_div(t.count * elem_bytes(t.dtype), 16), kUnit));
+      Item& it = a.item[a.items++];
+      it = Item{t.data, t.out ? t.out : t.data, t.count, (uint32_t)units, t.dtype};
+      units += more;
+    }
+    ++at;
+  }
+  a.units = (uint32_t)units;
+  return at;
+}
+
+}  // namespace
+}  // namespace gs
+
+using namespace gs;
+
+extern "C" size_t gs_clip_grads_workspace_bytes(int32_t num_tensors) {
+  if (num_tensors < 0) return 0;
+  return align_up(sizeof(double) * (size_t)(1 + launches_for(num_tensors) * kMaxGroups));
+}
+
+extern "C" int32_t gs_clip_grads(const gs_tensor* list, int32_t num_tensors, double max_norm, double* norm_out, void* ws,
+                                 size_t ws_bytes, void* stream_) {
+  hipStream_t stream = (hipStream_t)stream_;
+  if (num_tensors < 0 || (num_tensors > 0 && !list) || !norm_out || !(max_norm >= 0.0)) return GS_EINVAL;
+  if (!ws || !aligned(ws, 256)) return GS_EINVAL;
+  int64_t total = 0;
+  bool elsewhere = false;
+  for (int32_t i = 0; i < num_tensors; ++i) {
+    const gs_tensor& t = list[i];
+    if (t.dtype != GS_F32 && t.dtype != GS_BF16 && t.dtype != GS_F16) return GS_EINVAL;
+    if (t.count < 0 || t.count > ((int64_t)1 << 40)) return GS_EINVAL;
+    if (t.count == 0) continue;
+    if (!t.data || !aligned(t.data, (size_t)elem_bytes(t.dtype)) || !aligned(t.out, (size_t)elem_bytes(t.dtype))) return GS_EINVAL;
+    if (t.out && t.out != t.data) elsewhere = true;
+    total += t.count;
+    if (total > ((int64_t)1 << 40)) return GS_EINVAL;
+  }
+  if (ws_bytes < gs_clip_grads_workspace_bytes(num_tensors)) return GS_EWORKSPACE;
+  double* sum = static_cast<double*>(ws);
+  double* parts = sum + 1;
+  ClipArgs a{};
+  a.max_norm = max_norm;
+  int32_t num_parts = 0, launches = 0;
+  for (int32_t at = 0; at < num_tensors;) {
+    at = fill_args(list, num_tensors, at, a);
+    if (a.items == 0) break;
+    const unsigned groups = std::min<unsigned>(a.units, kMaxGroups);
+    a.parts = parts + num_parts;
+    squares_kernel<<<groups, kThreads, 0, stream>>>(a);
+    GS_LAUNCH_CHECK();
+    num_parts += (int32_t)groups;
+    ++launches;
+  }
+  a.parts = parts;
+  a.num_parts = num_parts;
+  a.norm_out = norm_out;
+  if (launches > 1) {                          // every workgroup of the second pass adds all parts: few of them
+    add_parts_kernel<<<1, kThreads, 0, stream>>>(parts, num_parts, sum);
+    GS_LAUNCH_CHECK();
+    a.parts = sum;
+    a.num_parts = 1;
+  }
+  const bool norm_alone = launches == 0 || (!elsewhere && std::isinf(max_norm));
+  if (norm_alone) {
+    a.items = 0;
+    a.units = 0;
+    clip_kernel<<<1, kThreads, 0, stream>>>(a);
+    GS_LAUNCH_CHECK();
+    return GS_OK;
+  }
+  for (int32_t at = 0; at < num_tensors;) {
+    at = fill_args(list, num_tensors, at, a);
+    if (a.items == 0) break;
+    clip_kernel<<<std::min<unsigned>(a.units, kMaxGroups), kThreads, 0, stream>>>(a);
+    GS_LAUNCH_CHECK();
+    a.norm_out = nullptr;
+  }
+  return GS_OK;
+}

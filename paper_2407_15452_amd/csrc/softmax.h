@@ -1,0 +1,774 @@
+// gs_softmax_loss, gs_scores: skip-gram's softmax over every node.
+//
+//   z_ij = scale * <h_i, c_j> + bias_j,   h_i = w_in[centers[i]],  c_j = w_out[j]
+//   loss_i = log sum_j exp(z_ij) - z_it,  t = contexts[i]
+//   g_in[i]  = grad_scale * scale * (sum_j p_ij c_j - c_t),      p_ij = exp(z_ij) / sum_j exp(z_ij)
+//   g_out[j] = grad_scale * scale * sum_i (p_ij - [t_i = j]) h_i
+//
+// The pairs x nodes matrices z and p are never stored.  One kernel shape does both directions.  A wave keeps 32 or 64 rows of
+// one operand in registers, as the right operand of the matrix instructions; the four waves of a workgroup stream the rows of
+// the other one through LDS.  A 32 x 32 block of products comes out with the kept rows across the lanes and the streamed rows
+// in the registers of a lane, so that a kept row's softmax statistics belong to its lane, and the block, once it is
+// probabilities, is the right operand of the second product without leaving the registers: the matrix instruction sums over
+// any numbering of its inner dimension, as long as both operands use the same one.  The left operand of the second product is
+// the streamed tile again, transposed on its way out of LDS (16-bit tables: ds_read_b64_tr_b16; fp32: one column per lane).
+//   forward: pairs kept, nodes streamed, running maximum and sum; gives the loss and sum_j p_ij c_j in one pass.
+//   table gradient: nodes kept, pairs streamed, p from the forward pass's log-sum; no atomics, each row of g_out has one owner.
+// Where the kept rows alone do not fill the chip the streamed ones are split, and a small kernel joins the parts in order.
+//
+// LDS tiles are written by the loads themselves (global_load_lds, 16 bytes per lane, one tile ahead).  Such a load puts lane
+// l's piece at base + 16 l, so rows cannot be padded; pieces are swapped inside a row instead, by a function of the row that
+// the source address undoes.  Rows beyond the table, pieces beyond `dim` and rows of masked nodes (bias -inf) are read from a
+// piece of zeros: whatever a masked row holds, infinities and NaN included, it takes no part.
+
+#pragma once
+
+#include "common.h"
+
+namespace gs {
+
+// One call, checked: what the format's own file launches.
+struct SoftmaxCall {
+  const void *w_in, *w_out;
+  int64_t num_in, num_nodes, num_pairs;
+  int32_t dim;
+  const int32_t *centers, *contexts;
+  const float* bias;
+  float scale, grad_scale;
+  float* loss;               // null: scores
+  void *g_in, *g_out;
+  float* scores;
+};
+enum { kLossOnly = 0, kForward = 1, kTableGrad = 2, kScores = 3 };
+
+// Sizes and places in the workspace (base null: sizes alone).
+struct SoftmaxPlan {
+  int padded;                // columns of a copied row: 64, 128 or 256
+  int64_t padded_pairs, pair_tiles, node_tiles;      // workgroups along the kept rows, either way
+  int splits, node_splits;                           // parts of the streamed rows
+  int64_t tiles_per_split, tiles_per_node_split;
+  void* rows;
+  int32_t* target;
+  float *lse2, *part_max, *part_acc;
+  double* part_sum;
+  size_t bytes;
+};
+template <typename E>
+SoftmaxPlan plan_softmax(void* ws, int64_t num_pairs, int64_t num_nodes, int32_t dim, bool loss, bool grad);
+template <typename E>
+int32_t run_softmax(const SoftmaxCall& call, const SoftmaxPlan& plan, hipStream_t stream);
+
+struct F32;
+struct BF16;
+struct F16;
+
+#if defined(GS_SOFTMAX_KERNELS)
+namespace {
+
+typedef float acc16 __attribute__((ext_vector_type(16)));
+typedef float vec4 __attribute__((ext_vector_type(4)));
+typedef float vec2 __attribute__((ext_vector_type(2)));
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef short short8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef _Float16 hf2 __attribute__((ext_vector_type(2)));
+typedef _Float16 hf8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) short4_t lds_short4;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr double kLn2 = 0.69314718055994530942;
+constexpr int kThreads = 256;
+
+__device__ uint4 zero_piece[1];                // never written
+
+__device__ __forceinline__ int64_t tiles_of(int64_t rows, int tile) { return (rows + tile - 1) / tile; }
+
+}  // namespace
+
+// Storage formats.  kShift: the powers of two by which probabilities are scaled before they are rounded to the format (undone
+// in fp32 afterwards): binary16 would lose those below 2^-24 otherwise; the scaled ones stay below 2^15.
+struct F32 {
+  typedef float elem;
+  static constexpr bool kWide = true;
+  static constexpr int kShift = 0;
+  static constexpr uint32_t kNan = 0x7fc00000u;
+  static __device__ __forceinline__ float load(const float* p) { return *p; }
+  static __device__ __forceinline__ void store4(float* p, vec4 v) { *reinterpret_cast<vec4*>(p) = v; }
+};
+struct BF16 {
+  typedef uint16_t elem;
+  static constexpr bool kWide = false;
+  static constexpr int kShift = 0;
+  static constexpr uint32_t kNan = 0x7fc07fc0u;
+  static __device__ __forceinline__ float load(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((vec2){lo, hi}, bf2));
+  }
+  static __device__ __forceinline__ acc16 mfma(vec4 a, vec4 b, acc16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ void store4(uint16_t* p, vec4 v) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack(v[0], v[1]), pack(v[2], v[3]));
+  }
+};
+struct F16 {
+  typedef uint16_t elem;
+  static constexpr bool kWide = false;
+  static constexpr int kShift = 14;
+  static constexpr uint32_t kNan = 0x7e007e00u;
+  static __device__ __forceinline__ float load(const uint16_t* p) { return __half2float(__ushort_as_half(*p)); }
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((vec2){lo, hi}, hf2));
+  }
+  static __device__ __forceinline__ acc16 mfma(vec4 a, vec4 b, acc16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(hf8, a), __builtin_bit_cast(hf8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ void store4(uint16_t* p, vec4 v) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack(v[0], v[1]), pack(v[2], v[3]));
+  }
+};
+
+namespace {
+
+// Tile shapes: kept rows per wave 32 * kNB, streamed rows per tile kTile.
+template <typename E, int DP>
+struct Shape {
+  static constexpr int kRowBytes = DP * (int)sizeof(typename E::elem);
+  static constexpr int kPieces = kRowBytes / 16;                   // 16-byte pieces of a row: 8, 16, 32 or 64
+  static constexpr int kPerPiece = 16 / (int)sizeof(typename E::elem);
+  static constexpr int kSteps = kPieces / 2;                       // pieces a half wave takes in the first product
+  static constexpr int kNB = (E::kWide || DP == 256) ? 1 : 2;
+  static constexpr int kTile = kRowBytes >= 1024 ? 32 : 64;
+  static constexpr int kBlocks = DP / 32;                          // 32-column blocks of the second product
+  static constexpr int kKept = 32 * kNB * 4;                       // kept rows per workgroup
+  static constexpr int kLoads = kTile * kPieces / kThreads;        // 16-byte loads per lane and tile
+};
+
+// Where a piece lies inside its row.  Reads of the first product take one piece of 32 consecutive rows, those of the second
+// four neighbouring pieces of four consecutive rows; both spread over all banks.
+template <int PIECES>
+__device__ __forceinline__ constexpr int swap_of(int row) {
+  return PIECES == 8 ? ((((row >> 1) & 1) << 2) | ((row >> 2) & 3)) : (((row & 3) << 2) | ((row >> 2) & 3));
+}
+
+__device__ __forceinline__ void load_piece_to_lds(const void* src, void* dst) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                   (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+}
+__device__ __forceinline__ void wait_loads_and_barrier() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+}
+
+// one step of the first product: 16 bytes of a streamed and of a kept row per lane
+template <typename E>
+__device__ __forceinline__ acc16 step(vec4 a, vec4 b, acc16 c) {
+  if constexpr (E::kWide) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[t], b[t], c, 0, 0, 0);
+    return c;
+  } else {
+    return E::mfma(a, b, c);
+  }
+}
+
+// ---- the pairs' rows, checked and copied -------------------------------------------------------------------------------
+// rows[i] = w_in[centers[i]], zero-padded to DP columns and to whole tiles; target[i] = context, or a negative word for a pair
+// without gradient: -1 left out (context -1), -2 an id that is no row, -3 the context is masked.  For scores (no contexts) a
+// centre that is no row gives a row of NaN.
+template <typename E>
+__global__ __launch_bounds__(kThreads) void gather_pairs_kernel(const typename E::elem* w_in, int64_t num_in, int64_t num_nodes,
+                                                                int dim, int padded, const int32_t* centers,
+                                                                const int32_t* contexts, const float* bias, int64_t num_pairs,
+                                                                int64_t padded_pairs, typename E::elem* rows, int32_t* target) {
+  constexpr int per = 16 / (int)sizeof(typename E::elem);
+  const int pieces = padded / per;
+  const int64_t total = padded_pairs * pieces;
+  for (int64_t s = (int64_t)blockIdx.x * kThreads + threadIdx.x; s < total; s += (int64_t)gridDim.x * kThreads) {
+    const int64_t i = s / pieces;
+    const int p = (int)(s - i * pieces);
+    int32_t t = -1;
+    int64_t c = 0;
+    if (i < num_pairs) {
+      c = centers[i];
+      t = contexts ? contexts[i] : 0;
+      if (c < 0 || c >= num_in || t < -1 || t >= num_nodes) t = -2;
+      else if (t >= 0 && contexts && bias && bias[t] == -INFINITY) t = -3;
+    }
+    if (p == 0 && target) target[i] = t;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (t >= 0 && p * per < dim) v = reinterpret_cast<const uint4*>(w_in)[(c * dim + p * per) / per];
+    if (t == -2 && !contexts) v = make_uint4(E::kNan, E::kNan, E::kNan, E::kNan);
+    reinterpret_cast<uint4*>(rows)[s] = v;
+  }
+}
+
+struct StreamArgs {
+  const void* kept;          // forward: the pairs' rows; table gradient: w_out
+  const void* streamed;      // the other one
+  int64_t kept_rows;         // rows that exist
+  int64_t streamed_rows;     // (the pairs' rows exist up to whole tiles)
+  int32_t dim;
+  float scale2;              // scale * log2(e); scores: scale
+  float out_scale;
+  const float* bias;         // [nodes] or null
+  const float* lse2;         // [pairs, whole tiles] base-2 log-sums (table gradient)
+  const int32_t* target;     // [pairs, whole tiles] (table gradient)
+  int64_t kept_tiles;        // workgroups along the kept rows
+  int32_t splits;
+  int64_t tiles_per_split;
+  float* part_max;           // forward: [splits][pairs]
+  double* part_sum;          // forward: [splits][pairs]
+  float* part_acc;           // [splits][kept_rows][DP], or null (table gradient without splits)
+  void* out;                 // table gradient without splits: g_out; scores: the scores
+};
+
+template <typename E, int DP, int MODE, bool BIAS>
+__global__ __launch_bounds__(kThreads, 1) void stream_kernel(StreamArgs a) {
+  using S = Shape<E, DP>;
+  using elem = typename E::elem;
+  constexpr int NB = S::kNB, TILE = S::kTile, ROWB = S::kRowBytes, PIECES = S::kPieces, KS = S::kSteps, DB = S::kBlocks;
+  constexpr bool NODES_STREAMED = MODE == kLossOnly || MODE == kForward;
+  constexpr bool SECOND = MODE == kForward || MODE == kTableGrad;
+  __shared__ __attribute__((aligned(1024))) char tile[2][TILE * ROWB];
+  __shared__ float side[2][TILE];              // nodes streamed: bias * log2(e); pairs streamed: base-2 log-sums
+  __shared__ int32_t side_target[2][TILE];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, l32 = lane & 31;
+  // workgroups of one split stream the same rows: they share an XCD (consecutive workgroups go round the eight of them)
+  int64_t kept_tile;
+  int split;
+  if (a.splits % 8 == 0) {
+    const int64_t q = blockIdx.x / 8;
+    split = (int)(blockIdx.x % 8 + 8 * (q / a.kept_tiles));
+    kept_tile = q % a.kept_tiles;
+  } else {
+    split = (int)(blockIdx.x / a.kept_tiles);
+    kept_tile = blockIdx.x % a.kept_tiles;
+  }
+  const int64_t all_tiles = tiles_of(a.streamed_rows, TILE);
+  const int64_t first = split * a.tiles_per_split;
+  const int64_t last = min(first + a.tiles_per_split, all_tiles);
+  const int64_t kept_row0 = kept_tile * S::kKept + wave * 32 * NB + l32;      // + 32 nb
+
+  // ---- kept rows into registers
+  vec4 kept[NB][KS];
+  float kept_bias[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int64_t row = kept_row0 + 32 * nb;
+    kept_bias[nb] = 0.0f;
+    bool live = true;
+    if (!NODES_STREAMED) {
+      live = row < a.kept_rows;
+      if (BIAS) {
+        kept_bias[nb] = live ? a.bias[row] * (MODE == kScores ? 1.0f : kLog2e) : -INFINITY;
+        live = live && kept_bias[nb] != -INFINITY;
+      }
+    }
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const int at = (2 * ks + half) * S::kPerPiece;
+      if (NODES_STREAMED) {
+        kept[nb][ks] = *reinterpret_cast<const vec4*>(static_cast<const elem*>(a.kept) + row * DP + at);
+      } else {
+        const bool read = live && at < a.dim;
+        const void* src = read ? static_cast<const void*>(static_cast<const elem*>(a.kept) + row * a.dim + at) : zero_piece;
+        kept[nb][ks] = *static_cast<const vec4*>(src);
+      }
+    }
+  }
+
+  // ---- staging: lane's loads go to slots wave * kLoads * 64 + 64 n + lane of a tile
+  float row_bias[S::kLoads];                   // nodes streamed, with bias: of the rows of the next tile to ask for
+  float side_value = 0.0f;
+  int32_t side_id = -1;
+  auto slot_row = [&](int n) { return ((wave * S::kLoads + n) * 64 + lane) / PIECES; };
+  auto fetch_bias = [&](int64_t t) {
+    if constexpr (NODES_STREAMED && BIAS) {
+#pragma unroll
+      for (int n = 0; n < S::kLoads; ++n) {
+        const int64_t row = t * TILE + slot_row(n);
+        row_bias[n] = row < a.streamed_rows ? a.bias[row] : -INFINITY;
+      }
+    }
+  };
+  auto issue = [&](int64_t t, int buf) {
+#pragma unroll
+    for (int n = 0; n < S::kLoads; ++n) {
+      const int r = slot_row(n);
+      const int piece = (lane % PIECES) ^ swap_of<PIECES>(r);
+      const int64_t row = t * TILE + r;
+      const elem* src;
+      if constexpr (NODES_STREAMED) {
+        bool read = row < a.streamed_rows && piece * S::kPerPiece < a.dim;
+        if constexpr (BIAS) read = read && row_bias[n] != -INFINITY;
+        src = read ? static_cast<const elem*>(a.streamed) + row * a.dim + piece * S::kPerPiece
+                   : reinterpret_cast<const elem*>(zero_piece);
+      } else {
+        src = static_cast<const elem*>(a.streamed) + row * DP + piece * S::kPerPiece;
+      }
+      load_piece_to_lds(src, &tile[buf][(wave * S::kLoads + n) * 1024]);
+    }
+    if (tid < TILE) {
+      const int64_t row = t * TILE + tid;
+      if constexpr (MODE == kTableGrad) {
+        side_value = a.lse2[row];
+        side_id = a.target[row];
+      } else if constexpr (NODES_STREAMED && BIAS) {
+        side_value = row < a.streamed_rows ? a.bias[row] * kLog2e : -INFINITY;
+      }
+    }
+  };
+  auto put_side = [&](int buf) {
+    if constexpr (MODE == kTableGrad || (NODES_STREAMED && BIAS)) {
+      if (tid < TILE) {
+        side[buf][tid] = side_value;
+        if constexpr (MODE == kTableGrad) side_target[buf][tid] = side_id;
+      }
+    }
+  };
+
+  acc16 out[SECOND ? DB : 1][NB];
+  if constexpr (SECOND) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) out[db][nb] = (acc16)0.0f;
+  }
+  float run_max[NB];
+  double run_sum[NB];                          // this half wave's streamed rows
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    run_max[nb] = -INFINITY;
+    run_sum[nb] = 0.0;
+  }
+
+  // lane's parts of the LDS addresses
+  const int read1 = l32 * ROWB + ((half ^ swap_of<PIECES>(l32)) << 4);
+  int read2;
+  if constexpr (E::kWide) {
+    read2 = (((l32 >> 2) ^ half) << 4) + (l32 & 3) * 4 + half * 4 * ROWB;
+  } else {
+    const int li = lane & 15, r = li >> 2;
+    constexpr int hi = PIECES == 8 ? 1 : 0;
+    const int turn = hi ? (((r >> 1) & 1) << 2) : (r << 2);
+    const int piece = (((lane >> 4) & 1) * 2 + ((li & 3) >> 1)) ^ turn ^ half;
+    read2 = (piece << 4) + (li & 1) * 8 + (4 * half + r) * ROWB;
+  }
+
+  if (first < last) {
+    fetch_bias(first);
+    issue(first, 0);
+    put_side(0);
+    if (first + 1 < last) fetch_bias(first + 1);
+  }
+  for (int64_t t = first; t < last; ++t) {
+    const int buf = (int)((t - first) & 1);
+    wait_loads_and_barrier();
+    if (t + 1 < last) {
+      issue(t + 1, buf ^ 1);
+      if (t + 2 < last) fetch_bias(t + 2);
+    }
+    const char* base = tile[buf];
+    // does any pair of this tile have its context among this wave's nodes?
+    bool any_target = false;
+    if constexpr (MODE == kTableGrad) {
+      const int64_t from = kept_tile * S::kKept + wave * 32 * NB;
+      const int64_t t_id = side_target[buf][lane % TILE];
+      any_target = __any(t_id >= from && t_id < from + 32 * NB);
+    }
+#pragma unroll
+    for (int jb = 0; jb < TILE / 32; ++jb) {
+      if (MODE == kScores && t * TILE + jb * 32 >= a.streamed_rows) break;
+      acc16 z[NB];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) z[nb] = (acc16)0.0f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const vec4 v = *reinterpret_cast<const vec4*>(base + (read1 ^ (ks << 5)) + jb * 32 * ROWB);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) z[nb] = step<E>(v, kept[nb][ks], z[nb]);
+      }
+      // ---- products to probabilities: register r holds streamed row 8 (r / 4) + 4 half + r % 4 of the block
+      if constexpr (NODES_STREAMED) {
+        if constexpr (BIAS) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const vec4 b = *reinterpret_cast<const vec4*>(&side[buf][jb * 32 + 8 * q + 4 * half]);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) z[nb][4 * q + e] = fmaf(z[nb][4 * q + e], a.scale2, b[e]);
+          }
+        } else if ((t + 1) * TILE > a.streamed_rows) {
+          const int64_t left = a.streamed_rows - t * TILE - jb * 32 - 4 * half;
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if (8 * (r / 4) + r % 4 >= left) z[nb][r] = -INFINITY;
+        }
+        bool moved = false;
+        float keep[NB];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          float m = z[nb][0];
+#pragma unroll
+          for (int r = 1; r < 16; ++r) m = fmaxf(m, z[nb][r]);
+          m = fmaxf(m, __shfl_xor(m, 32, 64));
+          if constexpr (!BIAS) m *= a.scale2;
+          const float next = fmaxf(run_max[nb], m);
+          moved = moved || next > run_max[nb];
+          const float from = next == -INFINITY ? 0.0f : next;       // nothing but masked nodes so far
+          keep[nb] = __builtin_amdgcn_exp2f(run_max[nb] - from);
+          run_max[nb] = next;
+          float sum = 0.0f;
+          const float add = (float)E::kShift - from;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float x = BIAS ? z[nb][r] + add : fmaf(z[nb][r], a.scale2, add);
+            z[nb][r] = __builtin_amdgcn_exp2f(x);
+            sum += z[nb][r];
+          }
+          run_sum[nb] = run_sum[nb] * (double)keep[nb] + (double)sum;
+        }
+        if constexpr (SECOND) {
+          if (__any(moved)) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+              for (int db = 0; db < DB; ++db) out[db][nb] *= keep[nb];
+          }
+        }
+      } else if constexpr (MODE == kScores) {
+        const int64_t pair0 = t * TILE + jb * 32 + 4 * half;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          const int64_t node = kept_row0 + 32 * nb;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int64_t pair = pair0 + 8 * (r / 4) + r % 4;
+            if (node < a.kept_rows && pair < a.streamed_rows)
+              static_cast<float*>(a.out)[pair * a.kept_rows + node] =
+                  BIAS ? fmaf(z[nb][r], a.scale2, kept_bias[nb]) : z[nb][r] * a.scale2;
+          }
+        }
+      } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const vec4 l = *reinterpret_cast<const vec4*>(&side[buf][jb * 32 + 8 * q + 4 * half]);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float add = BIAS ? kept_bias[nb] - l[e] : -l[e];
+              z[nb][4 * q + e] = __builtin_amdgcn_exp2f(fmaf(z[nb][4 * q + e], a.scale2, add));
+            }
+        }
+        if (any_target) {
+          constexpr float one = E::kShift ? 16384.0f : 1.0f;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int32_t t_id = side_target[buf][jb * 32 + 8 * (r / 4) + 4 * half + r % 4];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+              if (t_id == (int32_t)(kept_row0 + 32 * nb)) z[nb][r] -= one;
+          }
+        }
+      }
+      // ---- second product
+      if constexpr (SECOND) {
+        if constexpr (E::kWide) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+              const int turn = (db * 8) ^ ((r % 4) << 2) ^ (2 * ((r / 4) & 1));
+              const float v = *reinterpret_cast<const float*>(base + (read2 ^ (turn << 4)) + (jb * 32 + 8 * (r / 4) + r % 4) * ROWB);
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) out[db][nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, z[nb][r], out[db][nb], 0, 0, 0);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int q2 = 0; q2 < 2; ++q2) {
+            vec4 p[NB];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                p[nb][e] = __uint_as_float(E::pack(z[nb][8 * q2 + 2 * e], z[nb][8 * q2 + 2 * e + 1]));
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+              short4_t part[2];
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const int q = 2 * q2 + e;
+                const int turn = (db * 4) ^ (2 * (q & 1));
+                part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds_short4*)(base + (read2 ^ (turn << 4)) + (jb * 32 + 8 * q) * ROWB));
+              }
+              const vec4 v = __builtin_bit_cast(vec4, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) out[db][nb] = E::mfma(v, p[nb], out[db][nb]);
+            }
+          }
+        }
+      }
+    }
+    if (t + 1 < last) put_side(buf ^ 1);
+  }
+
+  // ---- results: lane's kept row, register r of block db is column 32 db + 8 (r / 4) + 4 half + r % 4
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int64_t row = kept_row0 + 32 * nb;
+    if constexpr (NODES_STREAMED) {
+      const double sum = run_sum[nb] + __shfl_xor(run_sum[nb], 32, 64);
+      if (row < a.kept_rows && half == 0) {
+        a.part_max[split * a.kept_rows + row] = run_max[nb];
+        a.part_sum[split * a.kept_rows + row] = sum;
+      }
+    }
+    if constexpr (SECOND) {
+      if (row < a.kept_rows) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int col = 32 * db + 8 * q + 4 * half;
+            vec4 v = {out[db][nb][4 * q], out[db][nb][4 * q + 1], out[db][nb][4 * q + 2], out[db][nb][4 * q + 3]};
+            if (MODE == kTableGrad && a.part_acc == nullptr) {
+              if (col < a.dim) E::store4(static_cast<elem*>(a.out) + row * a.dim + col, v * a.out_scale);
+            } else {
+              *reinterpret_cast<vec4*>(a.part_acc + (split * a.kept_rows + row) * DP + col) = v;
+            }
+          }
+      }
+    }
+  }
+}
+
+// ---- joining the parts of the forward pass: one wave per pair -----------------------------------------------------------
+template <typename E>
+__global__ __launch_bounds__(kThreads) void join_pairs_kernel(const typename E::elem* rows, const typename E::elem* w_out, int dim,
+                                                              int padded, const float* bias, float scale, float out_scale,
+                                                              int64_t num_pairs, int64_t padded_pairs, int splits,
+                                                              const float* part_max, const double* part_sum,
+                                                              const float* part_acc, int32_t* target, float* loss, float* lse2,
+                                                              typename E::elem* g_in) {
+  const int lane = threadIdx.x & 63;
+  const int64_t i = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  if (i >= padded_pairs) return;
+  const int32_t t = target[i];
+  float m = -INFINITY;
+  double sum = 0.0;
+  if (i < num_pairs) {
+    for (int s = lane; s < splits; s += 64) m = fmaxf(m, part_max[s * num_pairs + i]);
+#pragma unroll
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+    for (int s = lane; s < splits; s += 64) {
+      const float pm = part_max[s * num_pairs + i];
+      const double ps = part_sum[s * num_pairs + i];
+      // a split of masked nodes alone has sum 0, whatever its maximum
+      sum += pm == -INFINITY && ps == 0.0 ? 0.0 : ps * exp2((double)pm - (double)m);
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d, 64);
+  }
+  const double total2 = (double)m + log2(sum) - (double)E::kShift;         // base-2 log-sum
+  const bool live = i < num_pairs && t >= 0;
+  if (lse2 != nullptr && lane == 0) lse2[i] = live ? (float)(total2 - (double)E::kShift) : INFINITY;
+  if (i >= num_pairs) return;
+  const typename E::elem* c = w_out + (int64_t)max(t, 0) * dim;
+  double dot = 0.0;
+  if (live)
+    for (int d = lane; d < dim; d += 64) dot += (double)E::load(rows + i * padded + d) * (double)E::load(c + d);
+#pragma unroll
+  for (int d = 32; d; d >>= 1) dot += __shfl_xor(dot, d, 64);
+  if (lane == 0) {
+    double value = total2 * kLn2 - ((double)scale * dot + (live && bias ? (double)bias[t] : 0.0));
+    if (t == -1) value = 0.0;
+    if (t == -2) value = NAN;
+    if (t == -3) value = INFINITY;
+    loss[i] = (float)value;
+  }
+  if (g_in == nullptr) return;
+  const double inverse = 1.0 / sum;
+  for (int d0 = 4 * lane; d0 < dim; d0 += 256) {
+    vec4 g = (vec4)0.0f;
+    if (live) {
+      for (int s = 0; s < splits; ++s) {
+        const float pm = part_max[s * num_pairs + i];
+        if (pm == -INFINITY && part_sum[s * num_pairs + i] == 0.0) continue;       // masked nodes alone
+        const float w = (float)(exp2((double)pm - (double)m) * inverse);
+        g += w * *reinterpret_cast<const vec4*>(part_acc + (s * num_pairs + i) * padded + d0);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) g[e] = (g[e] - E::load(c + d0 + e)) * out_scale;
+    }
+    E::store4(g_in + i * dim + d0, g);
+  }
+}
+
+// g_out from the parts of a split table gradient, in order
+template <typename E>
+__global__ __launch_bounds__(kThreads) void join_nodes_kernel(const float* part_acc, int64_t num_nodes, int dim, int padded,
+                                                              int splits, float out_scale, typename E::elem* g_out) {
+  const int quads = dim / 4;
+  const int64_t total = num_nodes * quads;
+  for (int64_t s = (int64_t)blockIdx.x * kThreads + threadIdx.x; s < total; s += (int64_t)gridDim.x * kThreads) {
+    const int64_t row = s / quads;
+    const int d0 = 4 * (int)(s - row * quads);
+    vec4 g = (vec4)0.0f;
+    for (int k = 0; k < splits; ++k) g += *reinterpret_cast<const vec4*>(part_acc + (k * num_nodes + row) * padded + d0);
+    E::store4(g_out + row * dim + d0, g * out_scale);
+  }
+}
+
+// no pairs: every gradient is zero
+__global__ __launch_bounds__(kThreads) void zero_pieces_kernel(uint4* to, int64_t pieces) {
+  for (int64_t s = (int64_t)blockIdx.x * kThreads + threadIdx.x; s < pieces; s += (int64_t)gridDim.x * kThreads)
+    to[s] = make_uint4(0, 0, 0, 0);
+}
+
+}  // namespace
+
+// ---- host ----------------------------------------------------------------------------------------------------------------
+template <typename E, int DP>
+static void plan_tiles(SoftmaxPlan& p, int64_t num_pairs, int64_t num_nodes, bool grad, size_t& acc_rows, size_t& part_rows) {
+  using S = Shape<E, DP>;
+  constexpr int64_t want = 512;                // workgroups that fill the chip: two per compute unit
+  p.padded = DP;
+  p.padded_pairs = ceil_div(num_pairs, 256) * 256;
+  p.pair_tiles = ceil_div(num_pairs, S::kKept);
+  p.node_tiles = ceil_div(num_nodes, S::kKept);
+  const int64_t tiles = ceil_div(num_nodes, S::kTile), pair_parts = ceil_div(num_pairs, S::kTile);
+  auto split = [&](int64_t kept, int64_t streamed) {
+    int64_t n = std::max<int64_t>(1, std::min(streamed, want / std::max<int64_t>(1, kept)));
+    return (int)(n >= 8 ? n / 8 * 8 : n);
+  };
+  p.splits = split(p.pair_tiles, tiles);
+  p.tiles_per_split = ceil_div(tiles, p.splits);
+  p.node_splits = split(p.node_tiles, pair_parts);
+  p.tiles_per_node_split = ceil_div(std::max<int64_t>(1, pair_parts), p.node_splits);
+  // every size below only grows with the number of pairs, although the number of splits falls
+  part_rows = (size_t)std::max(num_pairs, std::min(std::min(tiles, want) * num_pairs, want * S::kKept));
+  acc_rows = grad ? part_rows : 0;
+  if (grad && p.node_splits > 1) acc_rows = std::max(acc_rows, (size_t)p.node_splits * (size_t)num_nodes);
+}
+
+template <typename E>
+SoftmaxPlan plan_softmax(void* ws, int64_t num_pairs, int64_t num_nodes, int32_t dim, bool loss, bool grad) {
+  SoftmaxPlan p{};
+  size_t acc_rows = 0, part_rows = 0;
+  if (dim <= 64) plan_tiles<E, 64>(p, num_pairs, num_nodes, grad, acc_rows, part_rows);
+  else if (dim <= 128) plan_tiles<E, 128>(p, num_pairs, num_nodes, grad, acc_rows, part_rows);
+  else plan_tiles<E, 256>(p, num_pairs, num_nodes, grad, acc_rows, part_rows);
+  Carver c(ws);
+  p.rows = c.take<typename E::elem>((size_t)p.padded_pairs * p.padded);
+  if (loss) {
+    p.target = c.take<int32_t>(p.padded_pairs);
+    p.lse2 = c.take<float>(p.padded_pairs);
+    p.part_max = c.take<float>(part_rows);
+    p.part_sum = c.take<double>(part_rows);
+    p.part_acc = c.take<float>(acc_rows * p.padded);
+  }
+  p.bytes = c.used;
+  return p;
+}
+
+template <typename E, int DP, int MODE>
+static int32_t launch_stream(const StreamArgs& a, hipStream_t stream) {
+  const int64_t groups = a.kept_tiles * a.splits;
+  if (a.bias) stream_kernel<E, DP, MODE, true><<<(unsigned)groups, kThreads, 0, stream>>>(a);
+  else stream_kernel<E, DP, MODE, false><<<(unsigned)groups, kThreads, 0, stream>>>(a);
+  GS_LAUNCH_CHECK();
+  return GS_OK;
+}
+
+template <typename E, int DP>
+static int32_t run_padded(const SoftmaxCall& q, const SoftmaxPlan& p, hipStream_t stream) {
+  using elem = typename E::elem;
+  elem* rows = static_cast<elem*>(p.rows);
+  constexpr int64_t most = ((int64_t)1 << 32) / kThreads;        // a launch takes fewer than 2^32 lanes
+  if ((!q.loss || q.g_out) && p.node_tiles * p.node_splits >= most) return GS_EOVERFLOW;
+  if (q.loss && p.pair_tiles * p.splits >= most) return GS_EOVERFLOW;
+  auto blocks_for = [](int64_t items) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(items, kThreads), 256 * 16)); };
+  gather_pairs_kernel<E><<<blocks_for(p.padded_pairs * (DP / (16 / (int)sizeof(elem)))), kThreads, 0, stream>>>(
+      static_cast<const elem*>(q.w_in), q.num_in, q.num_nodes, q.dim, DP, q.centers, q.contexts, q.bias, q.num_pairs,
+      p.padded_pairs, rows, q.loss ? p.target : nullptr);
+  GS_LAUNCH_CHECK();
+  StreamArgs a{};
+  a.dim = q.dim;
+  a.bias = q.bias;
+  if (!q.loss) {
+    a.kept = q.w_out;
+    a.streamed = rows;
+    a.kept_rows = q.num_nodes;
+    a.streamed_rows = q.num_pairs;
+    a.scale2 = q.scale;
+    a.kept_tiles = p.node_tiles;
+    a.splits = p.node_splits;
+    a.tiles_per_split = p.tiles_per_node_split;
+    a.out = q.scores;
+    return launch_stream<E, DP, kScores>(a, stream);
+  }
+  a.kept = rows;
+  a.streamed = q.w_out;
+  a.kept_rows = q.num_pairs;
+  a.streamed_rows = q.num_nodes;
+  a.scale2 = q.scale * kLog2e;
+  a.kept_tiles = p.pair_tiles;
+  a.splits = p.splits;
+  a.tiles_per_split = p.tiles_per_split;
+  a.part_max = p.part_max;
+  a.part_sum = p.part_sum;
+  a.part_acc = p.part_acc;
+  int32_t rc = q.g_in ? launch_stream<E, DP, kForward>(a, stream) : launch_stream<E, DP, kLossOnly>(a, stream);
+  if (rc != GS_OK) return rc;
+  const float out_scale = q.scale * q.grad_scale;
+  join_pairs_kernel<E><<<(unsigned)ceil_div(p.padded_pairs, kThreads / 64), kThreads, 0, stream>>>(
+      rows, static_cast<const elem*>(q.w_out), q.dim, DP, q.bias, q.scale, out_scale, q.num_pairs, p.padded_pairs, p.splits,
+      p.part_max, p.part_sum, p.part_acc, p.target, q.loss, q.g_out ? p.lse2 : nullptr, static_cast<elem*>(q.g_in));
+  GS_LAUNCH_CHECK();
+  if (!q.g_out) return GS_OK;
+  a.kept = q.w_out;
+  a.streamed = rows;
+  a.kept_rows = q.num_nodes;
+  a.streamed_rows = q.num_pairs;
+  a.lse2 = p.lse2;
+  a.target = p.target;
+  a.kept_tiles = p.node_tiles;
+  a.splits = p.node_splits;
+  a.tiles_per_split = p.tiles_per_node_split;
+  a.out_scale = out_scale / (float)(1 << E::kShift);
+  a.part_acc = p.node_splits > 1 ? p.part_acc : nullptr;
+  a.out = q.g_out;
+  rc = launch_stream<E, DP, kTableGrad>(a, stream);
+  if (rc != GS_OK || p.node_splits == 1) return rc;
+  join_nodes_kernel<E><<<blocks_for(q.num_nodes * (q.dim / 4)), kThreads, 0, stream>>>(
+      p.part_acc, q.num_nodes, q.dim, DP, p.node_splits, a.out_scale, static_cast<elem*>(q.g_out));
+  GS_LAUNCH_CHECK();
+  return GS_OK;
+}
+
+template <typename E>
+int32_t run_softmax(const SoftmaxCall& q, const SoftmaxPlan& p, hipStream_t stream) {
+  if (q.num_pairs == 0) {
+    if (!q.g_out) return GS_OK;
+    const int64_t pieces = q.num_nodes * q.dim * (int64_t)sizeof(typename E::elem) / 16;
+    zero_pieces_kernel<<<(unsigned)std::min<int64_t>(ceil_div(pieces, kThreads), 256 * 16), kThreads, 0, stream>>>(static_cast<uint4*>(q.g_out), pieces);
+    GS_LAUNCH_CHECK();
+    return GS_OK;
+  }
+  if (p.padded == 64) return run_padded<E, 64>(q, p, stream);
+  if (p.padded == 128) return run_padded<E, 128>(q, p, stream);
+  return run_padded<E, 256>(q, p, stream);
+}
+
+#endif  // GS_SOFTMAX_KERNELS
+
+}  // namespace gs
