@@ -29,7 +29,8 @@ HIPCC_FLAGS = [
 # Files whose kernels take sampling decisions that must match the CPU reference bit for bit
 # (one multiply, one compare per decision): no fused multiply-add may ever be formed there.
 # sgns.hip keeps contraction on (its only bit-exact part, the negative draws, is a compare).
-NO_CONTRACTION = {"walk.hip", "pairs_negs.hip", "alias_build.hip", "csr_build.hip"}
+# choose.hip sorts scores into steps in several kernels, which have to agree.
+NO_CONTRACTION = {"walk.hip", "pairs_negs.hip", "alias_build.hip", "csr_build.hip", "choose.hip"}
 
 
 def hipcc() -> str:

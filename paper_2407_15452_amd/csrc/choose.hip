@@ -4,24 +4,33 @@
 //   top-k: the first k;  top-p: those of them with sum of e before < top_p * sum of e;  min-p: e_j >= min_p
 //   answer: the smallest index j with  sum_{i <= j, kept} e_i > u * sum_{kept} e
 //
-// Nothing is sorted.  A score becomes a 32-bit key of the same order; what the first two filters keep is then "keys above a
-// cut, and the first `ties` of those equal to it", and a cut is found by histograms: the first over 2048 equal steps of the
-// score between the row's least and greatest (scores spread over them; over the bits of a float they would not), the next
-// ones over 2048 steps of the key inside the bin that holds the cut, until a bin is a single key.  At most four histograms
-// for any 32-bit keys, two for usual scores.  Weights are added as integers (multiples of 2^-62, in two halves of 31 bits), so
-// neither the order of the atomics nor the shape of the launch changes a sum; the choice itself adds fp64 weights in a fixed
-// order.  Comparisons near a border are why nothing here is fp32: an error of 1e-7 of the sum would move the answer to a
-// neighbour for one row in ten at a million nodes.
+// The row is never sorted.  A score becomes a 32-bit key of the same order, and a histogram over 2048 equal steps of the score
+// between the row's least and greatest (scores spread over them; over the bits of a float they would not) says in which step
+// the cut of top-k or top-p lies.  With top-k the nodes from that step up go to a short list, which is sorted and holds all
+// there is to decide; with top-p alone only that step's nodes do, while the weights of those above are added by pieces of the
+// index, so that the answer is looked for in one piece.  Weights are added as integers (multiples of 2^-62, in two halves of 31
+// bits): neither the order of the atomics nor the shape of the launch changes a sum.  Comparisons near a border are why nothing
+// here is fp32: an error of 1e-7 of the sum would move the answer to a neighbour for one row in ten at a million nodes.
+//
+// A list that would be too long (thousands of nodes of one step: k in the thousands, or equal scores) is not made: histograms of
+// the key inside the step, and of the index among equal keys, go down to the cut instead, over the whole row each time.
+//
+// Two routes.  Row by row: one workgroup does all of it.  Split: where rows are long and fewer than the compute units need,
+// three passes over the scores by several workgroups a row (least and greatest; histogram; list and pieces), and one workgroup
+// a row finishes.
 
 #include "common.h"
 
 namespace gs {
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / 64;
 constexpr int kBins = 2048;
-constexpr int kLdsKeys = 24 * 1024;            // keys of a row that fits LDS next to the histogram
+constexpr int kAhead = 4;                      // 16-byte loads per lane in flight
+constexpr int kListMost = kBins;               // elements of a row that may go to its list
+constexpr int kSplitGroups = 2048;             // of one launch: eight per compute unit
+constexpr int kSplitLeast = 8192;              // scores per workgroup at least
 
 struct SampleArgs {
   const void* scores;
@@ -55,6 +64,23 @@ __device__ __forceinline__ float score_of(uint32_t key) {
   return __uint_as_float((key >> 31) ? (key & 0x7fffffffu) : ~key);
 }
 
+// A row's parameters, as the filters see them.
+struct RowLimits {
+  float temperature, top_p;
+  double min_p, u;
+  int64_t k;
+  bool by_k, by_p;
+  __device__ __forceinline__ RowLimits(const SampleArgs& a, int64_t r) {
+    temperature = a.temperature ? a.temperature[r] : 1.0f;
+    k = a.top_k ? a.top_k[r] : 0;
+    top_p = a.top_p ? a.top_p[r] : 1.0f;
+    min_p = a.min_p && a.min_p[r] > 0.0f ? fmin((double)a.min_p[r], 1.0) : 0.0;
+    u = a.uniforms[r] < 0.0f ? 0.0 : (double)a.uniforms[r];       // NaN stays: no sum passes it
+    by_k = k > 0 && k < a.n;
+    by_p = top_p < 1.0f;
+  }
+};
+
 struct Weigh {
   float top;
   double inverse;                              // of the temperature
@@ -73,62 +99,130 @@ struct Sum {
     const uint64_t h = hi + (lo >> 31), l = lo & 0x7fffffffu;
     return h < (1ull << 53) ? ((double)h * 0x1p31 + (double)l) * 0x1p-62 : (double)h * 0x1p-31;
   }
+  __device__ __forceinline__ bool same_weight(const Sum& b) const {
+    return hi + (lo >> 31) == b.hi + (b.lo >> 31) && ((lo ^ b.lo) & 0x7fffffffu) == 0;
+  }
 };
 __device__ __forceinline__ Sum operator+(const Sum& a, const Sum& b) { return Sum{a.count + b.count, a.hi + b.hi, a.lo + b.lo}; }
 __device__ __forceinline__ Sum operator-(const Sum& a, const Sum& b) { return Sum{a.count - b.count, a.hi - b.hi, a.lo - b.lo}; }
+__device__ __forceinline__ uint64_t units_of(double weight) { return (uint64_t)(weight * 0x1p62); }
 
 struct Histogram {
   uint32_t count[kBins];
   unsigned long long hi[kBins], lo[kBins];
 };
-
-// 2048 equal steps between the row's least and greatest finite score
-struct Steps {
-  double least, inverse;
-  __device__ __forceinline__ Steps(uint32_t kmin, uint32_t kmax) {
-    const double greatest = fmin((double)score_of(kmax), 3.4028234663852886e38);
-    least = fmin((double)score_of(kmin), 3.4028234663852886e38);
-    inverse = greatest > least ? (kBins - 1) / (greatest - least) : 0.0;
-  }
-  __device__ __forceinline__ int operator()(uint32_t key) const {
-    const double d = fmin((double)score_of(key), 3.4028234663852886e38) - least;
-    return (int)fmin(d * inverse, (double)(kBins - 1));
-  }
-};
-
-struct Cut {                                   // kept: keys above, and the first `ties` of those equal to it
-  uint32_t key;
-  uint64_t ties;
-  bool all_ties;
-  Sum above;
-};
-
-struct Shared {
-  Histogram hist;
-  Sum wave_sum[kWaves];
-  double wave_weight[kWaves];
-  uint64_t wave_index[kWaves];
-  Sum found_above, found_in;
-  int found_bin;
-  uint32_t kmin, kmax;
-};
-
-template <typename V>
-struct RowSource {
-  const typename V::elem* row;
-  const uint32_t* keys;                        // LDS copy, or null
-  int64_t n;
-  __device__ __forceinline__ uint32_t operator()(int64_t j) const { return keys ? keys[j] : key_of(V::get(row[j])); }
-};
-
-__device__ __forceinline__ Sum shfl_up_sum(const Sum& s, int d) {
-  return Sum{(uint64_t)__shfl_up((unsigned long long)s.count, d, 64), (uint64_t)__shfl_up((unsigned long long)s.hi, d, 64),
-             (uint64_t)__shfl_up((unsigned long long)s.lo, d, 64)};
+__device__ __forceinline__ void add_to(Histogram& h, int b, bool weights, double weight) {
+  atomicAdd(&h.count[b], 1u);
+  if (!weights) return;
+  const uint64_t w = units_of(weight);
+  if (w == 0) return;
+  atomicAdd(&h.hi[b], (unsigned long long)(w >> 31));
+  atomicAdd(&h.lo[b], (unsigned long long)(w & 0x7fffffffu));
 }
 
-// The first bin from above at which `reached(sum of everything above and the bin)` holds; found_bin -1 if none does.
+// 2048 equal steps between the row's least and greatest finite score.  fp32: every operation is monotone, which is all that a
+// cut needs (this file is compiled without contraction: each pass has to find a score in the same step).  Halves, so that the
+// distance of two floats is one.
+struct Steps {
+  float least, inverse;
+  static __device__ __forceinline__ float half_of(uint32_t key) { return fminf(score_of(key), 3.4028234663852886e38f) * 0.5f; }
+  __device__ __forceinline__ Steps(uint32_t kmin, uint32_t kmax) {
+    least = half_of(kmin);
+    const float range = half_of(kmax) - least;
+    inverse = range > 0.0f ? fminf((float)(kBins - 1) / range, 3.4028234663852886e38f) : 0.0f;
+  }
+  __device__ __forceinline__ int operator()(uint32_t key) const {
+    return (int)fminf((half_of(key) - least) * inverse, (float)(kBins - 1));
+  }
+};
+// The first of the keys [lo, hi] for which `yes` holds, once it holds for hi and for every key after such a one: 64 keys at a time.
+template <typename Yes>
+__device__ __forceinline__ uint32_t first_key(uint32_t lo, uint32_t hi, Yes yes) {
+  const uint32_t lane = threadIdx.x & 63;
+  while (lo < hi) {
+    const uint32_t part = (hi - lo) / 64 + 1;
+    const uint64_t at = (uint64_t)lo + (uint64_t)part * lane;      // lane 0: lo itself
+    const uint64_t no = __ballot(at <= hi && !yes((uint32_t)min(at, (uint64_t)hi)));
+    if (no == 0) return lo;
+    const uint32_t last = 63 - __clzll((long long)no);             // the last key asked for that it does not hold for
+    hi = (uint32_t)min((uint64_t)hi, (uint64_t)lo + (uint64_t)part * (last + 1));
+    lo = lo + part * last + 1;
+  }
+  return lo;
+}
+// the keys of steps from .. to, among [kmin, kmax]; both steps hold a key
+__device__ __forceinline__ void keys_of_steps(const Steps& steps, int from, int to, uint32_t kmin, uint32_t kmax, uint32_t& lo, uint32_t& hi) {
+  lo = first_key(kmin, kmax, [=](uint32_t key) { return steps(key) >= from; });
+  hi = steps(kmax) <= to ? kmax : first_key(lo, kmax, [=](uint32_t key) { return steps(key) > to; }) - 1;
+}
+
+struct ListShared {
+  uint32_t list_count, list_base;
+  uint64_t list[kListMost];                    // ~key in the high half, index in the low one: sorts by the order of the nodes
+};
+struct Shared : ListShared {
+  Histogram hist;
+  Sum wave_sum[kWaves];
+  Sum found_above, found_in;
+  int found_bin;
+};
+
+// A row in 16-byte pieces: position = index + skew, so that pieces lie on 16-byte boundaries wherever the row begins.  The first
+// and the last piece are read element by element where they reach beyond the row.
+template <typename V>
+struct Row {
+  typedef typename V::elem elem;
+  static constexpr uint32_t kPer = 16 / sizeof(elem);
+  const elem* base;                            // 16-byte aligned, skew elements in front of the row
+  uint32_t skew, n;
+  __device__ __forceinline__ Row(const void* scores, int64_t r, int64_t n_) {
+    const elem* row = static_cast<const elem*>(scores) + r * n_;
+    skew = (uint32_t)(((uintptr_t)row & 15) / sizeof(elem));
+    base = row - skew;
+    n = (uint32_t)n_;
+  }
+  __device__ __forceinline__ uint32_t pieces() const { return (n + skew + kPer - 1) / kPer; }
+  __device__ __forceinline__ void load(uint32_t piece, uint32_t* key) const {        // 0 beyond the row
+    const uint32_t at = piece * kPer;
+    elem e[kPer];
+    if (at >= skew && at + kPer <= n + skew) {
+      const uint4 w = *reinterpret_cast<const uint4*>(base + at);
+      __builtin_memcpy(e, &w, 16);
+#pragma unroll
+      for (uint32_t k = 0; k < kPer; ++k) key[k] = key_of(V::get(e[k]));
+    } else {
+#pragma unroll
+      for (uint32_t k = 0; k < kPer; ++k) key[k] = at + k >= skew && at + k < n + skew ? key_of(V::get(base[at + k])) : 0;
+    }
+  }
+};
+// visit(index, key) for the valid elements of the pieces from .. to, by `threads` lanes of which this is number `lane`
+template <int AHEAD, typename V, typename Visit>
+__device__ __forceinline__ void for_row(const Row<V>& row, uint32_t from, uint32_t to, uint32_t lane, uint32_t threads, Visit visit) {
+  constexpr uint32_t per = Row<V>::kPer;
+  for (uint32_t p0 = from + lane; p0 < to; p0 += AHEAD * threads) {
+    uint32_t key[AHEAD][per];
+#pragma unroll
+    for (int e = 0; e < AHEAD; ++e) {
+      if (p0 + e * threads < to) row.load(p0 + e * threads, key[e]);
+      else
+#pragma unroll
+        for (uint32_t k = 0; k < per; ++k) key[e][k] = 0;
+    }
+#pragma unroll
+    for (int e = 0; e < AHEAD; ++e)
+#pragma unroll
+      for (uint32_t k = 0; k < per; ++k)
+        if (key[e][k] != 0) visit((p0 + e * threads) * per + k - row.skew, key[e][k]);
+  }
+}
+
+__device__ __forceinline__ uint64_t shfl_up64(uint64_t v, int d) { return (uint64_t)__shfl_up((unsigned long long)v, d, 64); }
+
+// The first bin from above at which `reached(sum of everything above and the bin)` holds, into sh.found_*; found_bin -1 if none
+// does.  Returns the sum of all bins.
 template <typename Reached>
-__device__ void find_bin(Shared& sh, const Sum& above, bool weights, Reached reached) {
+__device__ Sum find_bin(Shared& sh, const Sum& above, bool weights, Reached reached) {
   constexpr int per = kBins / kThreads;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   Sum own[per], total{0, 0, 0};
@@ -141,14 +235,28 @@ __device__ void find_bin(Shared& sh, const Sum& above, bool weights, Reached rea
   Sum upto = total;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const Sum up = shfl_up_sum(upto, d);
-    if (lane >= d) upto = upto + up;
+    const uint32_t c = __shfl_up((uint32_t)upto.count, d, 64);   // counts of one row: below 2^31
+    if (lane >= d) upto.count += c;
+  }
+  if (weights) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint64_t h = shfl_up64(upto.hi, d), l = shfl_up64(upto.lo, d);
+      if (lane >= d) {
+        upto.hi += h;
+        upto.lo += l;
+      }
+    }
   }
   if (lane == 63) sh.wave_sum[wave] = upto;
   if (tid == 0) sh.found_bin = -1;
   __syncthreads();
-  Sum before = above;
-  for (int w = 0; w < wave; ++w) before = before + sh.wave_sum[w];
+  Sum before = above, everything{0, 0, 0};
+  for (int w = 0; w < kWaves; ++w) {
+    const Sum s = sh.wave_sum[w];
+    if (w < wave) before = before + s;
+    everything = everything + s;
+  }
   before = before + (upto - total);
 #pragma unroll
   for (int k = 0; k < per; ++k) {
@@ -161,10 +269,10 @@ __device__ void find_bin(Shared& sh, const Sum& above, bool weights, Reached rea
     before = with;
   }
   __syncthreads();
+  return everything;
 }
 
-template <typename Source, typename Bin>
-__device__ void fill_histogram(Shared& sh, const Source& source, uint32_t lo, uint32_t hi, bool weights, const Weigh& weigh, Bin bin) {
+__device__ void clear_histogram(Shared& sh, bool weights) {
   for (int b = threadIdx.x; b < kBins; b += kThreads) {
     sh.hist.count[b] = 0;
     if (weights) {
@@ -173,43 +281,25 @@ __device__ void fill_histogram(Shared& sh, const Source& source, uint32_t lo, ui
     }
   }
   __syncthreads();
-  for (int64_t j = threadIdx.x; j < source.n; j += kThreads) {
-    const uint32_t key = source(j);
-    if (key == 0 || key < lo || key > hi) continue;
-    const int b = bin(key);
-    atomicAdd(&sh.hist.count[b], 1u);
-    if (weights) {
-      const uint64_t w = (uint64_t)(weigh(key) * 0x1p62);
-      if (w) {
-        atomicAdd(&sh.hist.hi[b], (unsigned long long)(w >> 31));
-        atomicAdd(&sh.hist.lo[b], (unsigned long long)(w & 0x7fffffffu));
-      }
-    }
-  }
+}
+
+// ---- the long way: histograms over the whole row down to the cut
+template <typename V, typename Bin>
+__device__ void fill_by_key(Shared& sh, const Row<V>& row, uint32_t lo, uint32_t hi, bool weights, const Weigh& weigh, Bin bin) {
+  clear_histogram(sh, weights);
+  for_row<1>(row, 0, row.pieces(), threadIdx.x, kThreads, [&](uint32_t, uint32_t key) {
+    if (key >= lo && key <= hi) add_to(sh.hist, bin(key), weights, weights ? weigh(key) : 0.0);
+  });
   __syncthreads();
 }
 
 // From the bin that find_bin left (of the histogram over `steps`) down to a single key.  false: no cut, everything is kept.
-template <typename Source, typename Reached>
-__device__ bool narrow(Shared& sh, const Source& source, const Steps& steps, uint32_t kmin, uint32_t kmax, bool weights,
+template <typename V, typename Reached>
+__device__ bool narrow(Shared& sh, const Row<V>& row, const Steps& steps, uint32_t kmin, uint32_t kmax, bool weights,
                        const Weigh& weigh, Reached reached, uint32_t& cut, Sum& above, Sum& in) {
   if (sh.found_bin < 0) return false;
-  const int bin = sh.found_bin;
-  uint32_t lo = kmin, hi = kmax;
-  {                                            // the keys of that bin: [first with steps >= bin, last with steps <= bin]
-    uint32_t a = kmin, b = kmax;
-    while (a < b) {
-      const uint32_t mid = a + ((b - a) >> 1);
-      if (steps(mid) >= bin) b = mid; else a = mid + 1;
-    }
-    lo = a;
-    b = kmax;
-    while (a < b) {
-      const uint32_t mid = b - ((b - a) >> 1);
-      if (steps(mid) <= bin) a = mid; else b = mid - 1;
-    }
-    hi = a;
-  }
+  uint32_t lo, hi;
+  keys_of_steps(steps, sh.found_bin, sh.found_bin, kmin, kmax, lo, hi);
   above = sh.found_above;
   in = sh.found_in;
   __syncthreads();
@@ -217,9 +307,9 @@ __device__ bool narrow(Shared& sh, const Source& source, const Steps& steps, uin
     const int bits = 32 - __clz(hi - lo);
     const int shift = bits > 11 ? bits - 11 : 0;
     const uint32_t from = lo;
-    fill_histogram(sh, source, lo, hi, weights, weigh, [=](uint32_t key) { return (int)((key - from) >> shift); });
+    fill_by_key(sh, row, lo, hi, weights, weigh, [=](uint32_t key) { return (int)((key - from) >> shift); });
     find_bin(sh, above, weights, reached);
-    const int b = sh.found_bin;                // the bin's sums are the interval's: one of them reaches what the interval did
+    const int b = sh.found_bin;                // the bins' sums add up to the interval's: one of them reaches what it did
     above = sh.found_above;
     in = sh.found_in;
     lo = from + ((uint32_t)b << shift);
@@ -230,218 +320,587 @@ __device__ bool narrow(Shared& sh, const Source& source, const Steps& steps, uin
   return true;
 }
 
-__device__ double block_sum(Shared& sh, double v, double* before) {        // total; *before: of the waves in front of this one
-#pragma unroll
-  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d, 64);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh.wave_weight[threadIdx.x >> 6] = v;
-  __syncthreads();
-  double total = 0.0;
-  for (int w = 0; w < kWaves; ++w) {
-    if (w == (int)(threadIdx.x >> 6)) *before = total;
-    total += sh.wave_weight[w];
-  }
-  return total;
+struct Cut {                                   // kept: keys above, and equal ones up to the index last_tie
+  uint32_t key, last_tie;
+};
+
+// ties i = 0, 1, .. of weight e stay while  above + i * e < target, at least one and at most `most` of them
+__device__ __forceinline__ uint64_t ties_below(double above, double e, double target, uint64_t most) {
+  uint64_t stay = e > 0.0 ? (uint64_t)fmin(fmax(ceil((target - above) / e), 1.0), (double)most) : most;
+  while (stay > 1 && above + (double)(stay - 1) * e >= target) --stay;
+  while (stay < most && above + (double)stay * e < target) ++stay;
+  return stay;
 }
 
-__device__ uint64_t block_min(Shared& sh, uint64_t v) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) v = min(v, (uint64_t)__shfl_xor((unsigned long long)v, d, 64));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh.wave_index[threadIdx.x >> 6] = v;
-  __syncthreads();
-  for (int w = 0; w < kWaves; ++w) v = min(v, sh.wave_index[w]);
-  return v;
-}
-
-// One row by one workgroup.
 template <typename V>
-__global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
-  extern __shared__ uint32_t lds_keys[];
-  __shared__ Shared sh;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t r = blockIdx.x;
-  const bool copied = a.n <= kLdsKeys;
-  RowSource<V> source{static_cast<const typename V::elem*>(a.scores) + r * a.n, nullptr, a.n};
-  const float temperature = a.temperature ? a.temperature[r] : 1.0f;
-  const int64_t k = a.top_k ? a.top_k[r] : 0;
-  const float top_p = a.top_p ? a.top_p[r] : 1.0f;
-  const double min_p = a.min_p && a.min_p[r] > 0.0f ? fmin((double)a.min_p[r], 1.0) : 0.0;
-
-  // ---- least and greatest key, and how many nodes may be chosen
-  if (tid == 0) {
-    sh.kmin = 0xffffffffu;
-    sh.kmax = 0;
-  }
-  __syncthreads();
-  uint32_t kmin = 0xffffffffu, kmax = 0;
-  for (int64_t j = tid; j < a.n; j += kThreads) {
-    const uint32_t key = source(j);
-    if (copied) lds_keys[j] = key;
-    if (key != 0) {
-      kmin = min(kmin, key);
-      kmax = max(kmax, key);
-    }
-  }
-  atomicMin(&sh.kmin, kmin);
-  atomicMax(&sh.kmax, kmax);
-  __syncthreads();
-  kmin = sh.kmin;
-  kmax = sh.kmax;
-  if (copied) source.keys = lds_keys;
-  if (kmax == 0 || !(temperature >= 0.0f)) {   // nothing may be chosen, or not by this temperature
-    if (tid == 0) {
-      a.ids[r] = -1;
-      if (a.probs) a.probs[r] = kmax == 0 ? 0.0f : NAN;
-    }
-    return;
-  }
-  if (temperature == 0.0f) {
-    uint64_t first = ~0ull;
-    for (int64_t j = tid; j < a.n; j += kThreads)
-      if (source(j) == kmax) {
-        first = (uint64_t)j;
-        break;
-      }
-    first = block_min(sh, first);
-    if (tid == 0) {
-      a.ids[r] = (int32_t)first;
-      if (a.probs) a.probs[r] = 1.0f;
-    }
-    return;
-  }
-  const Weigh weigh{score_of(kmax), 1.0 / (double)temperature};
-
-  // ---- the cut of top-k and top-p
-  const bool by_k = k > 0 && k < a.n, by_p = top_p < 1.0f;
-  uint32_t cut = 0;                            // every valid key lies above
+__device__ void cut_the_long_way(Shared& sh, const Row<V>& row, uint32_t kmin, uint32_t kmax, const Weigh& weigh, const RowLimits& limits, Cut& cut) {
+  const Steps steps(kmin, kmax);
   uint64_t ties = 0;
   bool all_ties = true;
-  if (by_k || by_p) {
-    const Steps steps(kmin, kmax);
-    fill_histogram(sh, source, kmin, kmax, by_p, weigh, steps);
-    Sum above, in, everything{0, 0, 0};
-    double whole = 0.0;
+  double whole = 0.0;
+  for (int by_p = limits.by_k ? 0 : 1; by_p <= (limits.by_p ? 1 : 0); ++by_p) {
+    fill_by_key(sh, row, kmin, kmax, limits.by_p, weigh, steps);
+    if (by_p && (!limits.by_k || cut.key == 0)) {                  // top-k, if any, keeps everything
+      whole = find_bin(sh, Sum{0, 0, 0}, true, [](const Sum&) { return false; }).value();
+      __syncthreads();
+    }
+    const double target = (double)limits.top_p * whole;
+    const uint64_t k = (uint64_t)limits.k;
+    const bool first_alone = by_p && !(limits.top_p > 0.0f);
+    auto reached = [=](const Sum& s) { return first_alone ? s.count >= 1 : by_p ? s.value() >= target : s.count >= k; };
+    find_bin(sh, Sum{0, 0, 0}, limits.by_p, reached);
+    uint32_t key;
+    Sum above, in;
+    if (!narrow(sh, row, steps, kmin, kmax, limits.by_p, weigh, reached, key, above, in) || key < cut.key) continue;
     if (by_p) {
-      find_bin(sh, Sum{0, 0, 0}, true, [](const Sum&) { return false; });     // for the sums of the waves alone
-      for (int w = 0; w < kWaves; ++w) everything = everything + sh.wave_sum[w];
-      whole = everything.value();
-      __syncthreads();
+      const uint64_t most = key == cut.key && !all_ties ? ties : in.count;
+      ties = first_alone ? 1 : ties_below(above.value(), weigh(key), target, most);
+    } else {
+      ties = k - above.count;
+      whole = above.value() + (double)ties * weigh(key);
     }
-    bool narrowed = false;
-    if (by_k) {
-      auto reached = [=](const Sum& s) { return s.count >= (uint64_t)k; };
-      find_bin(sh, Sum{0, 0, 0}, by_p, reached);
-      if (narrow(sh, source, steps, kmin, kmax, by_p, weigh, reached, cut, above, in)) {
-        ties = (uint64_t)k - above.count;
-        all_ties = ties == in.count;
-        whole = above.value() + (double)ties * weigh(cut);
-        narrowed = true;
-      }
-    }
-    if (by_p && !(top_p > 0.0f)) {
-      cut = kmax;
-      ties = 1;
-      all_ties = false;
-    } else if (by_p) {
-      const double target = (double)top_p * whole;
-      auto reached = [=](const Sum& s) { return s.value() >= target; };
-      if (narrowed) fill_histogram(sh, source, kmin, kmax, true, weigh, steps);
-      find_bin(sh, Sum{0, 0, 0}, true, reached);
-      uint32_t cut_p;
-      if (narrow(sh, source, steps, kmin, kmax, true, weigh, reached, cut_p, above, in) && cut_p >= cut) {
-        // ties i = 0, 1, .. stay while  above + i * e < target
-        const double w = above.value(), e = weigh(cut_p);
-        const uint64_t most = cut_p == cut ? min(ties, in.count) : in.count;
-        uint64_t stay = e > 0.0 ? (uint64_t)fmin(fmax(ceil((target - w) / e), 1.0), (double)most) : most;
-        while (stay > 1 && w + (double)(stay - 1) * e >= target) --stay;
-        while (stay < most && w + (double)stay * e < target) ++stay;
-        cut = cut_p;
-        ties = stay;
-        all_ties = stay == in.count;
-      }
-    }
+    cut.key = key;
+    all_ties = ties == in.count;
   }
-  // ---- among equal keys the lowest indices stay: where the last of them lies
-  int64_t last_tie = a.n;
-  if (!all_ties) {
-    uint64_t seen = 0;
-    for (int64_t j0 = 0; j0 < a.n; j0 += kThreads) {
-      const int64_t j = j0 + tid;
-      const bool tie = j < a.n && source(j) == cut;
-      const uint64_t mask = __ballot(tie);
-      __syncthreads();
-      if (lane == 0) sh.wave_index[wave] = __popcll(mask);
-      __syncthreads();
-      uint64_t before = seen, all = seen;
-      for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) before += sh.wave_index[w];
-        all += sh.wave_index[w];
-      }
-      const uint64_t rank = before + __popcll(mask & ((1ull << lane) - 1ull));
-      const uint64_t mine = tie && rank + 1 == ties ? (uint64_t)j : ~0ull;
-      if (all >= ties) {
-        last_tie = (int64_t)block_min(sh, mine);
-        break;
-      }
-      seen = all;
-    }
+  if (all_ties) return;
+  // equal keys stay from the lowest index on: which index is the last of them?
+  auto reached = [=](const Sum& s) { return s.count >= ties; };
+  uint32_t lo = 0, hi = row.n - 1;             // bins go down with the index: find_bin begins above
+  Sum above{0, 0, 0};
+  while (lo < hi) {
+    const int bits = 32 - __clz(hi - lo);
+    const int shift = bits > 11 ? bits - 11 : 0;
+    clear_histogram(sh, false);
+    for_row<1>(row, 0, row.pieces(), threadIdx.x, kThreads, [&](uint32_t at, uint32_t key) {
+      if (key == cut.key && at >= lo && at <= hi) atomicAdd(&sh.hist.count[kBins - 1 - ((at - lo) >> shift)], 1u);
+    });
+    __syncthreads();
+    find_bin(sh, above, false, reached);
+    const int b = kBins - 1 - sh.found_bin;
+    above = sh.found_above;
+    lo = lo + ((uint32_t)b << shift);
+    hi = min(hi, lo + ((1u << shift) - 1u));
+    __syncthreads();
   }
-  auto weight_at = [&](int64_t j) {
-    const uint32_t key = source(j);
-    if (key == 0 || key < cut || (key == cut && j > last_tie)) return 0.0;
-    const double e = weigh(key);
-    return min_p > 0.0 && !(e >= min_p) ? 0.0 : e;
-  };
+  cut.last_tie = lo;
+}
 
-  // ---- the choice: sixteenths of the range, until it is one element per lane
-  int64_t from = 0, to = a.n;
-  double base = 0.0, whole = -1.0, target = 0.0;
-  while (to - from > kThreads || whole < 0.0) {
-    const int64_t part = ((to - from + kWaves - 1) / kWaves + 63) / 64 * 64;
-    const int64_t lo = from + wave * part, hi = min(lo + part, to);
-    double s = 0.0;
-    for (int64_t j = lo + lane; j < hi; j += 64) s += weight_at(j);
-    double unused;
-    const double total = block_sum(sh, s, &unused);
-    if (whole < 0.0) {
-      whole = total;
-      target = (double)a.uniforms[r] * whole;
+__device__ __forceinline__ double kept_weight(uint32_t key, uint32_t at, const Cut& cut, double min_p, const Weigh& weigh) {
+  if (key < cut.key || (key == cut.key && at > cut.last_tie)) return 0.0;
+  const double e = weigh(key);
+  return min_p > 0.0 && !(e >= min_p) ? 0.0 : e;
+}
+
+// The bin (of a histogram whose bins go down with the index) that the random number falls into.  Past every weight there is:
+// the last that has any.
+__device__ __forceinline__ uint32_t find_answer(Shared& sh, const Sum& above, const Sum& total, double u) {
+  const double target = u * total.value();
+  const Sum all = total;
+  find_bin(sh, above, true, [=](const Sum& s) { return s.value() > target || s.same_weight(all); });
+  return kBins - 1 - sh.found_bin;
+}
+__device__ __forceinline__ Sum sum_of_bins(Shared& sh) {
+  const Sum total = find_bin(sh, Sum{0, 0, 0}, true, [](const Sum&) { return false; });
+  __syncthreads();
+  return total;
+}
+__device__ __forceinline__ void answer(const SampleArgs& a, int64_t r, uint32_t at, const Sum& in, const Sum& total) {
+  if (threadIdx.x != 0) return;
+  a.ids[r] = (int32_t)at;
+  if (a.probs) a.probs[r] = (float)(in.value() / total.value());
+}
+
+// The answer among the indices [lo, hi] of the row, of which `above` lies in front, of `total` in all (none: to be found).
+template <typename V>
+__device__ void choose_index(Shared& sh, const Row<V>& row, uint32_t lo, uint32_t hi, Sum above, Sum total, const Cut& cut,
+                             const Weigh& weigh, const RowLimits& limits, const SampleArgs& a, int64_t r) {
+  bool known = total.count != 0;
+  while (true) {
+    const int bits = lo < hi ? 32 - __clz(hi - lo) : 0;
+    const int shift = bits > 11 ? bits - 11 : 0;
+    clear_histogram(sh, true);
+    const uint32_t from = (lo + row.skew) / Row<V>::kPer, to = (hi + row.skew) / Row<V>::kPer + 1;
+    for_row<1>(row, from, to, threadIdx.x, kThreads, [&](uint32_t at, uint32_t key) {
+      if (at < lo || at > hi) return;
+      const double e = kept_weight(key, at, cut, limits.min_p, weigh);
+      if (e > 0.0) add_to(sh.hist, kBins - 1 - (int)((at - lo) >> shift), true, e);
+    });
+    __syncthreads();
+    if (!known) total = sum_of_bins(sh);
+    known = true;
+    const uint32_t b = find_answer(sh, above, total, limits.u);
+    above = sh.found_above;
+    const Sum in = sh.found_in;
+    lo = lo + (b << shift);
+    hi = min(hi, lo + ((1u << shift) - 1u));
+    __syncthreads();
+    if (shift == 0) {
+      answer(a, r, lo, in, total);
+      return;
     }
-    int chosen = -1;
-    double before = base, chosen_base = base;
-    for (int w = 0; w < kWaves; ++w) {
-      const double own = sh.wave_weight[w];
-      if (own > 0.0 && (chosen < 0 || !(chosen_base + sh.wave_weight[chosen] > target))) {
-        chosen = w;                            // the first that passes the target, or the last that has any weight
-        chosen_base = before;
+  }
+}
+
+// ---- the list
+__device__ __forceinline__ uint64_t entry_of(uint32_t key, uint32_t at) { return ((uint64_t)~key << 32) | at; }
+__device__ __forceinline__ uint32_t entry_key(uint64_t e) { return ~(uint32_t)(e >> 32); }
+
+__device__ __forceinline__ void put_entry(ListShared& sh, uint32_t key, uint32_t at) {
+  const uint32_t p = atomicAdd(&sh.list_count, 1u);
+  if (p < (uint32_t)kListMost) sh.list[p] = entry_of(key, at);     // always: the histogram has counted them
+}
+
+// Bitonic sort of sh.list[0 .. size), ascending; size a power of two.  Steps over fewer than 128 entries stay in a wave.
+__device__ void sort_list(ListShared& sh, uint32_t size) {
+  __syncthreads();
+  for (uint32_t block = 2; block <= size; block <<= 1) {
+    for (uint32_t stride = block >> 1; stride; stride >>= 1) {
+      for (uint32_t t = threadIdx.x; t < size / 2; t += kThreads) {
+        const uint32_t i = ((t & ~(stride - 1)) << 1) | (t & (stride - 1)), j = i + stride;
+        const uint64_t x = sh.list[i], y = sh.list[j];
+        if ((x > y) == ((i & block) == 0)) {
+          sh.list[i] = y;
+          sh.list[j] = x;
+        }
       }
-      before += own;
+      if (stride >= 128 || (stride == 1 && block >= 128)) __syncthreads();
+      else wave_fence();
+    }
+  }
+  __syncthreads();
+}
+// pads to a power of two (entries that sort last) and sorts
+__device__ void sort_entries(ListShared& sh, uint32_t length) {
+  uint32_t size = 2;
+  while (size < length) size <<= 1;
+  __syncthreads();
+  for (uint32_t j = length + threadIdx.x; j < size; j += kThreads) sh.list[j] = ~0ull;
+  sort_list(sh, size);
+}
+
+// What the first histogram says about a row.
+struct Plan {
+  bool listed;                                 // there is a cut, and it falls on an entry of the list
+  bool long_way;                               // .. which would be too long
+  bool pieces;                                 // the weights above the list are added by pieces of the index
+  uint32_t lo, hi, length;                     // keys and number of the list's entries
+  Sum above;                                   // of the cut's bin
+  double whole;                                // sum of all weights, where they were added
+};
+// The first histogram is in sh.hist (weights only for top-p without top-k).
+__device__ Plan make_plan(Shared& sh, uint32_t kmin, uint32_t kmax, const RowLimits& limits) {
+  Plan plan{false, false, true, 1, 0, 0, Sum{0, 0, 0}, 0.0};
+  if (!limits.by_k && !limits.by_p) return plan;
+  const bool weights = !limits.by_k;
+  double target = 0.0;
+  if (weights) {
+    plan.whole = sum_of_bins(sh).value();
+    target = (double)limits.top_p * plan.whole;
+  }
+  const uint64_t k = (uint64_t)limits.k;
+  // top_p <= 0 keeps the first node alone: the bin of the greatest
+  const bool first_alone = weights && !(limits.top_p > 0.0f);
+  find_bin(sh, Sum{0, 0, 0}, weights, [=](const Sum& s) { return first_alone ? s.count >= 1 : weights ? s.value() >= target : s.count >= k; });
+  plan.listed = sh.found_bin >= 0;
+  if (plan.listed) {
+    plan.above = sh.found_above;
+    plan.length = (uint32_t)(sh.found_in.count + (limits.by_k ? sh.found_above.count : 0));
+    plan.long_way = plan.length > (uint32_t)kListMost;
+    const int bin = sh.found_bin;
+    if (!plan.long_way) keys_of_steps(Steps(kmin, kmax), bin, limits.by_k ? kBins - 1 : bin, kmin, kmax, plan.lo, plan.hi);
+  } else {
+    plan.long_way = limits.by_p;               // fewer nodes than k: by top-p alone, for which no weights were added
+  }
+  plan.pieces = !plan.long_way && !(plan.listed && limits.by_k);
+  __syncthreads();
+  return plan;
+}
+
+// Sorted entries to the cut.  Entry number p lies in bin kBins - 1 - p.
+__device__ void cut_from_list(Shared& sh, const Plan& plan, const RowLimits& limits, const Weigh& weigh, Cut& cut) {
+  sort_entries(sh, plan.length);
+  uint32_t last = limits.by_k ? min((uint32_t)limits.k, plan.length) - 1 : plan.length - 1;
+  if (limits.by_p && !(limits.top_p > 0.0f)) {
+    last = 0;
+  } else if (limits.by_p) {
+    clear_histogram(sh, true);
+    for (uint32_t p = threadIdx.x; p <= last; p += kThreads) add_to(sh.hist, kBins - 1 - p, true, weigh(entry_key(sh.list[p])));
+    __syncthreads();
+    const double whole = limits.by_k ? sum_of_bins(sh).value() : plan.whole;
+    const double target = (double)limits.top_p * whole;
+    find_bin(sh, limits.by_k ? Sum{0, 0, 0} : plan.above, true, [=](const Sum& s) { return s.value() >= target; });
+    if (sh.found_bin >= 0) last = kBins - 1 - sh.found_bin;
+    __syncthreads();
+  }
+  cut.key = entry_key(sh.list[last]);
+  cut.last_tie = (uint32_t)sh.list[last];
+}
+
+// With top-k the list holds every node that may be chosen: by index now, with the weights.
+__device__ void choose_from_list(Shared& sh, const Plan& plan, const Cut& cut, const RowLimits& limits, const Weigh& weigh, const SampleArgs& a, int64_t r) {
+  __syncthreads();
+  uint64_t mine[(kListMost + kThreads - 1) / kThreads];
+#pragma unroll
+  for (int e = 0; e < (kListMost + kThreads - 1) / kThreads; ++e) {
+    const uint32_t p = e * kThreads + threadIdx.x;
+    const uint64_t x = p < plan.length ? sh.list[p] : ~0ull;
+    mine[e] = p < plan.length ? (x << 32) | (x >> 32) : ~0ull;     // index first
+  }
+  __syncthreads();
+  uint32_t size = 2;
+  while (size < plan.length) size <<= 1;
+#pragma unroll
+  for (int e = 0; e < (kListMost + kThreads - 1) / kThreads; ++e) {
+    const uint32_t p = e * kThreads + threadIdx.x;
+    if (p < size) sh.list[p] = mine[e];
+  }
+  sort_list(sh, size);
+  clear_histogram(sh, true);
+  for (uint32_t p = threadIdx.x; p < plan.length; p += kThreads) {
+    const uint64_t x = sh.list[p];
+    const double e = kept_weight(~(uint32_t)x, (uint32_t)(x >> 32), cut, limits.min_p, weigh);
+    if (e > 0.0) add_to(sh.hist, kBins - 1 - p, true, e);
+  }
+  __syncthreads();
+  const Sum total = sum_of_bins(sh);
+  const uint32_t p = find_answer(sh, Sum{0, 0, 0}, total, limits.u);
+  answer(a, r, (uint32_t)(sh.list[p] >> 32), sh.found_in, total);
+}
+
+__device__ __forceinline__ bool answer_without_weights(uint32_t kmax, uint32_t first, const RowLimits& limits, const SampleArgs& a, int64_t r) {
+  const bool none = kmax == 0 || !(limits.temperature >= 0.0f);    // nothing may be chosen, or not by this temperature
+  if (!none && limits.temperature != 0.0f) return false;
+  if (threadIdx.x == 0) {
+    a.ids[r] = none ? -1 : (int32_t)first;
+    if (a.probs) a.probs[r] = kmax == 0 ? 0.0f : none ? NAN : 1.0f;
+  }
+  return true;
+}
+
+// ---- least and greatest key, and the first index of the greatest
+struct Extreme {
+  uint32_t kmin, kmax, first, unused;
+  __device__ __forceinline__ void with(uint32_t lo, uint32_t hi, uint32_t at) {
+    kmin = min(kmin, lo);
+    if (hi > kmax || (hi == kmax && at < first)) {
+      kmax = hi;
+      first = at;
+    }
+  }
+  __device__ __forceinline__ void over_wave() {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) with(__shfl_xor(kmin, d, 64), __shfl_xor(kmax, d, 64), __shfl_xor(first, d, 64));
+  }
+};
+template <typename V>
+__device__ Extreme extreme_of(const Row<V>& row, uint32_t from, uint32_t to) {           // the same in every lane
+  __shared__ Extreme wave_x[kWaves];
+  Extreme x{0xffffffffu, 0, 0xffffffffu, 0};
+  for_row<kAhead>(row, from, to, threadIdx.x, kThreads, [&](uint32_t at, uint32_t key) { x.with(key, key, at); });
+  x.over_wave();
+  if ((threadIdx.x & 63) == 0) wave_x[threadIdx.x >> 6] = x;
+  __syncthreads();
+  for (int w = 0; w < kWaves; ++w) x.with(wave_x[w].kmin, wave_x[w].kmax, wave_x[w].first);
+  return x;
+}
+
+// The first histogram of the pieces from .. to.
+template <typename V>
+__device__ void first_histogram(Histogram& hist, const Row<V>& row, uint32_t from, uint32_t to, const Steps& steps, bool weights, const Weigh& weigh) {
+  if (weights)
+    for_row<1>(row, from, to, threadIdx.x, kThreads, [&](uint32_t, uint32_t key) { add_to(hist, steps(key), true, weigh(key)); });
+  else
+    for_row<kAhead>(row, from, to, threadIdx.x, kThreads, [&](uint32_t, uint32_t key) { atomicAdd(&hist.count[steps(key)], 1u); });
+}
+
+// ---- row by row --------------------------------------------------------------------------------------------------------
+template <typename V>
+__global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
+  __shared__ Shared sh;
+  const int64_t r = blockIdx.x;
+  const Row<V> row(a.scores, r, a.n);
+  const RowLimits limits(a, r);
+  const Extreme x = extreme_of(row, 0, row.pieces());
+  if (answer_without_weights(x.kmax, x.first, limits, a, r)) return;
+  const Weigh weigh{score_of(x.kmax), 1.0 / (double)limits.temperature};
+  Cut cut{0, row.n};                           // every valid key lies above 0
+  if (limits.by_k || limits.by_p) {
+    clear_histogram(sh, true);
+    first_histogram(sh.hist, row, 0, row.pieces(), Steps(x.kmin, x.kmax), !limits.by_k, weigh);
+    if (threadIdx.x == 0) sh.list_count = 0;
+    __syncthreads();
+    const Plan plan = make_plan(sh, x.kmin, x.kmax, limits);
+    if (plan.long_way) {
+      cut_the_long_way(sh, row, x.kmin, x.kmax, weigh, limits, cut);
+    } else if (plan.listed) {
+      for_row<kAhead>(row, 0, row.pieces(), threadIdx.x, kThreads, [&](uint32_t at, uint32_t key) {
+        if (key >= plan.lo && key <= plan.hi) put_entry(sh, key, at);
+      });
+      cut_from_list(sh, plan, limits, weigh, cut);
+      if (limits.by_k) {
+        choose_from_list(sh, plan, cut, limits, weigh, a, r);
+        return;
+      }
+    }
+  }
+  choose_index(sh, row, 0, row.n - 1, Sum{0, 0, 0}, Sum{0, 0, 0}, cut, weigh, limits, a, r);
+}
+
+// ---- split ---------------------------------------------------------------------------------------------------------------
+struct SplitArgs {
+  SampleArgs s;
+  int32_t groups;                              // workgroups per row
+  uint32_t parts;                              // of the positions of a row, `width` each (a multiple of 512: a 16-byte piece per lane), at most kBins
+  uint32_t width, parts_per_group;
+  Extreme* extremes;                           // [rows][groups]
+  Histogram* first_hist;                       // [rows]
+  unsigned long long* part_hi;                 // [rows][kBins]
+  unsigned long long* part_lo;
+  Plan* plans;                                 // [rows]
+  uint32_t* list_count;                        // [rows]
+  uint64_t* lists;                             // [rows][kListMost]
+};
+
+__device__ __forceinline__ Extreme row_extreme(const SplitArgs& a, int64_t r) {
+  Extreme x{0xffffffffu, 0, 0xffffffffu, 0};
+  for (int g = threadIdx.x & 63; g < a.groups; g += 64) {
+    const Extreme y = a.extremes[r * a.groups + g];
+    x.with(y.kmin, y.kmax, y.first);
+  }
+  x.over_wave();
+  return x;
+}
+// this workgroup's 16-byte pieces of its row
+template <typename V>
+__device__ __forceinline__ void group_pieces(const SplitArgs& a, const Row<V>& row, int g, uint32_t& from, uint32_t& to) {
+  const uint64_t span = (uint64_t)a.parts_per_group * a.width / Row<V>::kPer;
+  from = (uint32_t)min(g * span, (uint64_t)row.pieces());
+  to = (uint32_t)min((g + 1) * span, (uint64_t)row.pieces());
+}
+
+// first pass; also clears what the next ones add to
+template <typename V>
+__global__ __launch_bounds__(kThreads) void extremes_kernel(SplitArgs a) {
+  const int64_t r = blockIdx.x / a.groups;
+  const int g = (int)(blockIdx.x % a.groups);
+  uint32_t* words = reinterpret_cast<uint32_t*>(&a.first_hist[r]);
+  for (uint32_t w = g * kThreads + threadIdx.x; w < sizeof(Histogram) / 4; w += a.groups * kThreads) words[w] = 0;
+  if (g == 0 && threadIdx.x == 0) a.list_count[r] = 0;
+  const Row<V> row(a.s.scores, r, a.s.n);
+  uint32_t from, to;
+  group_pieces(a, row, g, from, to);
+  const Extreme x = extreme_of(row, from, to);
+  if (threadIdx.x == 0) a.extremes[blockIdx.x] = x;
+}
+
+// second pass: the first histogram.  Weights only for top-p without top-k: with it, the list holds all that top-p may keep.
+template <typename V>
+__global__ __launch_bounds__(kThreads) void first_histogram_kernel(SplitArgs a) {
+  __shared__ Histogram hist;
+  const int64_t r = blockIdx.x / a.groups;
+  const int g = (int)(blockIdx.x % a.groups);
+  const RowLimits limits(a.s, r);
+  const Extreme x = row_extreme(a, r);
+  if (x.kmax == 0 || !(limits.temperature > 0.0f) || !(limits.by_k || limits.by_p)) return;
+  const bool weights = !limits.by_k;
+  for (int b = threadIdx.x; b < kBins; b += kThreads) {
+    hist.count[b] = 0;
+    hist.hi[b] = 0;
+    hist.lo[b] = 0;
+  }
+  __syncthreads();
+  const Row<V> row(a.s.scores, r, a.s.n);
+  uint32_t from, to;
+  group_pieces(a, row, g, from, to);
+  first_histogram(hist, row, from, to, Steps(x.kmin, x.kmax), weights, Weigh{score_of(x.kmax), 1.0 / (double)limits.temperature});
+  __syncthreads();
+  Histogram& sum = a.first_hist[r];
+  for (int b = threadIdx.x; b < kBins; b += kThreads) {
+    if (hist.count[b] == 0) continue;
+    atomicAdd(&sum.count[b], hist.count[b]);
+    if (hist.hi[b] != 0) atomicAdd(&sum.hi[b], hist.hi[b]);
+    if (hist.lo[b] != 0) atomicAdd(&sum.lo[b], hist.lo[b]);
+  }
+}
+
+// what it says about each row
+__global__ __launch_bounds__(kThreads) void plan_kernel(SplitArgs a) {
+  __shared__ Shared sh;
+  const int64_t r = blockIdx.x;
+  const RowLimits limits(a.s, r);
+  const Extreme x = row_extreme(a, r);
+  if (x.kmax == 0 || !(limits.temperature > 0.0f)) return;
+  if (limits.by_k || limits.by_p) {
+    const Histogram& from = a.first_hist[r];
+    for (int b = threadIdx.x; b < kBins; b += kThreads) {
+      sh.hist.count[b] = from.count[b];
+      sh.hist.hi[b] = from.hi[b];
+      sh.hist.lo[b] = from.lo[b];
+    }
+  }
+  __syncthreads();
+  const Plan plan = make_plan(sh, x.kmin, x.kmax, limits);
+  if (threadIdx.x == 0) a.plans[r] = plan;
+}
+
+// third pass: the list, gathered in LDS and handed over with one atomic per workgroup, and the weights above it by parts of the
+// row, one wave a part
+template <typename V>
+__global__ __launch_bounds__(kThreads) void collect_kernel(SplitArgs a) {
+  __shared__ ListShared sh;
+  const int64_t r = blockIdx.x / a.groups;
+  const int g = (int)(blockIdx.x % a.groups);
+  const RowLimits limits(a.s, r);
+  const Extreme x = row_extreme(a, r);
+  if (x.kmax == 0 || !(limits.temperature > 0.0f)) return;
+  const Plan& plan = a.plans[r];
+  if (plan.long_way) return;
+  if (threadIdx.x == 0) sh.list_count = 0;
+  __syncthreads();
+  const uint32_t key_lo = plan.lo, key_hi = plan.hi;
+  const Row<V> row(a.s.scores, r, a.s.n);
+  auto to_list = [&](uint32_t at, uint32_t key) {
+    if (key >= key_lo && key <= key_hi) put_entry(sh, key, at);
+  };
+  if (!plan.pieces) {
+    uint32_t from, to;
+    group_pieces(a, row, g, from, to);
+    for_row<kAhead>(row, from, to, threadIdx.x, kThreads, to_list);
+  } else {
+    const Weigh weigh{score_of(x.kmax), 1.0 / (double)limits.temperature};
+    const uint32_t floor = plan.listed ? key_hi : 0, last = min(a.parts, (g + 1) * a.parts_per_group);
+    const uint32_t span = a.width / Row<V>::kPer;
+    for (uint32_t part = g * a.parts_per_group + (threadIdx.x >> 6); part < last; part += kWaves) {
+      uint64_t hi = 0, lo = 0;
+      for_row<1>(row, min(part * span, row.pieces()), min((part + 1) * span, row.pieces()), threadIdx.x & 63, 64, [&](uint32_t at, uint32_t key) {
+        if (key <= floor) {
+          to_list(at, key);
+          return;
+        }
+        const double w = weigh(key);
+        if (limits.min_p > 0.0 && !(w >= limits.min_p)) return;
+        const uint64_t units = units_of(w);
+        hi += units >> 31;
+        lo += units & 0x7fffffffu;
+      });
+#pragma unroll
+      for (int d = 32; d; d >>= 1) {
+        hi += (uint64_t)__shfl_xor((unsigned long long)hi, d, 64);
+        lo += (uint64_t)__shfl_xor((unsigned long long)lo, d, 64);
+      }
+      if ((threadIdx.x & 63) == 0) {
+        a.part_hi[r * kBins + part] = hi;
+        a.part_lo[r * kBins + part] = lo;
+      }
+    }
+  }
+  __syncthreads();
+  const uint32_t count = sh.list_count;
+  if (count == 0) return;
+  if (threadIdx.x == 0) sh.list_base = atomicAdd(&a.list_count[r], count);
+  __syncthreads();
+  for (uint32_t j = threadIdx.x; j < count; j += kThreads) a.lists[r * kListMost + sh.list_base + j] = sh.list[j];
+}
+
+// one workgroup a row finishes
+template <typename V>
+__global__ __launch_bounds__(kThreads) void finish_rows_kernel(SplitArgs a) {
+  __shared__ Shared sh;
+  const int64_t r = blockIdx.x;
+  const RowLimits limits(a.s, r);
+  const Extreme x = row_extreme(a, r);
+  if (answer_without_weights(x.kmax, x.first, limits, a.s, r)) return;
+  const Weigh weigh{score_of(x.kmax), 1.0 / (double)limits.temperature};
+  const Row<V> row(a.s.scores, r, a.s.n);
+  const Plan plan = a.plans[r];
+  Cut cut{0, row.n};
+  uint32_t lo = 0, hi = row.n - 1;
+  Sum above{0, 0, 0}, total{0, 0, 0};
+  if (plan.long_way) {
+    cut_the_long_way(sh, row, x.kmin, x.kmax, weigh, limits, cut);
+  } else {
+    if (plan.listed) {
+      for (uint32_t j = threadIdx.x; j < plan.length; j += kThreads) sh.list[j] = a.lists[r * kListMost + j];
+      cut_from_list(sh, plan, limits, weigh, cut);
+      if (!plan.pieces) {
+        choose_from_list(sh, plan, cut, limits, weigh, a.s, r);
+        return;
+      }
+    }
+    // the parts' weights, with what stays of the list, are a histogram along the index
+    clear_histogram(sh, true);
+    for (uint32_t p = threadIdx.x; p < a.parts; p += kThreads) {
+      const uint64_t p_hi = a.part_hi[r * kBins + p], p_lo = a.part_lo[r * kBins + p];
+      sh.hist.count[kBins - 1 - p] = (p_hi | p_lo) != 0;
+      sh.hist.hi[kBins - 1 - p] = p_hi;
+      sh.hist.lo[kBins - 1 - p] = p_lo;
     }
     __syncthreads();
-    from = from + (int64_t)max(chosen, 0) * part;
-    to = min(from + part, to);
-    base = chosen_base;
+    for (uint32_t j = threadIdx.x; j < plan.length; j += kThreads) {
+      const uint32_t at = (uint32_t)sh.list[j];
+      const double e = kept_weight(entry_key(sh.list[j]), at, cut, limits.min_p, weigh);
+      if (e > 0.0) add_to(sh.hist, kBins - 1 - (int)((at + row.skew) / a.width), true, e);
+    }
+    __syncthreads();
+    total = sum_of_bins(sh);
+    const uint32_t part = find_answer(sh, above, total, limits.u);
+    above = sh.found_above;
+    __syncthreads();
+    lo = (uint32_t)max((int64_t)part * a.width - row.skew, (int64_t)0);
+    hi = (uint32_t)min((int64_t)(part + 1) * a.width - row.skew, (int64_t)row.n) - 1;
   }
-  const int64_t j = from + tid;
-  const double e = j < to ? weight_at(j) : 0.0;
-  double upto = e;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const double up = __shfl_up(upto, d, 64);
-    if (lane >= d) upto += up;
+  choose_index(sh, row, lo, hi, above, total, cut, weigh, limits, a.s, r);
+}
+
+// ---- host ----------------------------------------------------------------------------------------------------------------
+// Split where a workgroup per row would leave compute units idle and rows are long enough for several.
+int32_t split_groups(int64_t rows, int64_t n) {
+  if (rows >= 512 || n < 2 * kSplitLeast) return 1;
+  return (int32_t)std::max<int64_t>(1, std::min<int64_t>(kSplitGroups / rows, ceil_div(n, kSplitLeast)));
+}
+
+SplitArgs plan_split(void* ws, int64_t rows, int64_t n, size_t& bytes) {
+  SplitArgs p{};
+  p.groups = split_groups(rows, n);
+  Carver c(ws);
+  if (p.groups > 1) {
+    p.width = (uint32_t)(ceil_div(ceil_div(n + 7, kBins), 512) * 512);    // 7: the farthest a row begins behind a boundary
+    p.parts = (uint32_t)ceil_div(n + 7, p.width);
+    p.parts_per_group = (uint32_t)ceil_div(p.parts, p.groups);
+    p.extremes = c.take<Extreme>((size_t)rows * p.groups);
+    p.first_hist = c.take<Histogram>(rows);
+    p.part_hi = c.take<unsigned long long>((size_t)rows * kBins);
+    p.part_lo = c.take<unsigned long long>((size_t)rows * kBins);
+    p.plans = c.take<Plan>(rows);
+    p.list_count = c.take<uint32_t>(rows);
+    p.lists = c.take<uint64_t>((size_t)rows * kListMost);
   }
-  if (lane == 63) sh.wave_weight[wave] = upto;
-  __syncthreads();
-  double before = base;
-  for (int w = 0; w < wave; ++w) before += sh.wave_weight[w];
-  const uint64_t first = block_min(sh, e > 0.0 && before + upto > target ? (uint64_t)j : ~0ull);
-  const uint64_t last = ~block_min(sh, e > 0.0 ? ~(uint64_t)j : ~0ull);
-  const uint64_t at = first != ~0ull ? first : last;
-  if ((uint64_t)j == at && j < to) {
-    a.ids[r] = (int32_t)j;
-    if (a.probs) a.probs[r] = (float)(e / whole);
+  bytes = std::max<size_t>(c.used, 256);
+  return p;
+}
+
+template <typename V>
+int32_t run_sample(const SampleArgs& a, SplitArgs& p, hipStream_t stream) {
+  if (p.groups == 1) {
+    sample_rows_kernel<V><<<(unsigned)a.rows, kThreads, 0, stream>>>(a);
+    GS_LAUNCH_CHECK();
+    return GS_OK;
   }
+  p.s = a;
+  const unsigned groups = (unsigned)(a.rows * p.groups);
+  extremes_kernel<V><<<groups, kThreads, 0, stream>>>(p);
+  GS_LAUNCH_CHECK();
+  if (a.top_k || a.top_p) {
+    first_histogram_kernel<V><<<groups, kThreads, 0, stream>>>(p);
+    GS_LAUNCH_CHECK();
+  }
+  plan_kernel<<<(unsigned)a.rows, kThreads, 0, stream>>>(p);
+  GS_LAUNCH_CHECK();
+  collect_kernel<V><<<groups, kThreads, 0, stream>>>(p);
+  GS_LAUNCH_CHECK();
+  finish_rows_kernel<V><<<(unsigned)a.rows, kThreads, 0, stream>>>(p);
+  GS_LAUNCH_CHECK();
+  return GS_OK;
 }
 
 }  // namespace
@@ -451,7 +910,10 @@ using namespace gs;
 
 extern "C" size_t gs_sample_scores_workspace_bytes(int64_t rows, int64_t n, int32_t dtype) {
   if (rows < 0 || n < 1 || n > (int64_t)INT32_MAX || (dtype != GS_F32 && dtype != GS_BF16 && dtype != GS_F16)) return 0;
-  return 256;
+  size_t bytes = 0, most = 0;
+  plan_split(nullptr, rows, n, bytes);
+  if (rows > 511) plan_split(nullptr, 511, n, most);             // what serves many rows serves fewer
+  return std::max(bytes, most);
 }
 
 extern "C" int32_t gs_sample_scores(const void* scores, int64_t rows, int64_t n, int32_t dtype, const float* uniforms,
@@ -462,14 +924,13 @@ extern "C" int32_t gs_sample_scores(const void* scores, int64_t rows, int64_t n,
   if (rows > 0 && (!scores || !uniforms || !ids_out)) return GS_EINVAL;
   if (!aligned(scores, dtype == GS_F32 ? 4 : 2)) return GS_EINVAL;
   if (!ws || !aligned(ws, 256)) return GS_EINVAL;
-  if (ws_bytes < gs_sample_scores_workspace_bytes(rows, n, dtype)) return GS_EWORKSPACE;
+  size_t need = 0;
+  SplitArgs p = plan_split(ws, rows, n, need);
+  if (ws_bytes < need) return GS_EWORKSPACE;
   if (rows >= ((int64_t)1 << 22)) return GS_EOVERFLOW;           // 2^32 lanes: more than one launch takes
   if (rows == 0) return GS_OK;
   const SampleArgs a{scores, rows, n, uniforms, temperature, top_k, top_p, min_p, ids_out, probs_out};
-  const size_t lds = n <= kLdsKeys ? sizeof(uint32_t) * (size_t)n : 0;
-  if (dtype == GS_F32) sample_rows_kernel<ScoreF32><<<(unsigned)rows, kThreads, lds, stream>>>(a);
-  else if (dtype == GS_BF16) sample_rows_kernel<ScoreHalf<bf16_t>><<<(unsigned)rows, kThreads, lds, stream>>>(a);
-  else sample_rows_kernel<ScoreHalf<f16_t>><<<(unsigned)rows, kThreads, lds, stream>>>(a);
-  GS_LAUNCH_CHECK();
-  return GS_OK;
+  if (dtype == GS_F32) return run_sample<ScoreF32>(a, p, stream);
+  if (dtype == GS_BF16) return run_sample<ScoreHalf<bf16_t>>(a, p, stream);
+  return run_sample<ScoreHalf<f16_t>>(a, p, stream);
 }

@@ -695,7 +695,7 @@ static int32_t run_padded(const SoftmaxCall& q, const SoftmaxPlan& p, hipStream_
   elem* rows = static_cast<elem*>(p.rows);
   constexpr int64_t most = ((int64_t)1 << 32) / kThreads;        // a launch takes fewer than 2^32 lanes
   if ((!q.loss || q.g_out) && p.node_tiles * p.node_splits >= most) return GS_EOVERFLOW;
-  if (q.loss && p.pair_tiles * p.splits >= most) return GS_EOVERFLOW;
+  if (q.loss && (p.pair_tiles * p.splits >= most || p.padded_pairs / (kThreads / 64) >= most)) return GS_EOVERFLOW;
   auto blocks_for = [](int64_t items) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(items, kThreads), 256 * 16)); };
   gather_pairs_kernel<E><<<blocks_for(p.padded_pairs * (DP / (16 / (int)sizeof(elem)))), kThreads, 0, stream>>>(
       static_cast<const elem*>(q.w_in), q.num_in, q.num_nodes, q.dim, DP, q.centers, q.contexts, q.bias, q.num_pairs,

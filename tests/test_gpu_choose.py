@@ -190,3 +190,35 @@ def test_graph_replays_on_another_stream(gs):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(ids, want[0]) and torch.equal(probs, want[1])
+
+
+@pytest.mark.parametrize("fmt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,n", [(1, 24_577), (2, 262_147), (7, 100_003), (3, 131_072)])
+def test_long_rows_shared_by_several_workgroups(gs, fmt, rows, n):
+    """Rows of mixed limits in one call: none, top-k, top-p, both, greedy, k beyond the row, everything left out."""
+    g = torch.Generator().manual_seed(rows + n)
+    z, _ = rows_of(rows * 8, n, fmt, seed=2)
+    if rows > 2:
+        z[5] = -math.inf
+        z[6, : n - 1] = -math.inf
+    u = torch.rand(rows * 8, generator=g)
+    u[0], u[1] = 0.0, 1.0
+    k = torch.tensor([0, 50, 0, 700, 1, n + 5, n - 1, 3000] * rows, dtype=torch.int32)
+    p = torch.tensor([1.0, 1.0, 0.9, 0.5, 0.3, 0.8, 0.999, 0.05] * rows)
+    t = torch.tensor([1.0, 0.7, 1.3, 1.0, 0.0, 1.0, 2.0, 0.5] * rows)
+    check(gs, z, u, temperature=t, top_k=k, top_p=p, min_p=[0.0, 0.01, 0.0, 0.05] * (2 * rows))
+    check(gs, z, u, temperature=t, top_k=k)
+    check(gs, z, u, temperature=t, top_p=p)
+    check(gs, z, u, min_p=[0.0, 0.01, 0.2, 1.0] * (2 * rows))
+
+
+@pytest.mark.parametrize("top_k,top_p", [(None, 0.6), (40_000, None), (40_000, 0.6), (7, None), (1_000_000, 0.5)])
+def test_long_rows_of_equal_scores(gs, top_k, top_p):
+    """More elements fall on the cut than a row's list has room for."""
+    rows, n = 4, 60_000
+    z = torch.zeros(rows, n)
+    z[1] = torch.randint(0, 3, (n,), generator=torch.Generator().manual_seed(1)).float()
+    z[2, ::2] = 1e-3 * torch.arange(n // 2) / n
+    z[3, 0] = 1e30
+    u = torch.tensor([0.3, 0.6, 0.9, 0.99])
+    check(gs, z, u, top_k=None if top_k is None else [top_k] * rows, top_p=None if top_p is None else [top_p] * rows)

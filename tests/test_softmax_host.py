@@ -91,6 +91,7 @@ def test_launches_too_large_for_one(lib):
     """2^24 workgroups of 256 lanes are 2^32 lanes, which no launch takes: refused before anything is enqueued."""
     assert scores(lib, nodes=(1 << 31) - 1, dim=4) == EOVERFLOW
     assert loss(lib, nodes=(1 << 31) - 1, dim=4) == EOVERFLOW
+    assert loss(lib, pairs=1 << 26) == EOVERFLOW              # a wave per pair
 
 
 def sample(lib, **k):
