@@ -23,6 +23,8 @@
 
 #pragma once
 
+#include <type_traits>
+
 #include "common.h"
 
 namespace gs {
@@ -80,18 +82,24 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr double kLn2 = 0.69314718055994530942;
 constexpr int kThreads = 256;
 
-__device__ uint4 zero_piece[1];                // never written
+// never written: what rows that are masked, or no rows, are read as
+__device__ uint4 zero_piece[1];
+template <typename E>
+__device__ uint4 nan_piece[1] = {{E::kNan, E::kNan, E::kNan, E::kNan}};
 
 __device__ __forceinline__ int64_t tiles_of(int64_t rows, int tile) { return (rows + tile - 1) / tile; }
 
 }  // namespace
 
 // Storage formats.  kShift: the powers of two by which probabilities are scaled before they are rounded to the format (undone
-// in fp32 afterwards): binary16 would lose those below 2^-24 otherwise; the scaled ones stay below 2^15.
+// in fp32 afterwards): binary16 would lose those below 2^-24 otherwise; the scaled ones stay below 2^15.  kForwardShift: the
+// same in the forward pass, where they may be 2^kSlack times larger.
 struct F32 {
   typedef float elem;
   static constexpr bool kWide = true;
   static constexpr int kShift = 0;
+  static constexpr int kForwardShift = 0;
+  static constexpr float kSlack = 8.0f;
   static constexpr uint32_t kNan = 0x7fc00000u;
   static __device__ __forceinline__ float load(const float* p) { return *p; }
   static __device__ __forceinline__ void store4(float* p, vec4 v) { *reinterpret_cast<vec4*>(p) = v; }
@@ -100,6 +108,8 @@ struct BF16 {
   typedef uint16_t elem;
   static constexpr bool kWide = false;
   static constexpr int kShift = 0;
+  static constexpr int kForwardShift = 0;
+  static constexpr float kSlack = 8.0f;
   static constexpr uint32_t kNan = 0x7fc07fc0u;
   static __device__ __forceinline__ float load(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
@@ -116,6 +126,8 @@ struct F16 {
   typedef uint16_t elem;
   static constexpr bool kWide = false;
   static constexpr int kShift = 14;
+  static constexpr int kForwardShift = 11;
+  static constexpr float kSlack = 4.0f;
   static constexpr uint32_t kNan = 0x7e007e00u;
   static __device__ __forceinline__ float load(const uint16_t* p) { return __half2float(__ushort_as_half(*p)); }
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
@@ -132,14 +144,17 @@ struct F16 {
 namespace {
 
 // Tile shapes: kept rows per wave 32 * kNB, streamed rows per tile kTile.
-template <typename E, int DP>
+template <typename E, int DP, int MODE>
 struct Shape {
   static constexpr int kRowBytes = DP * (int)sizeof(typename E::elem);
   static constexpr int kPieces = kRowBytes / 16;                   // 16-byte pieces of a row: 8, 16, 32 or 64
   static constexpr int kPerPiece = 16 / (int)sizeof(typename E::elem);
   static constexpr int kSteps = kPieces / 2;                       // pieces a half wave takes in the first product
-  static constexpr int kNB = (E::kWide || DP == 256) ? 1 : 2;
-  static constexpr int kTile = kRowBytes >= 1024 ? 32 : 64;
+  static constexpr int kNB = MODE != kScores || E::kWide || DP == 256 ? 1 : 2;
+  static constexpr int kTile = MODE == kScores || DP == 256 ? 32 : 64;
+  // waves per SIMD to leave registers for, and as many workgroups per compute unit: two, so that one's exponentials run beside the
+  // other's matrix instructions, but for fp32 rows of 256, which take 256 registers for the kept rows and the sums alone
+  static constexpr int kWaves = E::kWide && DP == 256 ? 1 : 2;
   static constexpr int kBlocks = DP / 32;                          // 32-column blocks of the second product
   static constexpr int kKept = 32 * kNB * 4;                       // kept rows per workgroup
   static constexpr int kLoads = kTile * kPieces / kThreads;        // 16-byte loads per lane and tile
@@ -161,6 +176,9 @@ __device__ __forceinline__ void wait_loads_and_barrier() {
   __syncthreads();
 }
 
+// in a branch that few tiles take: keeps the compiler from doing its work for all of them and selecting
+__device__ __forceinline__ void rare() { asm volatile(""); }
+
 // one step of the first product: 16 bytes of a streamed and of a kept row per lane
 template <typename E>
 __device__ __forceinline__ acc16 step(vec4 a, vec4 b, acc16 c) {
@@ -173,42 +191,32 @@ __device__ __forceinline__ acc16 step(vec4 a, vec4 b, acc16 c) {
   }
 }
 
-// ---- the pairs' rows, checked and copied -------------------------------------------------------------------------------
-// rows[i] = w_in[centers[i]], zero-padded to DP columns and to whole tiles; target[i] = context, or a negative word for a pair
-// without gradient: -1 left out (context -1), -2 an id that is no row, -3 the context is masked.  For scores (no contexts) a
-// centre that is no row gives a row of NaN.
+// ---- the pairs' rows, copied for the table gradient --------------------------------------------------------------------
+// rows[i] = w_in[centers[i]], zero-padded to DP columns and to whole tiles.
 template <typename E>
-__global__ __launch_bounds__(kThreads) void gather_pairs_kernel(const typename E::elem* w_in, int64_t num_in, int64_t num_nodes,
-                                                                int dim, int padded, const int32_t* centers,
-                                                                const int32_t* contexts, const float* bias, int64_t num_pairs,
-                                                                int64_t padded_pairs, typename E::elem* rows, int32_t* target) {
+__global__ __launch_bounds__(kThreads) void gather_pairs_kernel(const typename E::elem* w_in, int64_t num_in, int dim, int padded,
+                                                                const int32_t* centers, int64_t num_pairs, int64_t padded_pairs,
+                                                                typename E::elem* rows) {
   constexpr int per = 16 / (int)sizeof(typename E::elem);
   const int pieces = padded / per;
   const int64_t total = padded_pairs * pieces;
   for (int64_t s = (int64_t)blockIdx.x * kThreads + threadIdx.x; s < total; s += (int64_t)gridDim.x * kThreads) {
     const int64_t i = s / pieces;
     const int p = (int)(s - i * pieces);
-    int32_t t = -1;
-    int64_t c = 0;
-    if (i < num_pairs) {
-      c = centers[i];
-      t = contexts ? contexts[i] : 0;
-      if (c < 0 || c >= num_in || t < -1 || t >= num_nodes) t = -2;
-      else if (t >= 0 && contexts && bias && bias[t] == -INFINITY) t = -3;
-    }
-    if (p == 0 && target) target[i] = t;
+    const int64_t c = i < num_pairs ? centers[i] : -1;
     uint4 v = make_uint4(0, 0, 0, 0);
-    if (t >= 0 && p * per < dim) v = reinterpret_cast<const uint4*>(w_in)[(c * dim + p * per) / per];
-    if (t == -2 && !contexts) v = make_uint4(E::kNan, E::kNan, E::kNan, E::kNan);
+    if (c >= 0 && c < num_in && p * per < dim) v = reinterpret_cast<const uint4*>(w_in)[(c * dim + p * per) / per];
     reinterpret_cast<uint4*>(rows)[s] = v;
   }
 }
 
 struct StreamArgs {
-  const void* kept;          // forward: the pairs' rows; table gradient: w_out
-  const void* streamed;      // the other one
-  int64_t kept_rows;         // rows that exist
-  int64_t streamed_rows;     // (the pairs' rows exist up to whole tiles)
+  const void* kept;          // forward: w_in, through centers; table gradient and scores: w_out
+  const void* streamed;      // forward: w_out; table gradient: copies of the pairs' rows; scores: w_in, through centers
+  const int32_t* centers;
+  int64_t num_in;
+  int64_t kept_rows;         // pairs or nodes
+  int64_t streamed_rows;
   int32_t dim;
   float scale2;              // scale * log2(e); scores: scale
   float out_scale;
@@ -225,8 +233,8 @@ struct StreamArgs {
 };
 
 template <typename E, int DP, int MODE, bool BIAS>
-__global__ __launch_bounds__(kThreads, 1) void stream_kernel(StreamArgs a) {
-  using S = Shape<E, DP>;
+__global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream_kernel(StreamArgs a) {
+  using S = Shape<E, DP, MODE>;
   using elem = typename E::elem;
   constexpr int NB = S::kNB, TILE = S::kTile, ROWB = S::kRowBytes, PIECES = S::kPieces, KS = S::kSteps, DB = S::kBlocks;
   constexpr bool NODES_STREAMED = MODE == kLossOnly || MODE == kForward;
@@ -257,26 +265,21 @@ __global__ __launch_bounds__(kThreads, 1) void stream_kernel(StreamArgs a) {
   float kept_bias[NB];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
-    const int64_t row = kept_row0 + 32 * nb;
+    int64_t row = kept_row0 + 32 * nb;
+    bool live = row < a.kept_rows;
     kept_bias[nb] = 0.0f;
-    bool live = true;
-    if (!NODES_STREAMED) {
-      live = row < a.kept_rows;
-      if (BIAS) {
-        kept_bias[nb] = live ? a.bias[row] * (MODE == kScores ? 1.0f : kLog2e) : -INFINITY;
-        live = live && kept_bias[nb] != -INFINITY;
-      }
+    if constexpr (NODES_STREAMED) {
+      row = live ? a.centers[row] : -1;
+      live = row >= 0 && row < a.num_in;
+    } else if constexpr (BIAS) {
+      kept_bias[nb] = live ? a.bias[row] * (MODE == kScores ? 1.0f : kLog2e) : -INFINITY;
+      live = kept_bias[nb] != -INFINITY;
     }
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       const int at = (2 * ks + half) * S::kPerPiece;
-      if (NODES_STREAMED) {
-        kept[nb][ks] = *reinterpret_cast<const vec4*>(static_cast<const elem*>(a.kept) + row * DP + at);
-      } else {
-        const bool read = live && at < a.dim;
-        const void* src = read ? static_cast<const void*>(static_cast<const elem*>(a.kept) + row * a.dim + at) : zero_piece;
-        kept[nb][ks] = *static_cast<const vec4*>(src);
-      }
+      const void* src = live && at < a.dim ? static_cast<const void*>(static_cast<const elem*>(a.kept) + row * a.dim + at) : zero_piece;
+      kept[nb][ks] = *static_cast<const vec4*>(src);
     }
   }
 
@@ -306,6 +309,11 @@ __global__ __launch_bounds__(kThreads, 1) void stream_kernel(StreamArgs a) {
         if constexpr (BIAS) read = read && row_bias[n] != -INFINITY;
         src = read ? static_cast<const elem*>(a.streamed) + row * a.dim + piece * S::kPerPiece
                    : reinterpret_cast<const elem*>(zero_piece);
+      } else if constexpr (MODE == kScores) {
+        const int64_t c = row < a.streamed_rows ? a.centers[row] : -1;
+        const bool known = c >= 0 && c < a.num_in;
+        src = known && piece * S::kPerPiece < a.dim ? static_cast<const elem*>(a.streamed) + c * a.dim + piece * S::kPerPiece
+                                                   : reinterpret_cast<const elem*>(known ? zero_piece : nan_piece<E>);
       } else {
         src = static_cast<const elem*>(a.streamed) + row * DP + piece * S::kPerPiece;
       }
@@ -345,7 +353,7 @@ __global__ __launch_bounds__(kThreads, 1) void stream_kernel(StreamArgs a) {
     run_sum[nb] = 0.0;
   }
 
-  // lane's parts of the LDS addresses
+  // lane's parts of the LDS addresses; the swap turns bits 4 to 7 of them, what lies above is added
   const int read1 = l32 * ROWB + ((half ^ swap_of<PIECES>(l32)) << 4);
   int read2;
   if constexpr (E::kWide) {
@@ -364,85 +372,97 @@ __global__ __launch_bounds__(kThreads, 1) void stream_kernel(StreamArgs a) {
     put_side(0);
     if (first + 1 < last) fetch_bias(first + 1);
   }
-  for (int64_t t = first; t < last; ++t) {
-    const int buf = (int)((t - first) & 1);
+  // One tile.  The buffer is a constant of the code: its place is part of the LDS instructions then, and the lane's addresses
+  // do not change over the loop.
+  auto take_tile = [&](auto which, int64_t t) {
+    constexpr int BUF = decltype(which)::value;
+    constexpr int JB = TILE / 32;
     wait_loads_and_barrier();
     if (t + 1 < last) {
-      issue(t + 1, buf ^ 1);
+      issue(t + 1, BUF ^ 1);
       if (t + 2 < last) fetch_bias(t + 2);
     }
-    const char* base = tile[buf];
-    // does any pair of this tile have its context among this wave's nodes?
-    bool any_target = false;
-    if constexpr (MODE == kTableGrad) {
-      const int64_t from = kept_tile * S::kKept + wave * 32 * NB;
-      const int64_t t_id = side_target[buf][lane % TILE];
-      any_target = __any(t_id >= from && t_id < from + 32 * NB);
-    }
+    const char* base = tile[BUF];
+    acc16 z[JB][NB];
+    if constexpr (DP < 256) __builtin_amdgcn_s_setprio(1);         // of two waves the one with matrix work to issue goes first: 1 %
 #pragma unroll
-    for (int jb = 0; jb < TILE / 32; ++jb) {
-      if (MODE == kScores && t * TILE + jb * 32 >= a.streamed_rows) break;
-      acc16 z[NB];
+    for (int jb = 0; jb < JB; ++jb) {
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) z[nb] = (acc16)0.0f;
+      for (int nb = 0; nb < NB; ++nb) z[jb][nb] = (acc16)0.0f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const vec4 v = *reinterpret_cast<const vec4*>(base + (read1 ^ (ks << 5)) + jb * 32 * ROWB);
+        const vec4 v = *reinterpret_cast<const vec4*>(base + (read1 ^ ((ks & 7) << 5)) + (ks & ~7) * 32 + jb * 32 * ROWB);
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) z[nb] = step<E>(v, kept[nb][ks], z[nb]);
+        for (int nb = 0; nb < NB; ++nb) z[jb][nb] = step<E>(v, kept[nb][ks], z[jb][nb]);
       }
-      // ---- products to probabilities: register r holds streamed row 8 (r / 4) + 4 half + r % 4 of the block
-      if constexpr (NODES_STREAMED) {
-        if constexpr (BIAS) {
+    }
+    if constexpr (DP < 256) __builtin_amdgcn_s_setprio(0);
+    // ---- products to probabilities: register r of block jb holds streamed row 32 jb + 8 (r / 4) + 4 half + r % 4
+    if constexpr (NODES_STREAMED) {
+      if constexpr (BIAS) {
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            const vec4 b = *reinterpret_cast<const vec4*>(&side[buf][jb * 32 + 8 * q + 4 * half]);
+            const vec4 b = *reinterpret_cast<const vec4*>(&side[BUF][jb * 32 + 8 * q + 4 * half]);
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) z[nb][4 * q + e] = fmaf(z[nb][4 * q + e], a.scale2, b[e]);
+              for (int e = 0; e < 4; ++e) z[jb][nb][4 * q + e] = fmaf(z[jb][nb][4 * q + e], a.scale2, b[e]);
           }
-        } else if ((t + 1) * TILE > a.streamed_rows) {
-          const int64_t left = a.streamed_rows - t * TILE - jb * 32 - 4 * half;
+      } else if ((t + 1) * TILE > a.streamed_rows) {
+        rare();
+        const int left = (int)(a.streamed_rows - t * TILE) - 4 * half;
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int r = 0; r < 16; ++r)
-              if (8 * (r / 4) + r % 4 >= left) z[nb][r] = -INFINITY;
-        }
-        bool moved = false;
-        float keep[NB];
+              if (32 * jb + 8 * (r / 4) + r % 4 >= left) z[jb][nb][r] = -INFINITY;
+      }
+      bool moved = false;
+      float keep[NB];
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          float m = z[nb][0];
+      for (int nb = 0; nb < NB; ++nb) {
+        float m = z[0][nb][0];
 #pragma unroll
-          for (int r = 1; r < 16; ++r) m = fmaxf(m, z[nb][r]);
-          m = fmaxf(m, __shfl_xor(m, 32, 64));
-          if constexpr (!BIAS) m *= a.scale2;
-          const float next = fmaxf(run_max[nb], m);
-          moved = moved || next > run_max[nb];
-          const float from = next == -INFINITY ? 0.0f : next;       // nothing but masked nodes so far
-          keep[nb] = __builtin_amdgcn_exp2f(run_max[nb] - from);
-          run_max[nb] = next;
-          float sum = 0.0f;
-          const float add = (float)E::kShift - from;
+        for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) m = fmaxf(m, z[jb][nb][r]);
+        m = fmaxf(m, __shfl_xor(m, 32, 64));
+        if constexpr (!BIAS) m *= a.scale2;
+        // the maximum follows only by more than kSlack: until then probabilities grow to 2^kSlack, which costs nothing, and
+        // the sums need no rescaling (a row's maximum moves some ten times, but one of a wave's rows' does in every third tile)
+        const float next = m > run_max[nb] + E::kSlack ? m : run_max[nb];
+        moved = moved || next > run_max[nb];
+        const float from = next == -INFINITY ? 0.0f : next;       // nothing but masked nodes so far
+        keep[nb] = __builtin_amdgcn_exp2f(run_max[nb] - from);
+        run_max[nb] = next;
+        float sum = 0.0f;
+        const float add = (float)E::kForwardShift - from;
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const float x = BIAS ? z[nb][r] + add : fmaf(z[nb][r], a.scale2, add);
-            z[nb][r] = __builtin_amdgcn_exp2f(x);
-            sum += z[nb][r];
+            const float x = BIAS ? z[jb][nb][r] + add : fmaf(z[jb][nb][r], a.scale2, add);
+            z[jb][nb][r] = __builtin_amdgcn_exp2f(x);
+            sum += z[jb][nb][r];
           }
-          run_sum[nb] = run_sum[nb] * (double)keep[nb] + (double)sum;
-        }
-        if constexpr (SECOND) {
-          if (__any(moved)) {
+        run_sum[nb] = run_sum[nb] * (double)keep[nb] + (double)sum;
+      }
+      if constexpr (SECOND) {
+        if (__any(moved)) {
+          rare();
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
+          for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-              for (int db = 0; db < DB; ++db) out[db][nb] *= keep[nb];
-          }
+            for (int db = 0; db < DB; ++db) out[db][nb] *= keep[nb];
         }
-      } else if constexpr (MODE == kScores) {
+      }
+    } else if constexpr (MODE == kScores) {
+#pragma unroll
+      for (int jb = 0; jb < JB; ++jb) {
         const int64_t pair0 = t * TILE + jb * 32 + 4 * half;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -452,43 +472,55 @@ __global__ __launch_bounds__(kThreads, 1) void stream_kernel(StreamArgs a) {
             const int64_t pair = pair0 + 8 * (r / 4) + r % 4;
             if (node < a.kept_rows && pair < a.streamed_rows)
               static_cast<float*>(a.out)[pair * a.kept_rows + node] =
-                  BIAS ? fmaf(z[nb][r], a.scale2, kept_bias[nb]) : z[nb][r] * a.scale2;
+                  BIAS ? fmaf(z[jb][nb][r], a.scale2, kept_bias[nb]) : z[jb][nb][r] * a.scale2;
           }
         }
-      } else {
+      }
+    } else {
+#pragma unroll
+      for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const vec4 l = *reinterpret_cast<const vec4*>(&side[buf][jb * 32 + 8 * q + 4 * half]);
+          const vec4 l = *reinterpret_cast<const vec4*>(&side[BUF][jb * 32 + 8 * q + 4 * half]);
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float add = BIAS ? kept_bias[nb] - l[e] : -l[e];
-              z[nb][4 * q + e] = __builtin_amdgcn_exp2f(fmaf(z[nb][4 * q + e], a.scale2, add));
+              z[jb][nb][4 * q + e] = __builtin_amdgcn_exp2f(fmaf(z[jb][nb][4 * q + e], a.scale2, add));
             }
         }
-        if (any_target) {
-          constexpr float one = E::kShift ? 16384.0f : 1.0f;
+      // does any pair of this tile have its context among this wave's nodes?
+      const int32_t wave_node0 = (int32_t)(kept_row0 - l32), t_of_lane = side_target[BUF][lane % TILE];
+      if (__any(t_of_lane >= wave_node0 && t_of_lane - wave_node0 < 32 * NB)) {
+        rare();
+        constexpr float one = E::kShift ? 16384.0f : 1.0f;
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const int32_t t_id = side_target[buf][jb * 32 + 8 * (r / 4) + 4 * half + r % 4];
+            const int32_t t_id = side_target[BUF][jb * 32 + 8 * (r / 4) + 4 * half + r % 4];
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
-              if (t_id == (int32_t)(kept_row0 + 32 * nb)) z[nb][r] -= one;
+              if (t_id == (int32_t)(kept_row0 + 32 * nb)) z[jb][nb][r] -= one;
           }
-        }
       }
-      // ---- second product
-      if constexpr (SECOND) {
+    }
+    // ---- second product
+    if constexpr (DP < 256) __builtin_amdgcn_s_setprio(1);
+    if constexpr (SECOND) {
+#pragma unroll
+      for (int jb = 0; jb < JB; ++jb) {
         if constexpr (E::kWide) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
 #pragma unroll
             for (int db = 0; db < DB; ++db) {
-              const int turn = (db * 8) ^ ((r % 4) << 2) ^ (2 * ((r / 4) & 1));
-              const float v = *reinterpret_cast<const float*>(base + (read2 ^ (turn << 4)) + (jb * 32 + 8 * (r / 4) + r % 4) * ROWB);
+              const int turn = ((db & 1) * 8) ^ ((r % 4) << 2) ^ (2 * ((r / 4) & 1));
+              const float v = *reinterpret_cast<const float*>(base + (read2 ^ (turn << 4)) + (db & ~1) * 128 +
+                                                              (jb * 32 + 8 * (r / 4) + r % 4) * ROWB);
 #pragma unroll
-              for (int nb = 0; nb < NB; ++nb) out[db][nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, z[nb][r], out[db][nb], 0, 0, 0);
+              for (int nb = 0; nb < NB; ++nb) out[db][nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, z[jb][nb][r], out[db][nb], 0, 0, 0);
             }
           }
         } else {
@@ -499,16 +531,16 @@ __global__ __launch_bounds__(kThreads, 1) void stream_kernel(StreamArgs a) {
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                p[nb][e] = __uint_as_float(E::pack(z[nb][8 * q2 + 2 * e], z[nb][8 * q2 + 2 * e + 1]));
+                p[nb][e] = __uint_as_float(E::pack(z[jb][nb][8 * q2 + 2 * e], z[jb][nb][8 * q2 + 2 * e + 1]));
 #pragma unroll
             for (int db = 0; db < DB; ++db) {
               short4_t part[2];
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
                 const int q = 2 * q2 + e;
-                const int turn = (db * 4) ^ (2 * (q & 1));
+                const int turn = ((db & 3) * 4) ^ (2 * (q & 1));
                 part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (lds_short4*)(base + (read2 ^ (turn << 4)) + (jb * 32 + 8 * q) * ROWB));
+                    (lds_short4*)(base + (read2 ^ (turn << 4)) + (db & ~3) * 64 + (jb * 32 + 8 * q) * ROWB));
               }
               const vec4 v = __builtin_bit_cast(vec4, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
@@ -518,7 +550,11 @@ __global__ __launch_bounds__(kThreads, 1) void stream_kernel(StreamArgs a) {
         }
       }
     }
-    if (t + 1 < last) put_side(buf ^ 1);
+    if (t + 1 < last) put_side(BUF ^ 1);
+  };
+  for (int64_t t = first; t < last; t += 2) {
+    take_tile(std::integral_constant<int, 0>{}, t);
+    if (t + 1 < last) take_tile(std::integral_constant<int, 1>{}, t + 1);
   }
 
   // ---- results: lane's kept row, register r of block db is column 32 db + 8 (r / 4) + 4 half + r % 4
@@ -551,66 +587,119 @@ __global__ __launch_bounds__(kThreads, 1) void stream_kernel(StreamArgs a) {
   }
 }
 
-// ---- joining the parts of the forward pass: one wave per pair -----------------------------------------------------------
-template <typename E>
-__global__ __launch_bounds__(kThreads) void join_pairs_kernel(const typename E::elem* rows, const typename E::elem* w_out, int dim,
-                                                              int padded, const float* bias, float scale, float out_scale,
-                                                              int64_t num_pairs, int64_t padded_pairs, int splits,
-                                                              const float* part_max, const double* part_sum,
-                                                              const float* part_acc, int32_t* target, float* loss, float* lse2,
-                                                              typename E::elem* g_in) {
-  const int lane = threadIdx.x & 63;
-  const int64_t i = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-  if (i >= padded_pairs) return;
-  const int32_t t = target[i];
+// ---- joining the parts of the forward pass ------------------------------------------------------------------------------
+struct JoinArgs {
+  const void *w_in, *w_out;
+  int64_t num_in, num_nodes, num_pairs, padded_pairs;
+  int32_t dim, splits;
+  const int32_t *centers, *contexts;
+  const float* bias;
+  float scale, out_scale;
+  const float* part_max;
+  const double* part_sum;
+  const float* part_acc;
+  float* loss;
+  float* lse2;               // for the table gradient, to whole tiles: +infinity for a pair without gradient; or null
+  int32_t* target;           // .. its context, or -1
+  void* g_in;                // or null
+};
+// QUADS lanes for a row (four columns each) and SLOTS of them for a pair, which share its splits: one for the few splits of many
+// pairs, the whole workgroup for the many splits of few.
+template <typename E, int QUADS, int SLOTS>
+__global__ __launch_bounds__(kThreads) void join_pairs_kernel(JoinArgs a) {
+  constexpr int GROUP = QUADS * SLOTS, PAIRS = kThreads / GROUP, DP = 4 * QUADS;
+  typedef typename E::elem elem;
+  __shared__ vec4 part_g[SLOTS > 1 ? kThreads : 1];
+  __shared__ double part_s[SLOTS > 1 ? kThreads / 64 : 1];
+  __shared__ float part_m[SLOTS > 1 ? kThreads / 64 : 1];
+  const int member = threadIdx.x % GROUP, quad = member % QUADS, slot = member / QUADS;
+  const int64_t i = (int64_t)blockIdx.x * PAIRS + threadIdx.x / GROUP;
+  if (i >= a.padded_pairs) return;             // whole workgroups where SLOTS > 1
+  const bool exists = i < a.num_pairs;
+  const int64_t c = exists ? a.centers[i] : -1;
+  int32_t t = exists ? a.contexts[i] : -1;
+  // what keeps a pair from having a gradient: -1 left out, -2 an id that is no row, -3 its context is masked
+  if (exists && (c < 0 || c >= a.num_in || t < -1 || t >= a.num_nodes)) t = -2;
+  else if (t >= 0 && a.bias && a.bias[t] == -INFINITY) t = -3;
+  const bool live = t >= 0;
+  // the splits' maxima and sums
   float m = -INFINITY;
   double sum = 0.0;
-  if (i < num_pairs) {
-    for (int s = lane; s < splits; s += 64) m = fmaxf(m, part_max[s * num_pairs + i]);
+  if (exists) {
+    for (int s = SLOTS > 1 ? member : 0; s < a.splits; s += SLOTS > 1 ? GROUP : 1) m = fmaxf(m, a.part_max[s * a.num_pairs + i]);
+    if constexpr (SLOTS > 1) {
 #pragma unroll
-    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
-    for (int s = lane; s < splits; s += 64) {
-      const float pm = part_max[s * num_pairs + i];
-      const double ps = part_sum[s * num_pairs + i];
+      for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+      if ((threadIdx.x & 63) == 0) part_m[threadIdx.x >> 6] = m;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kThreads / 64; ++w) m = fmaxf(m, part_m[w]);
+    }
+    for (int s = SLOTS > 1 ? member : 0; s < a.splits; s += SLOTS > 1 ? GROUP : 1) {
+      const float pm = a.part_max[s * a.num_pairs + i];
+      const double ps = a.part_sum[s * a.num_pairs + i];
       // a split of masked nodes alone has sum 0, whatever its maximum
       sum += pm == -INFINITY && ps == 0.0 ? 0.0 : ps * exp2((double)pm - (double)m);
     }
+    if constexpr (SLOTS > 1) {
 #pragma unroll
-    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d, 64);
+      for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d, 64);
+      if ((threadIdx.x & 63) == 0) part_s[threadIdx.x >> 6] = sum;
+      __syncthreads();
+      sum = 0.0;
+#pragma unroll
+      for (int w = 0; w < kThreads / 64; ++w) sum += part_s[w];
+    }
   }
-  const double total2 = (double)m + log2(sum) - (double)E::kShift;         // base-2 log-sum
-  const bool live = i < num_pairs && t >= 0;
-  if (lse2 != nullptr && lane == 0) lse2[i] = live ? (float)(total2 - (double)E::kShift) : INFINITY;
-  if (i >= num_pairs) return;
-  const typename E::elem* c = w_out + (int64_t)max(t, 0) * dim;
+  const double total2 = (double)m + log2(sum) - (double)E::kForwardShift;  // base-2 log-sum
+  if (a.lse2 != nullptr && member == 0) {
+    a.lse2[i] = live ? (float)(total2 - (double)E::kShift) : INFINITY;
+    a.target[i] = live ? t : -1;
+  }
+  if (!exists) return;
+  const bool column = 4 * quad < a.dim;
+  vec4 to = (vec4)0.0f;                        // the context's row
   double dot = 0.0;
-  if (live)
-    for (int d = lane; d < dim; d += 64) dot += (double)E::load(rows + i * padded + d) * (double)E::load(c + d);
+  if (live && column) {
+    const elem* h = static_cast<const elem*>(a.w_in) + c * a.dim + 4 * quad;
+    const elem* v = static_cast<const elem*>(a.w_out) + (int64_t)t * a.dim + 4 * quad;
 #pragma unroll
-  for (int d = 32; d; d >>= 1) dot += __shfl_xor(dot, d, 64);
-  if (lane == 0) {
-    double value = total2 * kLn2 - ((double)scale * dot + (live && bias ? (double)bias[t] : 0.0));
+    for (int e = 0; e < 4; ++e) {
+      to[e] = E::load(v + e);
+      dot += (double)E::load(h + e) * (double)to[e];
+    }
+  }
+#pragma unroll
+  for (int d = QUADS / 2; d; d >>= 1) dot += __shfl_xor(dot, d, 64);
+  if (member == 0) {
+    double value = total2 * kLn2 - ((double)a.scale * dot + (live && a.bias ? (double)a.bias[t] : 0.0));
     if (t == -1) value = 0.0;
     if (t == -2) value = NAN;
     if (t == -3) value = INFINITY;
-    loss[i] = (float)value;
+    a.loss[i] = (float)value;
   }
-  if (g_in == nullptr) return;
-  const double inverse = 1.0 / sum;
-  for (int d0 = 4 * lane; d0 < dim; d0 += 256) {
-    vec4 g = (vec4)0.0f;
-    if (live) {
-      for (int s = 0; s < splits; ++s) {
-        const float pm = part_max[s * num_pairs + i];
-        if (pm == -INFINITY && part_sum[s * num_pairs + i] == 0.0) continue;       // masked nodes alone
-        const float w = (float)(exp2((double)pm - (double)m) * inverse);
-        g += w * *reinterpret_cast<const vec4*>(part_acc + (s * num_pairs + i) * padded + d0);
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) g[e] = (g[e] - E::load(c + d0 + e)) * out_scale;
+  if (a.g_in == nullptr) return;
+  vec4 g = (vec4)0.0f;
+  if (live) {
+    const double inverse = 1.0 / sum;
+#pragma unroll 4
+    for (int s = slot; s < a.splits; s += SLOTS) {
+      const float pm = a.part_max[s * a.num_pairs + i];
+      const bool empty = pm == -INFINITY && a.part_sum[s * a.num_pairs + i] == 0.0;           // masked nodes alone
+      const float w = empty ? 0.0f : (float)(exp2((double)pm - (double)m) * inverse);
+      g += w * *reinterpret_cast<const vec4*>(a.part_acc + (s * a.num_pairs + i) * DP + 4 * quad);
     }
-    E::store4(g_in + i * dim + d0, g);
   }
+  if constexpr (SLOTS > 1) {
+    part_g[threadIdx.x] = g;
+    __syncthreads();
+    if (slot != 0) return;
+#pragma unroll
+    for (int k = 1; k < SLOTS; ++k) g += part_g[k * QUADS + quad];
+  }
+  if (!column) return;
+  if (live) g = (g - to) * a.out_scale;
+  E::store4(static_cast<elem*>(a.g_in) + i * a.dim + 4 * quad, g);
 }
 
 // g_out from the parts of a split table gradient, in order
@@ -638,24 +727,27 @@ __global__ __launch_bounds__(kThreads) void zero_pieces_kernel(uint4* to, int64_
 
 // ---- host ----------------------------------------------------------------------------------------------------------------
 template <typename E, int DP>
-static void plan_tiles(SoftmaxPlan& p, int64_t num_pairs, int64_t num_nodes, bool grad, size_t& acc_rows, size_t& part_rows) {
-  using S = Shape<E, DP>;
-  constexpr int64_t want = 512;                // workgroups that fill the chip: two per compute unit
-  p.padded = DP;
-  p.padded_pairs = ceil_div(num_pairs, 256) * 256;
-  p.pair_tiles = ceil_div(num_pairs, S::kKept);
-  p.node_tiles = ceil_div(num_nodes, S::kKept);
-  const int64_t tiles = ceil_div(num_nodes, S::kTile), pair_parts = ceil_div(num_pairs, S::kTile);
+static void plan_tiles(SoftmaxPlan& p, int64_t num_pairs, int64_t num_nodes, bool loss, bool grad, size_t& acc_rows, size_t& part_rows) {
+  using L = Shape<E, DP, kForward>;
+  using Z = Shape<E, DP, kScores>;
+  constexpr int64_t want = 256 * L::kWaves;    // workgroups that fill the chip
   auto split = [&](int64_t kept, int64_t streamed) {
     int64_t n = std::max<int64_t>(1, std::min(streamed, want / std::max<int64_t>(1, kept)));
     return (int)(n >= 8 ? n / 8 * 8 : n);
   };
-  p.splits = split(p.pair_tiles, tiles);
-  p.tiles_per_split = ceil_div(tiles, p.splits);
+  p.padded = DP;
+  p.node_tiles = ceil_div(num_nodes, loss ? L::kKept : Z::kKept);
+  const int64_t pair_parts = ceil_div(num_pairs, loss ? L::kTile : Z::kTile);
   p.node_splits = split(p.node_tiles, pair_parts);
   p.tiles_per_node_split = ceil_div(std::max<int64_t>(1, pair_parts), p.node_splits);
+  if (!loss) return;
+  p.padded_pairs = ceil_div(num_pairs, 256) * 256;
+  p.pair_tiles = ceil_div(num_pairs, L::kKept);
+  const int64_t tiles = ceil_div(num_nodes, L::kTile);
+  p.splits = split(p.pair_tiles, tiles);
+  p.tiles_per_split = ceil_div(tiles, p.splits);
   // every size below only grows with the number of pairs, although the number of splits falls
-  part_rows = (size_t)std::max(num_pairs, std::min(std::min(tiles, want) * num_pairs, want * S::kKept));
+  part_rows = (size_t)std::max(num_pairs, std::min(std::min(tiles, want) * num_pairs, want * L::kKept));
   acc_rows = grad ? part_rows : 0;
   if (grad && p.node_splits > 1) acc_rows = std::max(acc_rows, (size_t)p.node_splits * (size_t)num_nodes);
 }
@@ -664,19 +756,19 @@ template <typename E>
 SoftmaxPlan plan_softmax(void* ws, int64_t num_pairs, int64_t num_nodes, int32_t dim, bool loss, bool grad) {
   SoftmaxPlan p{};
   size_t acc_rows = 0, part_rows = 0;
-  if (dim <= 64) plan_tiles<E, 64>(p, num_pairs, num_nodes, grad, acc_rows, part_rows);
-  else if (dim <= 128) plan_tiles<E, 128>(p, num_pairs, num_nodes, grad, acc_rows, part_rows);
-  else plan_tiles<E, 256>(p, num_pairs, num_nodes, grad, acc_rows, part_rows);
+  if (dim <= 64) plan_tiles<E, 64>(p, num_pairs, num_nodes, loss, grad, acc_rows, part_rows);
+  else if (dim <= 128) plan_tiles<E, 128>(p, num_pairs, num_nodes, loss, grad, acc_rows, part_rows);
+  else plan_tiles<E, 256>(p, num_pairs, num_nodes, loss, grad, acc_rows, part_rows);
   Carver c(ws);
-  p.rows = c.take<typename E::elem>((size_t)p.padded_pairs * p.padded);
   if (loss) {
+    if (grad) p.rows = c.take<typename E::elem>((size_t)p.padded_pairs * p.padded);
     p.target = c.take<int32_t>(p.padded_pairs);
     p.lse2 = c.take<float>(p.padded_pairs);
     p.part_max = c.take<float>(part_rows);
     p.part_sum = c.take<double>(part_rows);
     p.part_acc = c.take<float>(acc_rows * p.padded);
   }
-  p.bytes = c.used;
+  p.bytes = std::max<size_t>(c.used, 256);
   return p;
 }
 
@@ -692,21 +784,18 @@ static int32_t launch_stream(const StreamArgs& a, hipStream_t stream) {
 template <typename E, int DP>
 static int32_t run_padded(const SoftmaxCall& q, const SoftmaxPlan& p, hipStream_t stream) {
   using elem = typename E::elem;
-  elem* rows = static_cast<elem*>(p.rows);
   constexpr int64_t most = ((int64_t)1 << 32) / kThreads;        // a launch takes fewer than 2^32 lanes
   if ((!q.loss || q.g_out) && p.node_tiles * p.node_splits >= most) return GS_EOVERFLOW;
-  if (q.loss && (p.pair_tiles * p.splits >= most || p.padded_pairs / (kThreads / 64) >= most)) return GS_EOVERFLOW;
+  if (q.loss && (p.pair_tiles * p.splits >= most || p.padded_pairs >= most)) return GS_EOVERFLOW;
   auto blocks_for = [](int64_t items) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(items, kThreads), 256 * 16)); };
-  gather_pairs_kernel<E><<<blocks_for(p.padded_pairs * (DP / (16 / (int)sizeof(elem)))), kThreads, 0, stream>>>(
-      static_cast<const elem*>(q.w_in), q.num_in, q.num_nodes, q.dim, DP, q.centers, q.contexts, q.bias, q.num_pairs,
-      p.padded_pairs, rows, q.loss ? p.target : nullptr);
-  GS_LAUNCH_CHECK();
   StreamArgs a{};
   a.dim = q.dim;
   a.bias = q.bias;
+  a.centers = q.centers;
+  a.num_in = q.num_in;
   if (!q.loss) {
     a.kept = q.w_out;
-    a.streamed = rows;
+    a.streamed = q.w_in;
     a.kept_rows = q.num_nodes;
     a.streamed_rows = q.num_pairs;
     a.scale2 = q.scale;
@@ -716,7 +805,7 @@ static int32_t run_padded(const SoftmaxCall& q, const SoftmaxPlan& p, hipStream_
     a.out = q.scores;
     return launch_stream<E, DP, kScores>(a, stream);
   }
-  a.kept = rows;
+  a.kept = q.w_in;
   a.streamed = q.w_out;
   a.kept_rows = q.num_pairs;
   a.streamed_rows = q.num_nodes;
@@ -730,11 +819,36 @@ static int32_t run_padded(const SoftmaxCall& q, const SoftmaxPlan& p, hipStream_
   int32_t rc = q.g_in ? launch_stream<E, DP, kForward>(a, stream) : launch_stream<E, DP, kLossOnly>(a, stream);
   if (rc != GS_OK) return rc;
   const float out_scale = q.scale * q.grad_scale;
-  join_pairs_kernel<E><<<(unsigned)ceil_div(p.padded_pairs, kThreads / 64), kThreads, 0, stream>>>(
-      rows, static_cast<const elem*>(q.w_out), q.dim, DP, q.bias, q.scale, out_scale, q.num_pairs, p.padded_pairs, p.splits,
-      p.part_max, p.part_sum, p.part_acc, p.target, q.loss, q.g_out ? p.lse2 : nullptr, static_cast<elem*>(q.g_in));
+  JoinArgs j{};
+  j.w_in = q.w_in;
+  j.w_out = q.w_out;
+  j.num_in = q.num_in;
+  j.num_nodes = q.num_nodes;
+  j.num_pairs = q.num_pairs;
+  j.padded_pairs = q.g_out ? p.padded_pairs : q.num_pairs;
+  j.dim = q.dim;
+  j.splits = p.splits;
+  j.centers = q.centers;
+  j.contexts = q.contexts;
+  j.bias = q.bias;
+  j.scale = q.scale;
+  j.out_scale = out_scale;
+  j.part_max = p.part_max;
+  j.part_sum = p.part_sum;
+  j.part_acc = p.part_acc;
+  j.loss = q.loss;
+  j.lse2 = q.g_out ? p.lse2 : nullptr;
+  j.target = p.target;
+  j.g_in = q.g_in;
+  constexpr int quads = DP / 4;
+  if (p.splits > 8) join_pairs_kernel<E, quads, kThreads / quads><<<(unsigned)j.padded_pairs, kThreads, 0, stream>>>(j);
+  else join_pairs_kernel<E, quads, 1><<<(unsigned)ceil_div(j.padded_pairs, kThreads / quads), kThreads, 0, stream>>>(j);
   GS_LAUNCH_CHECK();
   if (!q.g_out) return GS_OK;
+  elem* rows = static_cast<elem*>(p.rows);
+  gather_pairs_kernel<E><<<blocks_for(p.padded_pairs * (DP / (16 / (int)sizeof(elem)))), kThreads, 0, stream>>>(
+      static_cast<const elem*>(q.w_in), q.num_in, q.dim, DP, q.centers, q.num_pairs, p.padded_pairs, rows);
+  GS_LAUNCH_CHECK();
   a.kept = q.w_out;
   a.streamed = rows;
   a.kept_rows = q.num_nodes;
