@@ -45,7 +45,7 @@ enum { kLossOnly = 0, kForward = 1, kTableGrad = 2, kScores = 3 };
 
 // Sizes and places in the workspace (base null: sizes alone).
 struct SoftmaxPlan {
-  int padded;                // columns of a copied row: 64, 128 or 256
+  int padded;                // columns of a copied row: dim up to a multiple of 32
   int64_t padded_pairs, pair_tiles, node_tiles;      // workgroups along the kept rows, either way
   int splits, node_splits;                           // parts of the streamed rows
   int64_t tiles_per_split, tiles_per_node_split;
@@ -143,30 +143,41 @@ struct F16 {
 
 namespace {
 
-// Tile shapes: kept rows per wave 32 * kNB, streamed rows per tile kTile.
+// Tile shapes: kept rows per wave 32 * kNB, streamed rows per tile kTile, rows padded to DP columns, a multiple of 32.
 template <typename E, int DP, int MODE>
 struct Shape {
   static constexpr int kRowBytes = DP * (int)sizeof(typename E::elem);
-  static constexpr int kPieces = kRowBytes / 16;                   // 16-byte pieces of a row: 8, 16, 32 or 64
+  static constexpr int kPieces = kRowBytes / 16;                   // 16-byte pieces of a row: a multiple of 4 (fp32: of 8)
   static constexpr int kPerPiece = 16 / (int)sizeof(typename E::elem);
   static constexpr int kSteps = kPieces / 2;                       // pieces a half wave takes in the first product
-  static constexpr int kNB = MODE != kScores || E::kWide || DP == 256 ? 1 : 2;
-  static constexpr int kTile = MODE == kScores || DP == 256 ? 32 : 64;
-  // waves per SIMD to leave registers for, and as many workgroups per compute unit: two, so that one's exponentials run beside the
-  // other's matrix instructions, but for fp32 rows of 256, which take 256 registers for the kept rows and the sums alone
-  static constexpr int kWaves = E::kWide && DP == 256 ? 1 : 2;
   static constexpr int kBlocks = DP / 32;                          // 32-column blocks of the second product
+  // Registers: DP / 2 for the sums, DP / 4 (fp32: DP / 2) for the kept rows, 16 for each 32 streamed rows.  Two waves per SIMD, so
+  // that one's exponentials run beside the other's matrix instructions, where 256 registers hold that.
+  static constexpr int kWaves = E::kWide && DP > 192 ? 1 : 2;
+  static constexpr int kTile = MODE == kScores || DP > (E::kWide ? 128 : 192) ? 32 : 64;
+  static constexpr int kNB = MODE == kScores && !E::kWide && DP <= 128 ? 2 : 1;
   static constexpr int kKept = 32 * kNB * 4;                       // kept rows per workgroup
-  static constexpr int kLoads = kTile * kPieces / kThreads;        // 16-byte loads per lane and tile
+  static constexpr int kChunks = kTile * kPieces / 64;             // loads of a wave (1 KB) that make a tile
+  static constexpr int kLoads = (kChunks + 3) / 4;                 // per wave
+  // pieces that are swapped among each other: as many as keep rows apart that begin at the same banks (64 of 4 bytes)
+  static constexpr int kSwapped = kPieces % 16 == 0 ? 16 : kPieces % 8 == 0 ? 8 : 4;
 };
 
 // Where a piece lies inside its row.  Reads of the first product take one piece of 32 consecutive rows, those of the second
 // four neighbouring pieces of four consecutive rows; both spread over all banks.
-template <int PIECES>
+template <int SWAPPED>
 __device__ __forceinline__ constexpr int swap_of(int row) {
-  return PIECES == 8 ? ((((row >> 1) & 1) << 2) | ((row >> 2) & 3)) : (((row & 3) << 2) | ((row >> 2) & 3));
+  return SWAPPED == 16 ? (((row & 3) << 2) | ((row >> 2) & 3)) : SWAPPED == 8 ? ((((row >> 1) & 1) << 2) | ((row >> 2) & 3)) : ((row >> 2) & 3);
 }
 
+// 16 bytes of a lane into LDS at dst + 16 lane: from its own address, or from a place in a range that is the wave's (pieces
+// outside of the range are zeros).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t range_of(const void* base, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00027000);
+}
+__device__ __forceinline__ void load_piece_to_lds(__amdgpu_buffer_rsrc_t range, int offset, void* dst) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(range, (__attribute__((address_space(3))) void*)dst, 16, offset, 0, 0, 0);
+}
 __device__ __forceinline__ void load_piece_to_lds(const void* src, void* dst) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
                                    (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
@@ -236,7 +247,7 @@ template <typename E, int DP, int MODE, bool BIAS>
 __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream_kernel(StreamArgs a) {
   using S = Shape<E, DP, MODE>;
   using elem = typename E::elem;
-  constexpr int NB = S::kNB, TILE = S::kTile, ROWB = S::kRowBytes, PIECES = S::kPieces, KS = S::kSteps, DB = S::kBlocks;
+  constexpr int NB = S::kNB, TILE = S::kTile, ROWB = S::kRowBytes, PIECES = S::kPieces, KS = S::kSteps, DB = S::kBlocks, SWAPPED = S::kSwapped;
   constexpr bool NODES_STREAMED = MODE == kLossOnly || MODE == kForward;
   constexpr bool SECOND = MODE == kForward || MODE == kTableGrad;
   __shared__ __attribute__((aligned(1024))) char tile[2][TILE * ROWB];
@@ -283,41 +294,53 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
     }
   }
 
-  // ---- staging: lane's loads go to slots wave * kLoads * 64 + 64 n + lane of a tile
+  // ---- staging: a wave's load number n fills the 64 pieces of chunk 4 n + wave of a tile
   float row_bias[S::kLoads];                   // nodes streamed, with bias: of the rows of the next tile to ask for
   float side_value = 0.0f;
   int32_t side_id = -1;
-  auto slot_row = [&](int n) { return ((wave * S::kLoads + n) * 64 + lane) / PIECES; };
+  auto slot_row = [&](int n) { return ((4 * n + wave) * 64 + lane) / PIECES; };
+  auto has_chunk = [&](int n) { return S::kChunks % 4 == 0 || 4 * n + wave < S::kChunks; };
   auto fetch_bias = [&](int64_t t) {
     if constexpr (NODES_STREAMED && BIAS) {
 #pragma unroll
       for (int n = 0; n < S::kLoads; ++n) {
         const int64_t row = t * TILE + slot_row(n);
-        row_bias[n] = row < a.streamed_rows ? a.bias[row] : -INFINITY;
+        row_bias[n] = has_chunk(n) && row < a.streamed_rows ? a.bias[row] : -INFINITY;
       }
     }
   };
-  auto issue = [&](int64_t t, int buf) {
+  constexpr int OUTSIDE = 1 << 30;
+  const int streamed_bytes = (MODE == kTableGrad ? DP : a.dim) * (int)sizeof(elem);
+  int place[S::kLoads];                        // in the tile's range
 #pragma unroll
-    for (int n = 0; n < S::kLoads; ++n) {
-      const int r = slot_row(n);
-      const int piece = (lane % PIECES) ^ swap_of<PIECES>(r);
-      const int64_t row = t * TILE + r;
-      const elem* src;
-      if constexpr (NODES_STREAMED) {
-        bool read = row < a.streamed_rows && piece * S::kPerPiece < a.dim;
-        if constexpr (BIAS) read = read && row_bias[n] != -INFINITY;
-        src = read ? static_cast<const elem*>(a.streamed) + row * a.dim + piece * S::kPerPiece
-                   : reinterpret_cast<const elem*>(zero_piece);
-      } else if constexpr (MODE == kScores) {
+  for (int n = 0; n < S::kLoads; ++n) {
+    const int r = slot_row(n);
+    const int piece = (((4 * n + wave) * 64 + lane) % PIECES) ^ swap_of<SWAPPED>(r);
+    place[n] = piece * 16 < streamed_bytes ? r * streamed_bytes + piece * 16 : OUTSIDE;
+    if (MODE == kScores) place[n] = piece;
+  }
+  auto issue = [&](int64_t t, int buf) {
+    if constexpr (MODE == kScores) {
+#pragma unroll
+      for (int n = 0; n < S::kLoads; ++n) {
+        if (!has_chunk(n)) continue;
+        const int64_t row = t * TILE + slot_row(n);
         const int64_t c = row < a.streamed_rows ? a.centers[row] : -1;
         const bool known = c >= 0 && c < a.num_in;
-        src = known && piece * S::kPerPiece < a.dim ? static_cast<const elem*>(a.streamed) + c * a.dim + piece * S::kPerPiece
-                                                   : reinterpret_cast<const elem*>(known ? zero_piece : nan_piece<E>);
-      } else {
-        src = static_cast<const elem*>(a.streamed) + row * DP + piece * S::kPerPiece;
+        const elem* src = known && place[n] * S::kPerPiece < a.dim ? static_cast<const elem*>(a.streamed) + c * a.dim + place[n] * S::kPerPiece
+                                                                 : reinterpret_cast<const elem*>(known ? zero_piece : nan_piece<E>);
+        load_piece_to_lds(src, &tile[buf][(4 * n + wave) * 1024]);
       }
-      load_piece_to_lds(src, &tile[buf][(wave * S::kLoads + n) * 1024]);
+    } else {
+      const int64_t rows = min((int64_t)TILE, (MODE == kTableGrad ? all_tiles * TILE : a.streamed_rows) - t * TILE);
+      const __amdgpu_buffer_rsrc_t range = range_of(static_cast<const char*>(a.streamed) + t * TILE * streamed_bytes, (int)rows * streamed_bytes);
+#pragma unroll
+      for (int n = 0; n < S::kLoads; ++n) {
+        if (!has_chunk(n)) continue;
+        int at = place[n];
+        if constexpr (NODES_STREAMED && BIAS) at = row_bias[n] != -INFINITY ? at : OUTSIDE;
+        load_piece_to_lds(range, at, &tile[buf][(4 * n + wave) * 1024]);
+      }
     }
     if (tid < TILE) {
       const int64_t row = t * TILE + tid;
@@ -353,15 +376,15 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
     run_sum[nb] = 0.0;
   }
 
-  // lane's parts of the LDS addresses; the swap turns bits 4 to 7 of them, what lies above is added
-  const int read1 = l32 * ROWB + ((half ^ swap_of<PIECES>(l32)) << 4);
+  // lane's parts of the LDS addresses; the swap turns bits of them that a row's place leaves zero, what lies above is added
+  constexpr int SWAP_KS = SWAPPED / 2 - 1;     // steps of the first product inside the swapped pieces
+  const int read1 = l32 * ROWB + ((half ^ swap_of<SWAPPED>(l32)) << 4);
   int read2;
   if constexpr (E::kWide) {
     read2 = (((l32 >> 2) ^ half) << 4) + (l32 & 3) * 4 + half * 4 * ROWB;
   } else {
     const int li = lane & 15, r = li >> 2;
-    constexpr int hi = PIECES == 8 ? 1 : 0;
-    const int turn = hi ? (((r >> 1) & 1) << 2) : (r << 2);
+    const int turn = SWAPPED == 16 ? r << 2 : SWAPPED == 8 ? ((r >> 1) & 1) << 2 : 0;
     const int piece = (((lane >> 4) & 1) * 2 + ((li & 3) >> 1)) ^ turn ^ half;
     read2 = (piece << 4) + (li & 1) * 8 + (4 * half + r) * ROWB;
   }
@@ -384,19 +407,19 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
     }
     const char* base = tile[BUF];
     acc16 z[JB][NB];
-    if constexpr (DP < 256) __builtin_amdgcn_s_setprio(1);         // of two waves the one with matrix work to issue goes first: 1 %
+    if constexpr (S::kWaves > 1) __builtin_amdgcn_s_setprio(1);         // of two waves the one with matrix work to issue goes first: 1 %
 #pragma unroll
     for (int jb = 0; jb < JB; ++jb) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) z[jb][nb] = (acc16)0.0f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const vec4 v = *reinterpret_cast<const vec4*>(base + (read1 ^ ((ks & 7) << 5)) + (ks & ~7) * 32 + jb * 32 * ROWB);
+        const vec4 v = *reinterpret_cast<const vec4*>(base + (read1 ^ ((ks & SWAP_KS) << 5)) + (ks & ~SWAP_KS) * 32 + jb * 32 * ROWB);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) z[jb][nb] = step<E>(v, kept[nb][ks], z[jb][nb]);
       }
     }
-    if constexpr (DP < 256) __builtin_amdgcn_s_setprio(0);
+    if constexpr (S::kWaves > 1) __builtin_amdgcn_s_setprio(0);
     // ---- products to probabilities: register r of block jb holds streamed row 32 jb + 8 (r / 4) + 4 half + r % 4
     if constexpr (NODES_STREAMED) {
       if constexpr (BIAS) {
@@ -507,7 +530,7 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
       }
     }
     // ---- second product
-    if constexpr (DP < 256) __builtin_amdgcn_s_setprio(1);
+    if constexpr (S::kWaves > 1) __builtin_amdgcn_s_setprio(1);
     if constexpr (SECOND) {
 #pragma unroll
       for (int jb = 0; jb < JB; ++jb) {
@@ -516,8 +539,9 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
           for (int r = 0; r < 16; ++r) {
 #pragma unroll
             for (int db = 0; db < DB; ++db) {
-              const int turn = ((db & 1) * 8) ^ ((r % 4) << 2) ^ (2 * ((r / 4) & 1));
-              const float v = *reinterpret_cast<const float*>(base + (read2 ^ (turn << 4)) + (db & ~1) * 128 +
+              constexpr int swap_db = SWAPPED == 16 ? 1 : 0;         // blocks of eight pieces
+              const int turn = ((db & swap_db) * 8) ^ (SWAPPED == 16 ? (r % 4) << 2 : ((r % 4) >> 1) << 2) ^ (2 * ((r / 4) & 1));
+              const float v = *reinterpret_cast<const float*>(base + (read2 ^ (turn << 4)) + (db & ~swap_db) * 128 +
                                                               (jb * 32 + 8 * (r / 4) + r % 4) * ROWB);
 #pragma unroll
               for (int nb = 0; nb < NB; ++nb) out[db][nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, z[jb][nb][r], out[db][nb], 0, 0, 0);
@@ -538,9 +562,10 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
                 const int q = 2 * q2 + e;
-                const int turn = ((db & 3) * 4) ^ (2 * (q & 1));
+                constexpr int swap_db = SWAPPED / 4 - 1;             // blocks of four pieces
+                const int turn = ((db & swap_db) * 4) ^ (2 * (q & 1));
                 part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (lds_short4*)(base + (read2 ^ (turn << 4)) + (db & ~3) * 64 + (jb * 32 + 8 * q) * ROWB));
+                    (lds_short4*)(base + (read2 ^ (turn << 4)) + (db & ~swap_db) * 64 + (jb * 32 + 8 * q) * ROWB));
               }
               const vec4 v = __builtin_bit_cast(vec4, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
@@ -591,7 +616,7 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
 struct JoinArgs {
   const void *w_in, *w_out;
   int64_t num_in, num_nodes, num_pairs, padded_pairs;
-  int32_t dim, splits;
+  int32_t dim, padded, splits;
   const int32_t *centers, *contexts;
   const float* bias;
   float scale, out_scale;
@@ -607,7 +632,7 @@ struct JoinArgs {
 // pairs, the whole workgroup for the many splits of few.
 template <typename E, int QUADS, int SLOTS>
 __global__ __launch_bounds__(kThreads) void join_pairs_kernel(JoinArgs a) {
-  constexpr int GROUP = QUADS * SLOTS, PAIRS = kThreads / GROUP, DP = 4 * QUADS;
+  constexpr int GROUP = QUADS * SLOTS, PAIRS = kThreads / GROUP;
   typedef typename E::elem elem;
   __shared__ vec4 part_g[SLOTS > 1 ? kThreads : 1];
   __shared__ double part_s[SLOTS > 1 ? kThreads / 64 : 1];
@@ -657,7 +682,7 @@ __global__ __launch_bounds__(kThreads) void join_pairs_kernel(JoinArgs a) {
     a.target[i] = live ? t : -1;
   }
   if (!exists) return;
-  const bool column = 4 * quad < a.dim;
+  const bool column = 4 * quad < a.dim;        // the lanes beyond read nothing
   vec4 to = (vec4)0.0f;                        // the context's row
   double dot = 0.0;
   if (live && column) {
@@ -680,14 +705,14 @@ __global__ __launch_bounds__(kThreads) void join_pairs_kernel(JoinArgs a) {
   }
   if (a.g_in == nullptr) return;
   vec4 g = (vec4)0.0f;
-  if (live) {
+  if (live && column) {
     const double inverse = 1.0 / sum;
 #pragma unroll 4
     for (int s = slot; s < a.splits; s += SLOTS) {
       const float pm = a.part_max[s * a.num_pairs + i];
       const bool empty = pm == -INFINITY && a.part_sum[s * a.num_pairs + i] == 0.0;           // masked nodes alone
       const float w = empty ? 0.0f : (float)(exp2((double)pm - (double)m) * inverse);
-      g += w * *reinterpret_cast<const vec4*>(a.part_acc + (s * a.num_pairs + i) * DP + 4 * quad);
+      g += w * *reinterpret_cast<const vec4*>(a.part_acc + (s * a.num_pairs + i) * a.padded + 4 * quad);
     }
   }
   if constexpr (SLOTS > 1) {
@@ -726,6 +751,21 @@ __global__ __launch_bounds__(kThreads) void zero_pieces_kernel(uint4* to, int64_
 }  // namespace
 
 // ---- host ----------------------------------------------------------------------------------------------------------------
+// f with the padded number of columns as a constant
+template <typename R, typename F>
+static R with_padded(int dim, F f) {
+  switch ((dim + 31) / 32) {
+    case 1: return f(std::integral_constant<int, 32>{});
+    case 2: return f(std::integral_constant<int, 64>{});
+    case 3: return f(std::integral_constant<int, 96>{});
+    case 4: return f(std::integral_constant<int, 128>{});
+    case 5: return f(std::integral_constant<int, 160>{});
+    case 6: return f(std::integral_constant<int, 192>{});
+    case 7: return f(std::integral_constant<int, 224>{});
+    default: return f(std::integral_constant<int, 256>{});
+  }
+}
+
 template <typename E, int DP>
 static void plan_tiles(SoftmaxPlan& p, int64_t num_pairs, int64_t num_nodes, bool loss, bool grad, size_t& acc_rows, size_t& part_rows) {
   using L = Shape<E, DP, kForward>;
@@ -756,9 +796,10 @@ template <typename E>
 SoftmaxPlan plan_softmax(void* ws, int64_t num_pairs, int64_t num_nodes, int32_t dim, bool loss, bool grad) {
   SoftmaxPlan p{};
   size_t acc_rows = 0, part_rows = 0;
-  if (dim <= 64) plan_tiles<E, 64>(p, num_pairs, num_nodes, loss, grad, acc_rows, part_rows);
-  else if (dim <= 128) plan_tiles<E, 128>(p, num_pairs, num_nodes, loss, grad, acc_rows, part_rows);
-  else plan_tiles<E, 256>(p, num_pairs, num_nodes, loss, grad, acc_rows, part_rows);
+  with_padded<int>(dim, [&](auto padded) {
+    plan_tiles<E, decltype(padded)::value>(p, num_pairs, num_nodes, loss, grad, acc_rows, part_rows);
+    return 0;
+  });
   Carver c(ws);
   if (loss) {
     if (grad) p.rows = c.take<typename E::elem>((size_t)p.padded_pairs * p.padded);
@@ -827,6 +868,7 @@ static int32_t run_padded(const SoftmaxCall& q, const SoftmaxPlan& p, hipStream_
   j.num_pairs = q.num_pairs;
   j.padded_pairs = q.g_out ? p.padded_pairs : q.num_pairs;
   j.dim = q.dim;
+  j.padded = DP;
   j.splits = p.splits;
   j.centers = q.centers;
   j.contexts = q.contexts;
@@ -840,7 +882,7 @@ static int32_t run_padded(const SoftmaxCall& q, const SoftmaxPlan& p, hipStream_
   j.lse2 = q.g_out ? p.lse2 : nullptr;
   j.target = p.target;
   j.g_in = q.g_in;
-  constexpr int quads = DP / 4;
+  constexpr int quads = DP <= 64 ? 16 : DP <= 128 ? 32 : 64;
   if (p.splits > 8) join_pairs_kernel<E, quads, kThreads / quads><<<(unsigned)j.padded_pairs, kThreads, 0, stream>>>(j);
   else join_pairs_kernel<E, quads, 1><<<(unsigned)ceil_div(j.padded_pairs, kThreads / quads), kThreads, 0, stream>>>(j);
   GS_LAUNCH_CHECK();
@@ -878,9 +920,7 @@ int32_t run_softmax(const SoftmaxCall& q, const SoftmaxPlan& p, hipStream_t stre
     GS_LAUNCH_CHECK();
     return GS_OK;
   }
-  if (p.padded == 64) return run_padded<E, 64>(q, p, stream);
-  if (p.padded == 128) return run_padded<E, 128>(q, p, stream);
-  return run_padded<E, 256>(q, p, stream);
+  return with_padded<int32_t>(q.dim, [&](auto padded) { return run_padded<E, decltype(padded)::value>(q, p, stream); });
 }
 
 #endif  // GS_SOFTMAX_KERNELS

@@ -278,3 +278,19 @@ def test_a_larger_workspace_serves_and_a_smaller_one_does_not(gs):
     with pytest.raises(gs.GsError) as e:
         gs.gs_softmax_loss(w_in, w_out, c, t, ws=ws[:need - 256])
     assert e.value.status == gs.GS_EWORKSPACE
+
+
+@pytest.mark.parametrize("fmt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("dim", [32, 56, 96, 120, 160, 192, 224, 240])
+def test_every_padding_of_a_row(gs, fmt, dim):
+    """Rows are padded to a multiple of 32 columns; each has its own layout in LDS."""
+    w_in, w_out, c, t = make(150, 333, dim, fmt, rows=60)
+    bias = torch.randn(333, generator=torch.Generator().manual_seed(dim))
+    bias[::7] = -math.inf
+    t = torch.where(t % 7 == 0, t + 1, t).clamp(max=332)
+    t[t % 7 == 0] = 1
+    check(gs, w_in, w_out, c, t, fmt)
+    check(gs, w_in, w_out, c, t, fmt, bias=bias)
+    got = gs.gs_scores(w_in.to(DEV), w_out.to(DEV), c.to(DEV)).cpu().double()
+    h, w = w_in.double()[c.long()], w_out.double()
+    assert torch.all((got - h @ w.T).abs() <= (dim + 4) * V * (h.abs() @ w.abs().T) + 4 * V * (h @ w.T).abs())
