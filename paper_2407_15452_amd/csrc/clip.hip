@@ -2,11 +2,13 @@
 //
 //   norm = sqrt(sum over tensors and elements of x^2);  x <- x * (max_norm / norm) where norm > max_norm
 //
-// Both passes run over the same pieces of work (32 KB of one tensor each), dealt to a fixed number of workgroups, and are
-// bound by memory.  The squares are summed in fp64 (fp32 would overflow from 1.8e19 on and lose small tensors next to large
+// Both passes run over the same units of work (32 KB of one tensor each), dealt in ranges to a fixed number of workgroups, and
+// are bound by memory.  The squares are summed in fp64 (fp32 would overflow from 1.8e19 on and lose small tensors next to large
 // ones); every workgroup leaves one partial sum and the second pass adds them in order, so the same tensors give the same
 // bits on every run.  The second pass runs backwards: what the first one read last is still in the caches.
-// Addresses and sizes travel in the kernel arguments (nothing is copied to the device), kPerLaunch tensors a launch.
+// Addresses and sizes travel in the kernel arguments (nothing is copied to the device): of up to kPerLaunch tensors in those of
+// the two passes, of more in those of small kernels that write them to a table in the workspace first (301 tensors of 80 MB in
+// all: three launches for each pass took 82 us).
 
 #include <cmath>
 
@@ -25,27 +27,37 @@ struct Item {
   void* data;
   void* out;
   int64_t count;
-  uint32_t first_unit;                         // of this launch
+  uint32_t first_unit;
   int32_t dtype;
 };
-struct ClipArgs {
+struct Items {
   Item item[kPerLaunch];
   int32_t items;
+};
+struct Pass {
+  const Item* table;                           // or null: in the arguments
+  int32_t items;
   uint32_t units;
-  double* parts;                               // first pass: this launch's; second: all
+  double* parts;                               // one per workgroup of the first pass
   int32_t num_parts;
   double max_norm;
-  double* norm_out;                            // second pass: null but for one launch
+  double* norm_out;
 };
-static_assert(sizeof(ClipArgs) <= 4096, "kernel arguments");
+static_assert(sizeof(Items) + sizeof(Pass) <= 4096, "kernel arguments");
 
-__device__ __forceinline__ int find_item(const ClipArgs& a, uint32_t unit) {
-  int lo = 0, hi = a.items - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (a.item[mid].first_unit <= unit) lo = mid; else hi = mid - 1;
+// The item that holds `unit`, by a whole wave: 64 places at a time.
+template <bool TABLE>
+__device__ __forceinline__ int find_item(const Items& list, const Pass& a, uint32_t unit) {
+  int lo = 0, n = a.items;                     // the last of items lo .. lo + n - 1 that begins at or before `unit`; lo does
+  const int lane = threadIdx.x & 63;
+  while (n > 1) {
+    const int part = (n + 63) / 64, at = lane * part;
+    const bool before = at < n && (TABLE ? a.table[lo + at].first_unit : list.item[lo + at].first_unit) <= unit;
+    const int last = 63 - __clzll((long long)__ballot(before));
+    lo += last * part;
+    n = min(part, n - last * part);
   }
-  return lo;
+  return __builtin_amdgcn_readfirstlane(lo);
 }
 
 // elements in front of the first 16-byte boundary
@@ -173,65 +185,97 @@ __device__ double group_sum(double s) {
   return s;
 }
 
-__global__ __launch_bounds__(kThreads) void squares_kernel(ClipArgs a) {
+// this workgroup's units: body(item, unit of the item)
+template <bool TABLE, typename Body>
+__device__ __forceinline__ void for_units(const Items& list, const Pass& a, uint32_t group, Body body) {
+  const uint32_t per = a.units / gridDim.x, more = a.units % gridDim.x;
+  const uint32_t first = group * per + min(group, more), last = first + per + (group < more ? 1 : 0);
+  if (first >= last) return;
+  int at = find_item<TABLE>(list, a, first);
+  uint32_t end = 0;
+  Item it;
+  for (uint32_t u = first; u < last; ++u) {
+    if (u == first || u >= end) {
+      if (u != first) ++at;
+      it = TABLE ? a.table[at] : list.item[at];
+      end = at + 1 < a.items ? (TABLE ? a.table[at + 1].first_unit : list.item[at + 1].first_unit) : a.units;
+    }
+    body(it, u - it.first_unit);
+  }
+}
+
+template <bool TABLE>
+__global__ __launch_bounds__(kThreads) void squares_kernel(Items list, Pass a) {
   double s = 0.0;
-  for (uint32_t u = blockIdx.x; u < a.units; u += gridDim.x) {
-    const Item& it = a.item[find_item(a, u)];
-    const uint32_t unit = u - it.first_unit;
+  for_units<TABLE>(list, a, blockIdx.x, [&](const Item& it, uint32_t unit) {
     if (it.dtype == GS_F32) s += unit_squares<F32Value>(it, unit);
     else if (it.dtype == GS_BF16) s += unit_squares<HalfValue<bf16_t>>(it, unit);
     else s += unit_squares<HalfValue<f16_t>>(it, unit);
-  }
+  });
   s = group_sum(s);
   if (threadIdx.x == 0) a.parts[blockIdx.x] = s;
 }
 
-// many launches' parts into one
-__global__ __launch_bounds__(kThreads) void add_parts_kernel(const double* parts, int32_t num_parts, double* to) {
-  double s = 0.0;
-  for (int32_t k = threadIdx.x; k < num_parts; k += kThreads) s += parts[k];
-  s = group_sum(s);
-  if (threadIdx.x == 0) *to = s;
-}
-
-__global__ __launch_bounds__(kThreads) void clip_kernel(ClipArgs a) {
+template <bool TABLE>
+__global__ __launch_bounds__(kThreads) void clip_kernel(Items list, Pass a) {
   double s = 0.0;
   for (int32_t k = threadIdx.x; k < a.num_parts; k += kThreads) s += a.parts[k];
   const double norm = sqrt(group_sum(s));
-  if (a.norm_out != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *a.norm_out = norm;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.norm_out = norm;
   // a norm that is no number, or infinite, says that some gradient is: nothing is scaled by it
   const bool reached = norm > a.max_norm && norm < INFINITY;
   const float factor = reached ? (float)(a.max_norm / norm) : 1.0f;
-  for (uint32_t v = blockIdx.x; v < a.units; v += gridDim.x) {
-    const uint32_t u = a.units - 1 - v;
-    const Item& it = a.item[find_item(a, u)];
-    if (!reached && it.out == it.data) continue;
-    const uint32_t unit = u - it.first_unit;
+  for_units<TABLE>(list, a, gridDim.x - 1 - blockIdx.x, [&](const Item& it, uint32_t unit) {
+    if (!reached && it.out == it.data) return;
     if (it.dtype == GS_F32) unit_scaled<F32Value>(it, unit, factor, !reached);
     else if (it.dtype == GS_BF16) unit_scaled<HalfValue<bf16_t>>(it, unit, factor, !reached);
     else unit_scaled<HalfValue<f16_t>>(it, unit, factor, !reached);
-  }
+  });
+}
+
+__global__ __launch_bounds__(kThreads) void table_kernel(Items list, Item* to) {
+  for (int k = threadIdx.x; k < list.items; k += kThreads) to[k] = list.item[k];
 }
 
 int64_t elem_bytes(int32_t dtype) { return dtype == GS_F32 ? 4 : 2; }
-int64_t launches_for(int64_t num_tensors) { return std::max<int64_t>(1, ceil_div(num_tensors, kPerLaunch)); }
-
-// the next launch's tensors from `at` on; returns where the one after it begins
-int32_t fill_args(const gs_tensor* list, int32_t num_tensors, int32_t at, ClipArgs& a) {
-  uint64_t units = 0;
-  a.items = 0;
-  while (at < num_tensors && a.items < kPerLaunch) {
-    const gs_tensor& t = list[at];
-    if (t.count > 0) {
-      const uint64_t more = (uint64_t)std::max<int64_t>(1, ceil_div(ceil_div(t.count * elem_bytes(t.dtype), 16), kUnit));
-      Item& it = a.item[a.items++];
-      it = Item{t.data, t.out ? t.out : t.data, t.count, (uint32_t)units, t.dtype};
-      units += more;
-    }
-    ++at;
+// the next kPerLaunch tensors that are not empty, from `at` on; returns where the ones after them begin
+int32_t fill_items(const gs_tensor* list, int32_t num_tensors, int32_t at, Items& to, uint32_t& units) {
+  to.items = 0;
+  while (at < num_tensors && to.items < kPerLaunch) {
+    const gs_tensor& t = list[at++];
+    if (t.count == 0) continue;
+    to.item[to.items++] = Item{t.data, t.out ? t.out : t.data, t.count, units, t.dtype};
+    units += (uint32_t)std::max<int64_t>(1, ceil_div(ceil_div(t.count * elem_bytes(t.dtype), 16), kUnit));
   }
-  a.units = (uint32_t)units;
   return at;
+}
+
+struct ClipPlan {
+  double* parts;
+  Item* table;
+  size_t bytes;
+};
+ClipPlan plan_clip(void* ws, int64_t num_tensors) {
+  ClipPlan p{};
+  Carver c(ws);
+  p.parts = c.take<double>(kMaxGroups);
+  if (num_tensors > kPerLaunch) p.table = c.take<Item>((size_t)num_tensors);
+  p.bytes = c.used;
+  return p;
+}
+
+template <bool TABLE>
+int32_t run_passes(const Items& list, const Pass& a, bool norm_alone, hipStream_t stream) {
+  const unsigned groups = (unsigned)a.num_parts;
+  if (groups > 0) {
+    squares_kernel<TABLE><<<groups, kThreads, 0, stream>>>(list, a);
+    GS_LAUNCH_CHECK();
+  }
+  Pass second = a;
+  if (norm_alone) second.units = 0;
+  clip_kernel<TABLE><<<norm_alone ? 1 : groups, kThreads, 0, stream>>>(list, second);
+  GS_LAUNCH_CHECK();
+  return GS_OK;
 }
 
 }  // namespace
@@ -240,8 +284,7 @@ int32_t fill_args(const gs_tensor* list, int32_t num_tensors, int32_t at, ClipAr
 using namespace gs;
 
 extern "C" size_t gs_clip_grads_workspace_bytes(int32_t num_tensors) {
-  if (num_tensors < 0) return 0;
-  return align_up(sizeof(double) * (size_t)(1 + launches_for(num_tensors) * kMaxGroups));
+  return num_tensors < 0 ? 0 : plan_clip(nullptr, num_tensors).bytes;
 }
 
 extern "C" int32_t gs_clip_grads(const gs_tensor* list, int32_t num_tensors, double max_norm, double* norm_out, void* ws,
@@ -261,45 +304,20 @@ extern "C" int32_t gs_clip_grads(const gs_tensor* list, int32_t num_tensors, dou
     total += t.count;
     if (total > ((int64_t)1 << 40)) return GS_EINVAL;
   }
-  if (ws_bytes < gs_clip_grads_workspace_bytes(num_tensors)) return GS_EWORKSPACE;
-  double* sum = static_cast<double*>(ws);
-  double* parts = sum + 1;
-  ClipArgs a{};
-  a.max_norm = max_norm;
-  int32_t num_parts = 0, launches = 0;
-  for (int32_t at = 0; at < num_tensors;) {
-    at = fill_args(list, num_tensors, at, a);
-    if (a.items == 0) break;
-    const unsigned groups = std::min<unsigned>(a.units, kMaxGroups);
-    a.parts = parts + num_parts;
-    squares_kernel<<<groups, kThreads, 0, stream>>>(a);
+  const ClipPlan p = plan_clip(ws, num_tensors);
+  if (ws_bytes < p.bytes) return GS_EWORKSPACE;
+  Items items;
+  uint32_t units = 0;
+  int32_t count = 0;
+  int32_t at = fill_items(list, num_tensors, 0, items, units);
+  const bool table = at < num_tensors;
+  while (table && items.items > 0) {
+    table_kernel<<<1, kThreads, 0, stream>>>(items, p.table + count);
     GS_LAUNCH_CHECK();
-    num_parts += (int32_t)groups;
-    ++launches;
+    count += items.items;
+    at = fill_items(list, num_tensors, at, items, units);
   }
-  a.parts = parts;
-  a.num_parts = num_parts;
-  a.norm_out = norm_out;
-  if (launches > 1) {                          // every workgroup of the second pass adds all parts: few of them
-    add_parts_kernel<<<1, kThreads, 0, stream>>>(parts, num_parts, sum);
-    GS_LAUNCH_CHECK();
-    a.parts = sum;
-    a.num_parts = 1;
-  }
-  const bool norm_alone = launches == 0 || (!elsewhere && std::isinf(max_norm));
-  if (norm_alone) {
-    a.items = 0;
-    a.units = 0;
-    clip_kernel<<<1, kThreads, 0, stream>>>(a);
-    GS_LAUNCH_CHECK();
-    return GS_OK;
-  }
-  for (int32_t at = 0; at < num_tensors;) {
-    at = fill_args(list, num_tensors, at, a);
-    if (a.items == 0) break;
-    clip_kernel<<<std::min<unsigned>(a.units, kMaxGroups), kThreads, 0, stream>>>(a);
-    GS_LAUNCH_CHECK();
-    a.norm_out = nullptr;
-  }
-  return GS_OK;
+  const bool norm_alone = units == 0 || (!elsewhere && std::isinf(max_norm));
+  const Pass a{p.table, table ? count : items.items, units, p.parts, (int32_t)std::min<uint32_t>(units, kMaxGroups), max_norm, norm_out};
+  return table ? run_passes<true>(items, a, norm_alone, stream) : run_passes<false>(items, a, norm_alone, stream);
 }
