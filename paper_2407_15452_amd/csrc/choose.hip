@@ -84,8 +84,7 @@ struct RowLimits {
 struct Weigh {
   float top;
   double inverse;                              // of the temperature
-  __device__ __forceinline__ double operator()(uint32_t key) const {
-    const float s = score_of(key);
+  __device__ __forceinline__ double operator()(float s) const {
     if (s == top) return 1.0;
     const double d = (double)s - (double)top;
     return d == -INFINITY ? 0.0 : exp(d * inverse);
@@ -125,14 +124,14 @@ __device__ __forceinline__ void add_to(Histogram& h, int b, bool weights, double
 // distance of two floats is one.
 struct Steps {
   float least, inverse;
-  static __device__ __forceinline__ float half_of(uint32_t key) { return fminf(score_of(key), 3.4028234663852886e38f) * 0.5f; }
+  static __device__ __forceinline__ float half_of(float s) { return fminf(s, 3.4028234663852886e38f) * 0.5f; }
   __device__ __forceinline__ Steps(uint32_t kmin, uint32_t kmax) {
-    least = half_of(kmin);
-    const float range = half_of(kmax) - least;
+    least = half_of(score_of(kmin));
+    const float range = half_of(score_of(kmax)) - least;
     inverse = range > 0.0f ? fminf((float)(kBins - 1) / range, 3.4028234663852886e38f) : 0.0f;
   }
-  __device__ __forceinline__ int operator()(uint32_t key) const {
-    return (int)fminf((half_of(key) - least) * inverse, (float)(kBins - 1));
+  __device__ __forceinline__ int operator()(float s) const {
+    return (int)fminf((half_of(s) - least) * inverse, (float)(kBins - 1));
   }
 };
 // The first of the keys [lo, hi] for which `yes` holds, once it holds for hi and for every key after such a one: 64 keys at a time.
@@ -152,8 +151,8 @@ __device__ __forceinline__ uint32_t first_key(uint32_t lo, uint32_t hi, Yes yes)
 }
 // the keys of steps from .. to, among [kmin, kmax]; both steps hold a key
 __device__ __forceinline__ void keys_of_steps(const Steps& steps, int from, int to, uint32_t kmin, uint32_t kmax, uint32_t& lo, uint32_t& hi) {
-  lo = first_key(kmin, kmax, [=](uint32_t key) { return steps(key) >= from; });
-  hi = steps(kmax) <= to ? kmax : first_key(lo, kmax, [=](uint32_t key) { return steps(key) > to; }) - 1;
+  lo = first_key(kmin, kmax, [=](uint32_t key) { return steps(score_of(key)) >= from; });
+  hi = steps(score_of(kmax)) <= to ? kmax : first_key(lo, kmax, [=](uint32_t key) { return steps(score_of(key)) > to; }) - 1;
 }
 
 struct ListShared {
@@ -182,38 +181,39 @@ struct Row {
     n = (uint32_t)n_;
   }
   __device__ __forceinline__ uint32_t pieces() const { return (n + skew + kPer - 1) / kPer; }
-  __device__ __forceinline__ void load(uint32_t piece, uint32_t* key) const {        // 0 beyond the row
+  __device__ __forceinline__ void load(uint32_t piece, float* s) const {             // -infinity beyond the row
     const uint32_t at = piece * kPer;
     elem e[kPer];
     if (at >= skew && at + kPer <= n + skew) {
       const uint4 w = *reinterpret_cast<const uint4*>(base + at);
       __builtin_memcpy(e, &w, 16);
 #pragma unroll
-      for (uint32_t k = 0; k < kPer; ++k) key[k] = key_of(V::get(e[k]));
+      for (uint32_t k = 0; k < kPer; ++k) s[k] = V::get(e[k]);
     } else {
 #pragma unroll
-      for (uint32_t k = 0; k < kPer; ++k) key[k] = at + k >= skew && at + k < n + skew ? key_of(V::get(base[at + k])) : 0;
+      for (uint32_t k = 0; k < kPer; ++k) s[k] = at + k >= skew && at + k < n + skew ? V::get(base[at + k]) : -INFINITY;
     }
   }
 };
-// visit(index, key) for the valid elements of the pieces from .. to, by `threads` lanes of which this is number `lane`
+// visit(index, score) for the elements of the pieces from .. to that are not left out, by `threads` lanes of which this is
+// number `lane`
 template <int AHEAD, typename V, typename Visit>
 __device__ __forceinline__ void for_row(const Row<V>& row, uint32_t from, uint32_t to, uint32_t lane, uint32_t threads, Visit visit) {
   constexpr uint32_t per = Row<V>::kPer;
   for (uint32_t p0 = from + lane; p0 < to; p0 += AHEAD * threads) {
-    uint32_t key[AHEAD][per];
+    float s[AHEAD][per];
 #pragma unroll
     for (int e = 0; e < AHEAD; ++e) {
-      if (p0 + e * threads < to) row.load(p0 + e * threads, key[e]);
+      if (p0 + e * threads < to) row.load(p0 + e * threads, s[e]);
       else
 #pragma unroll
-        for (uint32_t k = 0; k < per; ++k) key[e][k] = 0;
+        for (uint32_t k = 0; k < per; ++k) s[e][k] = -INFINITY;
     }
 #pragma unroll
     for (int e = 0; e < AHEAD; ++e)
 #pragma unroll
       for (uint32_t k = 0; k < per; ++k)
-        if (key[e][k] != 0) visit((p0 + e * threads) * per + k - row.skew, key[e][k]);
+        if (s[e][k] > -INFINITY) visit((p0 + e * threads) * per + k - row.skew, s[e][k]);
   }
 }
 
@@ -287,8 +287,9 @@ __device__ void clear_histogram(Shared& sh, bool weights) {
 template <typename V, typename Bin>
 __device__ void fill_by_key(Shared& sh, const Row<V>& row, uint32_t lo, uint32_t hi, bool weights, const Weigh& weigh, Bin bin) {
   clear_histogram(sh, weights);
-  for_row<1>(row, 0, row.pieces(), threadIdx.x, kThreads, [&](uint32_t, uint32_t key) {
-    if (key >= lo && key <= hi) add_to(sh.hist, bin(key), weights, weights ? weigh(key) : 0.0);
+  for_row<1>(row, 0, row.pieces(), threadIdx.x, kThreads, [&](uint32_t, float s) {
+    const uint32_t key = key_of(s);
+    if (key >= lo && key <= hi) add_to(sh.hist, bin(key, s), weights, weights ? weigh(s) : 0.0);
   });
   __syncthreads();
 }
@@ -307,7 +308,7 @@ __device__ bool narrow(Shared& sh, const Row<V>& row, const Steps& steps, uint32
     const int bits = 32 - __clz(hi - lo);
     const int shift = bits > 11 ? bits - 11 : 0;
     const uint32_t from = lo;
-    fill_by_key(sh, row, lo, hi, weights, weigh, [=](uint32_t key) { return (int)((key - from) >> shift); });
+    fill_by_key(sh, row, lo, hi, weights, weigh, [=](uint32_t key, float) { return (int)((key - from) >> shift); });
     find_bin(sh, above, weights, reached);
     const int b = sh.found_bin;                // the bins' sums add up to the interval's: one of them reaches what it did
     above = sh.found_above;
@@ -339,7 +340,7 @@ __device__ void cut_the_long_way(Shared& sh, const Row<V>& row, uint32_t kmin, u
   bool all_ties = true;
   double whole = 0.0;
   for (int by_p = limits.by_k ? 0 : 1; by_p <= (limits.by_p ? 1 : 0); ++by_p) {
-    fill_by_key(sh, row, kmin, kmax, limits.by_p, weigh, steps);
+    fill_by_key(sh, row, kmin, kmax, limits.by_p, weigh, [=](uint32_t, float s) { return steps(s); });
     if (by_p && (!limits.by_k || cut.key == 0)) {                  // top-k, if any, keeps everything
       whole = find_bin(sh, Sum{0, 0, 0}, true, [](const Sum&) { return false; }).value();
       __syncthreads();
@@ -354,10 +355,10 @@ __device__ void cut_the_long_way(Shared& sh, const Row<V>& row, uint32_t kmin, u
     if (!narrow(sh, row, steps, kmin, kmax, limits.by_p, weigh, reached, key, above, in) || key < cut.key) continue;
     if (by_p) {
       const uint64_t most = key == cut.key && !all_ties ? ties : in.count;
-      ties = first_alone ? 1 : ties_below(above.value(), weigh(key), target, most);
+      ties = first_alone ? 1 : ties_below(above.value(), weigh(score_of(key)), target, most);
     } else {
       ties = k - above.count;
-      whole = above.value() + (double)ties * weigh(key);
+      whole = above.value() + (double)ties * weigh(score_of(key));
     }
     cut.key = key;
     all_ties = ties == in.count;
@@ -371,8 +372,8 @@ __device__ void cut_the_long_way(Shared& sh, const Row<V>& row, uint32_t kmin, u
     const int bits = 32 - __clz(hi - lo);
     const int shift = bits > 11 ? bits - 11 : 0;
     clear_histogram(sh, false);
-    for_row<1>(row, 0, row.pieces(), threadIdx.x, kThreads, [&](uint32_t at, uint32_t key) {
-      if (key == cut.key && at >= lo && at <= hi) atomicAdd(&sh.hist.count[kBins - 1 - ((at - lo) >> shift)], 1u);
+    for_row<1>(row, 0, row.pieces(), threadIdx.x, kThreads, [&](uint32_t at, float s) {
+      if (key_of(s) == cut.key && at >= lo && at <= hi) atomicAdd(&sh.hist.count[kBins - 1 - ((at - lo) >> shift)], 1u);
     });
     __syncthreads();
     find_bin(sh, above, false, reached);
@@ -387,7 +388,7 @@ __device__ void cut_the_long_way(Shared& sh, const Row<V>& row, uint32_t kmin, u
 
 __device__ __forceinline__ double kept_weight(uint32_t key, uint32_t at, const Cut& cut, double min_p, const Weigh& weigh) {
   if (key < cut.key || (key == cut.key && at > cut.last_tie)) return 0.0;
-  const double e = weigh(key);
+  const double e = weigh(score_of(key));
   return min_p > 0.0 && !(e >= min_p) ? 0.0 : e;
 }
 
@@ -420,9 +421,9 @@ __device__ void choose_index(Shared& sh, const Row<V>& row, uint32_t lo, uint32_
     const int shift = bits > 11 ? bits - 11 : 0;
     clear_histogram(sh, true);
     const uint32_t from = (lo + row.skew) / Row<V>::kPer, to = (hi + row.skew) / Row<V>::kPer + 1;
-    for_row<1>(row, from, to, threadIdx.x, kThreads, [&](uint32_t at, uint32_t key) {
+    for_row<1>(row, from, to, threadIdx.x, kThreads, [&](uint32_t at, float s) {
       if (at < lo || at > hi) return;
-      const double e = kept_weight(key, at, cut, limits.min_p, weigh);
+      const double e = kept_weight(key_of(s), at, cut, limits.min_p, weigh);
       if (e > 0.0) add_to(sh.hist, kBins - 1 - (int)((at - lo) >> shift), true, e);
     });
     __syncthreads();
@@ -450,20 +451,45 @@ __device__ __forceinline__ void put_entry(ListShared& sh, uint32_t key, uint32_t
   if (p < (uint32_t)kListMost) sh.list[p] = entry_of(key, at);     // always: the histogram has counted them
 }
 
-// Bitonic sort of sh.list[0 .. size), ascending; size a power of two.  Steps over fewer than 128 entries stay in a wave.
+// Bitonic sort of sh.list[0 .. size), ascending; size a power of two and at least 4.  A pass takes two strides: four entries per
+// lane, once through LDS.  Passes over blocks of at most 256 entries stay in a wave.
+__device__ __forceinline__ void order(uint64_t& x, uint64_t& y, bool up) {
+  const bool turn = (x > y) == up;
+  const uint64_t a = turn ? y : x, b = turn ? x : y;
+  x = a;
+  y = b;
+}
 __device__ void sort_list(ListShared& sh, uint32_t size) {
   __syncthreads();
   for (uint32_t block = 2; block <= size; block <<= 1) {
-    for (uint32_t stride = block >> 1; stride; stride >>= 1) {
+    uint32_t stride = block >> 1;
+    if (__popc(block - 1) & 1) {               // an odd number of strides: the first alone
       for (uint32_t t = threadIdx.x; t < size / 2; t += kThreads) {
-        const uint32_t i = ((t & ~(stride - 1)) << 1) | (t & (stride - 1)), j = i + stride;
-        const uint64_t x = sh.list[i], y = sh.list[j];
-        if ((x > y) == ((i & block) == 0)) {
-          sh.list[i] = y;
-          sh.list[j] = x;
-        }
+        const uint32_t i = ((t & ~(stride - 1)) << 1) | (t & (stride - 1));
+        uint64_t x = sh.list[i], y = sh.list[i + stride];
+        order(x, y, (i & block) == 0);
+        sh.list[i] = x;
+        sh.list[i + stride] = y;
       }
-      if (stride >= 128 || (stride == 1 && block >= 128)) __syncthreads();
+      __syncthreads();                         // the next pass deals the entries to other lanes
+      stride >>= 1;
+    }
+    for (; stride >= 2; stride >>= 2) {
+      const uint32_t h = stride >> 1;
+      for (uint32_t t = threadIdx.x; t < size / 4; t += kThreads) {
+        const uint32_t i = ((t & ~(h - 1)) << 2) | (t & (h - 1));
+        const bool up = (i & block) == 0;
+        uint64_t x0 = sh.list[i], x1 = sh.list[i + h], x2 = sh.list[i + stride], x3 = sh.list[i + stride + h];
+        order(x0, x2, up);
+        order(x1, x3, up);
+        order(x0, x1, up);
+        order(x2, x3, up);
+        sh.list[i] = x0;
+        sh.list[i + h] = x1;
+        sh.list[i + stride] = x2;
+        sh.list[i + stride + h] = x3;
+      }
+      if (stride > 128 || stride <= 3) __syncthreads();
       else wave_fence();
     }
   }
@@ -471,7 +497,7 @@ __device__ void sort_list(ListShared& sh, uint32_t size) {
 }
 // pads to a power of two (entries that sort last) and sorts
 __device__ void sort_entries(ListShared& sh, uint32_t length) {
-  uint32_t size = 2;
+  uint32_t size = 4;
   while (size < length) size <<= 1;
   __syncthreads();
   for (uint32_t j = length + threadIdx.x; j < size; j += kThreads) sh.list[j] = ~0ull;
@@ -524,7 +550,7 @@ __device__ void cut_from_list(Shared& sh, const Plan& plan, const RowLimits& lim
     last = 0;
   } else if (limits.by_p) {
     clear_histogram(sh, true);
-    for (uint32_t p = threadIdx.x; p <= last; p += kThreads) add_to(sh.hist, kBins - 1 - p, true, weigh(entry_key(sh.list[p])));
+    for (uint32_t p = threadIdx.x; p <= last; p += kThreads) add_to(sh.hist, kBins - 1 - p, true, weigh(score_of(entry_key(sh.list[p]))));
     __syncthreads();
     const double whole = limits.by_k ? sum_of_bins(sh).value() : plan.whole;
     const double target = (double)limits.top_p * whole;
@@ -547,7 +573,7 @@ __device__ void choose_from_list(Shared& sh, const Plan& plan, const Cut& cut, c
     mine[e] = p < plan.length ? (x << 32) | (x >> 32) : ~0ull;     // index first
   }
   __syncthreads();
-  uint32_t size = 2;
+  uint32_t size = 4;
   while (size < plan.length) size <<= 1;
 #pragma unroll
   for (int e = 0; e < (kListMost + kThreads - 1) / kThreads; ++e) {
@@ -596,7 +622,10 @@ template <typename V>
 __device__ Extreme extreme_of(const Row<V>& row, uint32_t from, uint32_t to) {           // the same in every lane
   __shared__ Extreme wave_x[kWaves];
   Extreme x{0xffffffffu, 0, 0xffffffffu, 0};
-  for_row<kAhead>(row, from, to, threadIdx.x, kThreads, [&](uint32_t at, uint32_t key) { x.with(key, key, at); });
+  for_row<kAhead>(row, from, to, threadIdx.x, kThreads, [&](uint32_t at, float s) {
+    const uint32_t key = key_of(s);
+    x.with(key, key, at);
+  });
   x.over_wave();
   if ((threadIdx.x & 63) == 0) wave_x[threadIdx.x >> 6] = x;
   __syncthreads();
@@ -608,9 +637,9 @@ __device__ Extreme extreme_of(const Row<V>& row, uint32_t from, uint32_t to) {  
 template <typename V>
 __device__ void first_histogram(Histogram& hist, const Row<V>& row, uint32_t from, uint32_t to, const Steps& steps, bool weights, const Weigh& weigh) {
   if (weights)
-    for_row<1>(row, from, to, threadIdx.x, kThreads, [&](uint32_t, uint32_t key) { add_to(hist, steps(key), true, weigh(key)); });
+    for_row<1>(row, from, to, threadIdx.x, kThreads, [&](uint32_t, float s) { add_to(hist, steps(s), true, weigh(s)); });
   else
-    for_row<kAhead>(row, from, to, threadIdx.x, kThreads, [&](uint32_t, uint32_t key) { atomicAdd(&hist.count[steps(key)], 1u); });
+    for_row<kAhead>(row, from, to, threadIdx.x, kThreads, [&](uint32_t, float s) { atomicAdd(&hist.count[steps(s)], 1u); });
 }
 
 // ---- row by row --------------------------------------------------------------------------------------------------------
@@ -633,8 +662,9 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
     if (plan.long_way) {
       cut_the_long_way(sh, row, x.kmin, x.kmax, weigh, limits, cut);
     } else if (plan.listed) {
-      for_row<kAhead>(row, 0, row.pieces(), threadIdx.x, kThreads, [&](uint32_t at, uint32_t key) {
-        if (key >= plan.lo && key <= plan.hi) put_entry(sh, key, at);
+      const float lo = score_of(plan.lo), hi = score_of(plan.hi);
+      for_row<kAhead>(row, 0, row.pieces(), threadIdx.x, kThreads, [&](uint32_t at, float s) {
+        if (s >= lo && s <= hi) put_entry(sh, key_of(s), at);
       });
       cut_from_list(sh, plan, limits, weigh, cut);
       if (limits.by_k) {
@@ -757,10 +787,10 @@ __global__ __launch_bounds__(kThreads) void collect_kernel(SplitArgs a) {
   if (plan.long_way) return;
   if (threadIdx.x == 0) sh.list_count = 0;
   __syncthreads();
-  const uint32_t key_lo = plan.lo, key_hi = plan.hi;
+  const float list_lo = score_of(plan.lo), list_hi = score_of(plan.hi);
   const Row<V> row(a.s.scores, r, a.s.n);
-  auto to_list = [&](uint32_t at, uint32_t key) {
-    if (key >= key_lo && key <= key_hi) put_entry(sh, key, at);
+  auto to_list = [&](uint32_t at, float s) {
+    if (s >= list_lo && s <= list_hi) put_entry(sh, key_of(s), at);
   };
   if (!plan.pieces) {
     uint32_t from, to;
@@ -768,16 +798,17 @@ __global__ __launch_bounds__(kThreads) void collect_kernel(SplitArgs a) {
     for_row<kAhead>(row, from, to, threadIdx.x, kThreads, to_list);
   } else {
     const Weigh weigh{score_of(x.kmax), 1.0 / (double)limits.temperature};
-    const uint32_t floor = plan.listed ? key_hi : 0, last = min(a.parts, (g + 1) * a.parts_per_group);
+    const float floor = plan.listed ? list_hi : -INFINITY;
+    const uint32_t last = min(a.parts, (g + 1) * a.parts_per_group);
     const uint32_t span = a.width / Row<V>::kPer;
     for (uint32_t part = g * a.parts_per_group + (threadIdx.x >> 6); part < last; part += kWaves) {
       uint64_t hi = 0, lo = 0;
-      for_row<1>(row, min(part * span, row.pieces()), min((part + 1) * span, row.pieces()), threadIdx.x & 63, 64, [&](uint32_t at, uint32_t key) {
-        if (key <= floor) {
-          to_list(at, key);
+      for_row<1>(row, min(part * span, row.pieces()), min((part + 1) * span, row.pieces()), threadIdx.x & 63, 64, [&](uint32_t at, float s) {
+        if (s <= floor) {
+          to_list(at, s);
           return;
         }
-        const double w = weigh(key);
+        const double w = weigh(s);
         if (limits.min_p > 0.0 && !(w >= limits.min_p)) return;
         const uint64_t units = units_of(w);
         hi += units >> 31;
