@@ -28,7 +28,8 @@ constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / 64;
 constexpr int kBins = 2048;
 constexpr int kAhead = 4;                      // 16-byte loads per lane in flight
-constexpr int kListMost = kBins;               // elements of a row that may go to its list
+constexpr int kListMost = 2 * kBins;           // elements of a row that may go to its list: room for two values of a 16-bit
+                                               // format, which a step may hold, in rows of a million nodes
 constexpr int kSplitGroups = 2048;             // of one launch: eight per compute unit
 constexpr int kSplitLeast = 8192;              // scores per workgroup at least
 
@@ -542,21 +543,47 @@ __device__ Plan make_plan(Shared& sh, uint32_t kmin, uint32_t kmax, const RowLim
   return plan;
 }
 
-// Sorted entries to the cut.  Entry number p lies in bin kBins - 1 - p.
+// The weights of the list's entries from .. to, entry `from` in the highest bin.
+template <typename Weight>
+__device__ void fill_by_place(Shared& sh, uint32_t from, uint32_t to, Weight weight) {
+  clear_histogram(sh, true);
+  for (uint32_t p = from + threadIdx.x; p < to; p += kThreads) {
+    const double e = weight(sh.list[p]);
+    if (e > 0.0) add_to(sh.hist, kBins - 1 - (p - from), true, e);
+  }
+  __syncthreads();
+}
+// The place of the first entry at which `reached` holds; `to` if there is none.  What lies in front is in `above` then.
+template <typename Weight, typename Reached>
+__device__ uint32_t find_place(Shared& sh, uint32_t to, Sum& above, Weight weight, Reached reached) {
+  for (uint32_t from = 0; from < to; from += kBins) {
+    fill_by_place(sh, from, min(from + kBins, to), weight);
+    const Sum part = find_bin(sh, above, true, reached);
+    if (sh.found_bin >= 0) return from + kBins - 1 - sh.found_bin;
+    above = above + part;
+    __syncthreads();
+  }
+  return to;
+}
+template <typename Weight>
+__device__ Sum sum_of_list(Shared& sh, uint32_t to, Weight weight) {
+  Sum total{0, 0, 0};
+  find_place(sh, to, total, weight, [](const Sum&) { return false; });
+  return total;
+}
+
+// The list, sorted, to the cut.
 __device__ void cut_from_list(Shared& sh, const Plan& plan, const RowLimits& limits, const Weigh& weigh, Cut& cut) {
   sort_entries(sh, plan.length);
   uint32_t last = limits.by_k ? min((uint32_t)limits.k, plan.length) - 1 : plan.length - 1;
   if (limits.by_p && !(limits.top_p > 0.0f)) {
     last = 0;
   } else if (limits.by_p) {
-    clear_histogram(sh, true);
-    for (uint32_t p = threadIdx.x; p <= last; p += kThreads) add_to(sh.hist, kBins - 1 - p, true, weigh(score_of(entry_key(sh.list[p]))));
-    __syncthreads();
-    const double whole = limits.by_k ? sum_of_bins(sh).value() : plan.whole;
+    auto weight = [&](uint64_t entry) { return weigh(score_of(entry_key(entry))); };
+    const double whole = limits.by_k ? sum_of_list(sh, last + 1, weight).value() : plan.whole;
     const double target = (double)limits.top_p * whole;
-    find_bin(sh, limits.by_k ? Sum{0, 0, 0} : plan.above, true, [=](const Sum& s) { return s.value() >= target; });
-    if (sh.found_bin >= 0) last = kBins - 1 - sh.found_bin;
-    __syncthreads();
+    Sum above = limits.by_k ? Sum{0, 0, 0} : plan.above;
+    last = min(last, find_place(sh, last + 1, above, weight, [=](const Sum& s) { return s.value() >= target; }));
   }
   cut.key = entry_key(sh.list[last]);
   cut.last_tie = (uint32_t)sh.list[last];
@@ -565,31 +592,16 @@ __device__ void cut_from_list(Shared& sh, const Plan& plan, const RowLimits& lim
 // With top-k the list holds every node that may be chosen: by index now, with the weights.
 __device__ void choose_from_list(Shared& sh, const Plan& plan, const Cut& cut, const RowLimits& limits, const Weigh& weigh, const SampleArgs& a, int64_t r) {
   __syncthreads();
-  uint64_t mine[(kListMost + kThreads - 1) / kThreads];
-#pragma unroll
-  for (int e = 0; e < (kListMost + kThreads - 1) / kThreads; ++e) {
-    const uint32_t p = e * kThreads + threadIdx.x;
-    const uint64_t x = p < plan.length ? sh.list[p] : ~0ull;
-    mine[e] = p < plan.length ? (x << 32) | (x >> 32) : ~0ull;     // index first
-  }
-  __syncthreads();
-  uint32_t size = 4;
-  while (size < plan.length) size <<= 1;
-#pragma unroll
-  for (int e = 0; e < (kListMost + kThreads - 1) / kThreads; ++e) {
-    const uint32_t p = e * kThreads + threadIdx.x;
-    if (p < size) sh.list[p] = mine[e];
-  }
-  sort_list(sh, size);
-  clear_histogram(sh, true);
   for (uint32_t p = threadIdx.x; p < plan.length; p += kThreads) {
     const uint64_t x = sh.list[p];
-    const double e = kept_weight(~(uint32_t)x, (uint32_t)(x >> 32), cut, limits.min_p, weigh);
-    if (e > 0.0) add_to(sh.hist, kBins - 1 - p, true, e);
+    sh.list[p] = (x << 32) | (x >> 32);        // index first
   }
-  __syncthreads();
-  const Sum total = sum_of_bins(sh);
-  const uint32_t p = find_answer(sh, Sum{0, 0, 0}, total, limits.u);
+  sort_entries(sh, plan.length);
+  auto weight = [&](uint64_t x) { return kept_weight(~(uint32_t)x, (uint32_t)(x >> 32), cut, limits.min_p, weigh); };
+  const Sum total = sum_of_list(sh, plan.length, weight);
+  const double target = limits.u * total.value();
+  Sum above{0, 0, 0};
+  const uint32_t p = find_place(sh, plan.length, above, weight, [=](const Sum& s) { return s.value() > target || s.same_weight(total); });
   answer(a, r, (uint32_t)(sh.list[p] >> 32), sh.found_in, total);
 }
 

@@ -222,3 +222,15 @@ def test_long_rows_of_equal_scores(gs, top_k, top_p):
     z[3, 0] = 1e30
     u = torch.tensor([0.3, 0.6, 0.9, 0.99])
     check(gs, z, u, top_k=None if top_k is None else [top_k] * rows, top_p=None if top_p is None else [top_p] * rows)
+
+
+@pytest.mark.parametrize("n", [9000, 120_000])
+@pytest.mark.parametrize("fmt", ["f32", "bf16"])
+def test_lists_of_more_than_one_histogram(gs, n, fmt):
+    """Thousands of nodes kept by top-k, or equal to the score that top-p cuts at."""
+    z, u = rows_of(6, n, fmt, seed=11)
+    check(gs, z, u, top_k=[2047, 2048, 2049, 4095, 4096, 4097])
+    check(gs, z, u, top_k=[2047, 2048, 2049, 3900, 4096, 4097], top_p=[0.999, 0.99, 0.9, 0.9999, 0.5, 0.7], min_p=[0.0, 1e-4] * 3)
+    z = torch.round(z * 4) / 4                       # some hundred values
+    check(gs, z, u, top_p=[0.5, 0.7, 0.9, 0.95, 0.99, 0.999])
+    check(gs, z, u, top_k=[1500, 2500, 3500, 4000, 5000, 8000], top_p=[0.5, 0.7, 0.9, 0.95, 0.99, 0.999])
