@@ -85,10 +85,10 @@ struct RowLimits {
 struct Weigh {
   float top;
   double inverse;                              // of the temperature
-  __device__ __forceinline__ double operator()(float s) const {
-    if (s == top) return 1.0;
-    const double d = (double)s - (double)top;
-    return d == -INFINITY ? 0.0 : exp(d * inverse);
+  __device__ __forceinline__ double operator()(float s) const {     // without branches: they would split every wave
+    const double d = (double)s - (double)top;                      // infinities: NaN for the greatest, -infinity for the others
+    const double e = exp(d * inverse);
+    return s == top ? 1.0 : d == -INFINITY ? 0.0 : e;
   }
 };
 
@@ -544,32 +544,35 @@ __device__ Plan make_plan(Shared& sh, uint32_t kmin, uint32_t kmax, const RowLim
 }
 
 // The weights of the list's entries from .. to, entry `from` in the highest bin.
-template <typename Weight>
-__device__ void fill_by_place(Shared& sh, uint32_t from, uint32_t to, Weight weight) {
+__device__ void fill_by_place(Shared& sh, uint32_t from, uint32_t to, const Weigh& weigh) {
   clear_histogram(sh, true);
-  for (uint32_t p = from + threadIdx.x; p < to; p += kThreads) {
-    const double e = weight(sh.list[p]);
-    if (e > 0.0) add_to(sh.hist, kBins - 1 - (p - from), true, e);
-  }
+  for (uint32_t p = from + threadIdx.x; p < to; p += kThreads) add_to(sh.hist, kBins - 1 - (p - from), true, weigh(score_of(entry_key(sh.list[p]))));
   __syncthreads();
 }
-// The place of the first entry at which `reached` holds; `to` if there is none.  What lies in front is in `above` then.
-template <typename Weight, typename Reached>
-__device__ uint32_t find_place(Shared& sh, uint32_t to, Sum& above, Weight weight, Reached reached) {
-  for (uint32_t from = 0; from < to; from += kBins) {
-    fill_by_place(sh, from, min(from + kBins, to), weight);
-    const Sum part = find_bin(sh, above, true, reached);
+// The first of the sorted entries 0 .. to - 1 at which the weights, with those of `above`, reach top_p of `whole` (negative: of
+// these entries' sum); to - 1 if rounding leaves none.
+__device__ uint32_t place_of_top_p(Shared& sh, uint32_t to, Sum above, double whole, float top_p, const Weigh& weigh) {
+  uint32_t from = 0;
+  fill_by_place(sh, 0, min((uint32_t)kBins, to), weigh);
+  if (whole < 0.0) {
+    Sum total = sum_of_bins(sh);
+    for (from = kBins; from < to; from += kBins) {
+      fill_by_place(sh, from, min(from + kBins, to), weigh);
+      total = total + sum_of_bins(sh);
+    }
+    if (to > (uint32_t)kBins) fill_by_place(sh, 0, kBins, weigh);
+    whole = total.value();
+  }
+  const double target = (double)top_p * whole;
+  for (from = 0;;) {
+    const Sum part = find_bin(sh, above, true, [=](const Sum& s) { return s.value() >= target; });
     if (sh.found_bin >= 0) return from + kBins - 1 - sh.found_bin;
+    from += kBins;
+    if (from >= to) return to - 1;
     above = above + part;
     __syncthreads();
+    fill_by_place(sh, from, min(from + kBins, to), weigh);
   }
-  return to;
-}
-template <typename Weight>
-__device__ Sum sum_of_list(Shared& sh, uint32_t to, Weight weight) {
-  Sum total{0, 0, 0};
-  find_place(sh, to, total, weight, [](const Sum&) { return false; });
-  return total;
 }
 
 // The list, sorted, to the cut.
@@ -579,30 +582,40 @@ __device__ void cut_from_list(Shared& sh, const Plan& plan, const RowLimits& lim
   if (limits.by_p && !(limits.top_p > 0.0f)) {
     last = 0;
   } else if (limits.by_p) {
-    auto weight = [&](uint64_t entry) { return weigh(score_of(entry_key(entry))); };
-    const double whole = limits.by_k ? sum_of_list(sh, last + 1, weight).value() : plan.whole;
-    const double target = (double)limits.top_p * whole;
-    Sum above = limits.by_k ? Sum{0, 0, 0} : plan.above;
-    last = min(last, find_place(sh, last + 1, above, weight, [=](const Sum& s) { return s.value() >= target; }));
+    last = place_of_top_p(sh, last + 1, limits.by_k ? Sum{0, 0, 0} : plan.above, limits.by_k ? -1.0 : plan.whole, limits.top_p, weigh);
   }
   cut.key = entry_key(sh.list[last]);
   cut.last_tie = (uint32_t)sh.list[last];
 }
 
-// With top-k the list holds every node that may be chosen: by index now, with the weights.
+// With top-k the list holds every node that may be chosen: histograms of its weights along the index, down to one.
 __device__ void choose_from_list(Shared& sh, const Plan& plan, const Cut& cut, const RowLimits& limits, const Weigh& weigh, const SampleArgs& a, int64_t r) {
-  __syncthreads();
-  for (uint32_t p = threadIdx.x; p < plan.length; p += kThreads) {
-    const uint64_t x = sh.list[p];
-    sh.list[p] = (x << 32) | (x >> 32);        // index first
+  uint32_t lo = 0, hi = (uint32_t)a.n - 1;
+  Sum above{0, 0, 0}, total{0, 0, 0};
+  while (true) {
+    const int bits = lo < hi ? 32 - __clz(hi - lo) : 0;
+    const int shift = bits > 11 ? bits - 11 : 0;
+    clear_histogram(sh, true);
+    for (uint32_t p = threadIdx.x; p < plan.length; p += kThreads) {
+      const uint64_t x = sh.list[p];
+      const uint32_t at = (uint32_t)x;
+      if (at < lo || at > hi) continue;
+      const double e = kept_weight(entry_key(x), at, cut, limits.min_p, weigh);
+      if (e > 0.0) add_to(sh.hist, kBins - 1 - (int)((at - lo) >> shift), true, e);
+    }
+    __syncthreads();
+    if (total.count == 0) total = sum_of_bins(sh);
+    const uint32_t b = find_answer(sh, above, total, limits.u);
+    above = sh.found_above;
+    const Sum in = sh.found_in;
+    lo = lo + (b << shift);
+    hi = min(hi, lo + ((1u << shift) - 1u));
+    __syncthreads();
+    if (shift == 0) {
+      answer(a, r, lo, in, total);
+      return;
+    }
   }
-  sort_entries(sh, plan.length);
-  auto weight = [&](uint64_t x) { return kept_weight(~(uint32_t)x, (uint32_t)(x >> 32), cut, limits.min_p, weigh); };
-  const Sum total = sum_of_list(sh, plan.length, weight);
-  const double target = limits.u * total.value();
-  Sum above{0, 0, 0};
-  const uint32_t p = find_place(sh, plan.length, above, weight, [=](const Sum& s) { return s.value() > target || s.same_weight(total); });
-  answer(a, r, (uint32_t)(sh.list[p] >> 32), sh.found_in, total);
 }
 
 __device__ __forceinline__ bool answer_without_weights(uint32_t kmax, uint32_t first, const RowLimits& limits, const SampleArgs& a, int64_t r) {
