@@ -223,7 +223,7 @@ __device__ __forceinline__ uint64_t shfl_up64(uint64_t v, int d) { return (uint6
 // The first bin from above at which `reached(sum of everything above and the bin)` holds, into sh.found_*; found_bin -1 if none
 // does.  Returns the sum of all bins.
 template <typename Reached>
-__device__ Sum find_bin(Shared& sh, const Sum& above, bool weights, Reached reached) {
+__device__ __forceinline__ Sum find_bin(Shared& sh, const Sum& above, bool weights, Reached reached) {
   constexpr int per = kBins / kThreads;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   Sum own[per], total{0, 0, 0};
@@ -273,7 +273,7 @@ __device__ Sum find_bin(Shared& sh, const Sum& above, bool weights, Reached reac
   return everything;
 }
 
-__device__ void clear_histogram(Shared& sh, bool weights) {
+__device__ __forceinline__ void clear_histogram(Shared& sh, bool weights) {
   for (int b = threadIdx.x; b < kBins; b += kThreads) {
     sh.hist.count[b] = 0;
     if (weights) {
@@ -286,7 +286,7 @@ __device__ void clear_histogram(Shared& sh, bool weights) {
 
 // ---- the long way: histograms over the whole row down to the cut
 template <typename V, typename Bin>
-__device__ void fill_by_key(Shared& sh, const Row<V>& row, uint32_t lo, uint32_t hi, bool weights, const Weigh& weigh, Bin bin) {
+__device__ __forceinline__ void fill_by_key(Shared& sh, const Row<V>& row, uint32_t lo, uint32_t hi, bool weights, const Weigh& weigh, Bin bin) {
   clear_histogram(sh, weights);
   for_row<1>(row, 0, row.pieces(), threadIdx.x, kThreads, [&](uint32_t, float s) {
     const uint32_t key = key_of(s);
@@ -297,7 +297,7 @@ __device__ void fill_by_key(Shared& sh, const Row<V>& row, uint32_t lo, uint32_t
 
 // From the bin that find_bin left (of the histogram over `steps`) down to a single key.  false: no cut, everything is kept.
 template <typename V, typename Reached>
-__device__ bool narrow(Shared& sh, const Row<V>& row, const Steps& steps, uint32_t kmin, uint32_t kmax, bool weights,
+__device__ __forceinline__ bool narrow(Shared& sh, const Row<V>& row, const Steps& steps, uint32_t kmin, uint32_t kmax, bool weights,
                        const Weigh& weigh, Reached reached, uint32_t& cut, Sum& above, Sum& in) {
   if (sh.found_bin < 0) return false;
   uint32_t lo, hi;
@@ -335,7 +335,7 @@ __device__ __forceinline__ uint64_t ties_below(double above, double e, double ta
 }
 
 template <typename V>
-__device__ void cut_the_long_way(Shared& sh, const Row<V>& row, uint32_t kmin, uint32_t kmax, const Weigh& weigh, const RowLimits& limits, Cut& cut) {
+__device__ __noinline__ void cut_the_long_way(Shared& sh, const Row<V>& row, uint32_t kmin, uint32_t kmax, const Weigh& weigh, const RowLimits& limits, Cut& cut) {
   const Steps steps(kmin, kmax);
   uint64_t ties = 0;
   bool all_ties = true;
@@ -414,7 +414,7 @@ __device__ __forceinline__ void answer(const SampleArgs& a, int64_t r, uint32_t 
 
 // The answer among the indices [lo, hi] of the row, of which `above` lies in front, of `total` in all (none: to be found).
 template <typename V>
-__device__ void choose_index(Shared& sh, const Row<V>& row, uint32_t lo, uint32_t hi, Sum above, Sum total, const Cut& cut,
+__device__ __forceinline__ void choose_index(Shared& sh, const Row<V>& row, uint32_t lo, uint32_t hi, Sum above, Sum total, const Cut& cut,
                              const Weigh& weigh, const RowLimits& limits, const SampleArgs& a, int64_t r) {
   bool known = total.count != 0;
   while (true) {
@@ -460,7 +460,7 @@ __device__ __forceinline__ void order(uint64_t& x, uint64_t& y, bool up) {
   x = a;
   y = b;
 }
-__device__ void sort_list(ListShared& sh, uint32_t size) {
+__device__ __forceinline__ void sort_list(ListShared& sh, uint32_t size) {
   __syncthreads();
   for (uint32_t block = 2; block <= size; block <<= 1) {
     uint32_t stride = block >> 1;
@@ -497,7 +497,7 @@ __device__ void sort_list(ListShared& sh, uint32_t size) {
   __syncthreads();
 }
 // pads to a power of two (entries that sort last) and sorts
-__device__ void sort_entries(ListShared& sh, uint32_t length) {
+__device__ __forceinline__ void sort_entries(ListShared& sh, uint32_t length) {
   uint32_t size = 4;
   while (size < length) size <<= 1;
   __syncthreads();
@@ -515,7 +515,7 @@ struct Plan {
   double whole;                                // sum of all weights, where they were added
 };
 // The first histogram is in sh.hist (weights only for top-p without top-k).
-__device__ Plan make_plan(Shared& sh, uint32_t kmin, uint32_t kmax, const RowLimits& limits) {
+__device__ __forceinline__ Plan make_plan(Shared& sh, uint32_t kmin, uint32_t kmax, const RowLimits& limits) {
   Plan plan{false, false, true, 1, 0, 0, Sum{0, 0, 0}, 0.0};
   if (!limits.by_k && !limits.by_p) return plan;
   const bool weights = !limits.by_k;
@@ -544,14 +544,14 @@ __device__ Plan make_plan(Shared& sh, uint32_t kmin, uint32_t kmax, const RowLim
 }
 
 // The weights of the list's entries from .. to, entry `from` in the highest bin.
-__device__ void fill_by_place(Shared& sh, uint32_t from, uint32_t to, const Weigh& weigh) {
+__device__ __forceinline__ void fill_by_place(Shared& sh, uint32_t from, uint32_t to, const Weigh& weigh) {
   clear_histogram(sh, true);
   for (uint32_t p = from + threadIdx.x; p < to; p += kThreads) add_to(sh.hist, kBins - 1 - (p - from), true, weigh(score_of(entry_key(sh.list[p]))));
   __syncthreads();
 }
 // The first of the sorted entries 0 .. to - 1 at which the weights, with those of `above`, reach top_p of `whole` (negative: of
 // these entries' sum); to - 1 if rounding leaves none.
-__device__ uint32_t place_of_top_p(Shared& sh, uint32_t to, Sum above, double whole, float top_p, const Weigh& weigh) {
+__device__ __forceinline__ uint32_t place_of_top_p(Shared& sh, uint32_t to, Sum above, double whole, float top_p, const Weigh& weigh) {
   uint32_t from = 0;
   fill_by_place(sh, 0, min((uint32_t)kBins, to), weigh);
   if (whole < 0.0) {
@@ -576,7 +576,7 @@ __device__ uint32_t place_of_top_p(Shared& sh, uint32_t to, Sum above, double wh
 }
 
 // The list, sorted, to the cut.
-__device__ void cut_from_list(Shared& sh, const Plan& plan, const RowLimits& limits, const Weigh& weigh, Cut& cut) {
+__device__ __forceinline__ void cut_from_list(Shared& sh, const Plan& plan, const RowLimits& limits, const Weigh& weigh, Cut& cut) {
   sort_entries(sh, plan.length);
   uint32_t last = limits.by_k ? min((uint32_t)limits.k, plan.length) - 1 : plan.length - 1;
   if (limits.by_p && !(limits.top_p > 0.0f)) {
@@ -589,7 +589,7 @@ __device__ void cut_from_list(Shared& sh, const Plan& plan, const RowLimits& lim
 }
 
 // With top-k the list holds every node that may be chosen: histograms of its weights along the index, down to one.
-__device__ void choose_from_list(Shared& sh, const Plan& plan, const Cut& cut, const RowLimits& limits, const Weigh& weigh, const SampleArgs& a, int64_t r) {
+__device__ __forceinline__ void choose_from_list(Shared& sh, const Plan& plan, const Cut& cut, const RowLimits& limits, const Weigh& weigh, const SampleArgs& a, int64_t r) {
   uint32_t lo = 0, hi = (uint32_t)a.n - 1;
   Sum above{0, 0, 0}, total{0, 0, 0};
   while (true) {
@@ -644,7 +644,7 @@ struct Extreme {
   }
 };
 template <typename V>
-__device__ Extreme extreme_of(const Row<V>& row, uint32_t from, uint32_t to) {           // the same in every lane
+__device__ __forceinline__ Extreme extreme_of(const Row<V>& row, uint32_t from, uint32_t to) {           // the same in every lane
   __shared__ Extreme wave_x[kWaves];
   Extreme x{0xffffffffu, 0, 0xffffffffu, 0};
   for_row<kAhead>(row, from, to, threadIdx.x, kThreads, [&](uint32_t at, float s) {
@@ -660,7 +660,7 @@ __device__ Extreme extreme_of(const Row<V>& row, uint32_t from, uint32_t to) {  
 
 // The first histogram of the pieces from .. to.
 template <typename V>
-__device__ void first_histogram(Histogram& hist, const Row<V>& row, uint32_t from, uint32_t to, const Steps& steps, bool weights, const Weigh& weigh) {
+__device__ __forceinline__ void first_histogram(Histogram& hist, const Row<V>& row, uint32_t from, uint32_t to, const Steps& steps, bool weights, const Weigh& weigh) {
   if (weights)
     for_row<1>(row, from, to, threadIdx.x, kThreads, [&](uint32_t, float s) { add_to(hist, steps(s), true, weigh(s)); });
   else
