@@ -218,14 +218,51 @@ __device__ __forceinline__ void for_row(const Row<V>& row, uint32_t from, uint32
   }
 }
 
-__device__ __forceinline__ uint64_t shfl_up64(uint64_t v, int d) { return (uint64_t)__shfl_up((unsigned long long)v, d, 64); }
+// Inclusive sums over the lanes of a wave, by moves inside and between the rows of 16 lanes (an add each, where a shuffle goes
+// through LDS: half the time of a histogram's search was shuffles).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t moved(uint64_t v) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xf, false);
+  return ((uint64_t)hi << 32) | lo;
+}
+__device__ __forceinline__ uint64_t wave_sums(uint64_t v) {
+  v += moved<0x111, 0xf>(v);                   // row_shr:1, 2, 4, 8
+  v += moved<0x112, 0xf>(v);
+  v += moved<0x114, 0xf>(v);
+  v += moved<0x118, 0xf>(v);
+  v += moved<0x142, 0xa>(v);                   // row_bcast:15 into rows 1 and 3, row_bcast:31 into rows 2 and 3
+  v += moved<0x143, 0xc>(v);
+  return v;
+}
+
+// Sums of `own` over the workgroup: before this lane, and of all lanes.
+__device__ __forceinline__ void block_sums(Shared& sh, const Sum& own, bool weights, Sum& before, Sum& all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  Sum upto{wave_sums(own.count), 0, 0};
+  if (weights) {
+    upto.hi = wave_sums(own.hi);
+    upto.lo = wave_sums(own.lo);
+  }
+  if (lane == 63) sh.wave_sum[wave] = upto;
+  if (threadIdx.x == 0) sh.found_bin = -1;
+  __syncthreads();
+  before = upto - own;
+  all = Sum{0, 0, 0};
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const Sum s = sh.wave_sum[w];
+    if (w < wave) before = before + s;
+    all = all + s;
+  }
+}
 
 // The first bin from above at which `reached(sum of everything above and the bin)` holds, into sh.found_*; found_bin -1 if none
-// does.  Returns the sum of all bins.
-template <typename Reached>
-__device__ __forceinline__ Sum find_bin(Shared& sh, const Sum& above, bool weights, Reached reached) {
+// does.  `make_reached` gets the sum of all bins, which is returned.
+template <typename MakeReached>
+__device__ __forceinline__ Sum find_bin_of(Shared& sh, const Sum& above, bool weights, MakeReached make_reached) {
   constexpr int per = kBins / kThreads;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x;
   Sum own[per], total{0, 0, 0};
 #pragma unroll
   for (int k = 0; k < per; ++k) {
@@ -233,44 +270,30 @@ __device__ __forceinline__ Sum find_bin(Shared& sh, const Sum& above, bool weigh
     own[k] = Sum{sh.hist.count[b], weights ? sh.hist.hi[b] : 0, weights ? sh.hist.lo[b] : 0};
     total = total + own[k];
   }
-  Sum upto = total;
+  Sum before, all;
+  block_sums(sh, total, weights, before, all);
+  before = before + above;
+  const auto reached = make_reached(all);
+  if (total.count != 0 && reached(before + total) && !reached(before)) {           // one lane
+    bool found = false;
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t c = __shfl_up((uint32_t)upto.count, d, 64);   // counts of one row: below 2^31
-    if (lane >= d) upto.count += c;
-  }
-  if (weights) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint64_t h = shfl_up64(upto.hi, d), l = shfl_up64(upto.lo, d);
-      if (lane >= d) {
-        upto.hi += h;
-        upto.lo += l;
+    for (int k = 0; k < per; ++k) {
+      const Sum with = before + own[k];
+      if (!found && own[k].count != 0 && reached(with)) {
+        found = true;
+        sh.found_bin = kBins - 1 - (tid * per + k);
+        sh.found_above = before;
+        sh.found_in = own[k];
       }
+      before = with;
     }
   }
-  if (lane == 63) sh.wave_sum[wave] = upto;
-  if (tid == 0) sh.found_bin = -1;
   __syncthreads();
-  Sum before = above, everything{0, 0, 0};
-  for (int w = 0; w < kWaves; ++w) {
-    const Sum s = sh.wave_sum[w];
-    if (w < wave) before = before + s;
-    everything = everything + s;
-  }
-  before = before + (upto - total);
-#pragma unroll
-  for (int k = 0; k < per; ++k) {
-    const Sum with = before + own[k];
-    if (own[k].count != 0 && reached(with) && !reached(before)) {
-      sh.found_bin = kBins - 1 - (tid * per + k);
-      sh.found_above = before;
-      sh.found_in = own[k];
-    }
-    before = with;
-  }
-  __syncthreads();
-  return everything;
+  return all;
+}
+template <typename Reached>
+__device__ __forceinline__ Sum find_bin(Shared& sh, const Sum& above, bool weights, Reached reached) {
+  return find_bin_of(sh, above, weights, [=](const Sum&) { return reached; });
 }
 
 __device__ __forceinline__ void clear_histogram(Shared& sh, bool weights) {
@@ -282,6 +305,12 @@ __device__ __forceinline__ void clear_histogram(Shared& sh, bool weights) {
     }
   }
   __syncthreads();
+}
+
+__device__ __forceinline__ Sum sum_of_bins(Shared& sh) {
+  const Sum total = find_bin(sh, Sum{0, 0, 0}, true, [](const Sum&) { return false; });
+  __syncthreads();
+  return total;
 }
 
 // ---- the long way: histograms over the whole row down to the cut
@@ -342,10 +371,7 @@ __device__ __noinline__ void cut_the_long_way(Shared& sh, const Row<V>& row, uin
   double whole = 0.0;
   for (int by_p = limits.by_k ? 0 : 1; by_p <= (limits.by_p ? 1 : 0); ++by_p) {
     fill_by_key(sh, row, kmin, kmax, limits.by_p, weigh, [=](uint32_t, float s) { return steps(s); });
-    if (by_p && (!limits.by_k || cut.key == 0)) {                  // top-k, if any, keeps everything
-      whole = find_bin(sh, Sum{0, 0, 0}, true, [](const Sum&) { return false; }).value();
-      __syncthreads();
-    }
+    if (by_p && (!limits.by_k || cut.key == 0)) whole = sum_of_bins(sh).value();     // top-k, if any, keeps everything
     const double target = (double)limits.top_p * whole;
     const uint64_t k = (uint64_t)limits.k;
     const bool first_alone = by_p && !(limits.top_p > 0.0f);
@@ -393,18 +419,18 @@ __device__ __forceinline__ double kept_weight(uint32_t key, uint32_t at, const C
   return min_p > 0.0 && !(e >= min_p) ? 0.0 : e;
 }
 
-// The bin (of a histogram whose bins go down with the index) that the random number falls into.  Past every weight there is:
-// the last that has any.
-__device__ __forceinline__ uint32_t find_answer(Shared& sh, const Sum& above, const Sum& total, double u) {
-  const double target = u * total.value();
-  const Sum all = total;
-  find_bin(sh, above, true, [=](const Sum& s) { return s.value() > target || s.same_weight(all); });
+// The bin (of a histogram whose bins go down with the index) that the random number falls into; `total`, of all weights, is what
+// the bins add up to if it is not known yet.  Past every weight there is: the last that has any.
+__device__ __forceinline__ uint32_t find_answer(Shared& sh, const Sum& above, Sum& total, double u) {
+  const bool known = total.count != 0;
+  const Sum given = total;
+  const Sum bins = find_bin_of(sh, above, true, [=](const Sum& sum) {
+    const Sum all = known ? given : sum;
+    const double target = u * all.value();
+    return [=](const Sum& s) { return s.value() > target || s.same_weight(all); };
+  });
+  if (!known) total = bins;
   return kBins - 1 - sh.found_bin;
-}
-__device__ __forceinline__ Sum sum_of_bins(Shared& sh) {
-  const Sum total = find_bin(sh, Sum{0, 0, 0}, true, [](const Sum&) { return false; });
-  __syncthreads();
-  return total;
 }
 __device__ __forceinline__ void answer(const SampleArgs& a, int64_t r, uint32_t at, const Sum& in, const Sum& total) {
   if (threadIdx.x != 0) return;
@@ -416,7 +442,6 @@ __device__ __forceinline__ void answer(const SampleArgs& a, int64_t r, uint32_t 
 template <typename V>
 __device__ __forceinline__ void choose_index(Shared& sh, const Row<V>& row, uint32_t lo, uint32_t hi, Sum above, Sum total, const Cut& cut,
                              const Weigh& weigh, const RowLimits& limits, const SampleArgs& a, int64_t r) {
-  bool known = total.count != 0;
   while (true) {
     const int bits = lo < hi ? 32 - __clz(hi - lo) : 0;
     const int shift = bits > 11 ? bits - 11 : 0;
@@ -428,8 +453,6 @@ __device__ __forceinline__ void choose_index(Shared& sh, const Row<V>& row, uint
       if (e > 0.0) add_to(sh.hist, kBins - 1 - (int)((at - lo) >> shift), true, e);
     });
     __syncthreads();
-    if (!known) total = sum_of_bins(sh);
-    known = true;
     const uint32_t b = find_answer(sh, above, total, limits.u);
     above = sh.found_above;
     const Sum in = sh.found_in;
@@ -519,15 +542,14 @@ __device__ __forceinline__ Plan make_plan(Shared& sh, uint32_t kmin, uint32_t km
   Plan plan{false, false, true, 1, 0, 0, Sum{0, 0, 0}, 0.0};
   if (!limits.by_k && !limits.by_p) return plan;
   const bool weights = !limits.by_k;
-  double target = 0.0;
-  if (weights) {
-    plan.whole = sum_of_bins(sh).value();
-    target = (double)limits.top_p * plan.whole;
-  }
-  const uint64_t k = (uint64_t)limits.k;
+  const double top_p = (double)limits.top_p;
   // top_p <= 0 keeps the first node alone: the bin of the greatest
-  const bool first_alone = weights && !(limits.top_p > 0.0f);
-  find_bin(sh, Sum{0, 0, 0}, weights, [=](const Sum& s) { return first_alone ? s.count >= 1 : weights ? s.value() >= target : s.count >= k; });
+  const bool by_sum = weights && limits.top_p > 0.0f;
+  const uint64_t k = weights ? 1 : (uint64_t)limits.k;
+  plan.whole = find_bin_of(sh, Sum{0, 0, 0}, weights, [=](const Sum& all) {
+    const double target = top_p * all.value();
+    return [=](const Sum& s) { return by_sum ? s.value() >= target : s.count >= k; };
+  }).value();
   plan.listed = sh.found_bin >= 0;
   if (plan.listed) {
     plan.above = sh.found_above;
@@ -543,36 +565,36 @@ __device__ __forceinline__ Plan make_plan(Shared& sh, uint32_t kmin, uint32_t km
   return plan;
 }
 
-// The weights of the list's entries from .. to, entry `from` in the highest bin.
-__device__ __forceinline__ void fill_by_place(Shared& sh, uint32_t from, uint32_t to, const Weigh& weigh) {
-  clear_histogram(sh, true);
-  for (uint32_t p = from + threadIdx.x; p < to; p += kThreads) add_to(sh.hist, kBins - 1 - (p - from), true, weigh(score_of(entry_key(sh.list[p]))));
-  __syncthreads();
-}
-// The first of the sorted entries 0 .. to - 1 at which the weights, with those of `above`, reach top_p of `whole` (negative: of
-// these entries' sum); to - 1 if rounding leaves none.
-__device__ __forceinline__ uint32_t place_of_top_p(Shared& sh, uint32_t to, Sum above, double whole, float top_p, const Weigh& weigh) {
-  uint32_t from = 0;
-  fill_by_place(sh, 0, min((uint32_t)kBins, to), weigh);
-  if (whole < 0.0) {
-    Sum total = sum_of_bins(sh);
-    for (from = kBins; from < to; from += kBins) {
-      fill_by_place(sh, from, min(from + kBins, to), weigh);
-      total = total + sum_of_bins(sh);
+// The first of the sorted entries 0 .. to - 1 at which `reached` holds for the sum of the weights up to it; to - 1 if there is
+// none.  make_reached gets the sum of all of them.  `chosen`: that entry's weight, `total`: the sum of all.
+template <typename Weight, typename MakeReached>
+__device__ __forceinline__ uint32_t place_in_list(Shared& sh, uint32_t to, const Sum& above, Weight weight, MakeReached make_reached,
+                                                  Sum& chosen, Sum& total) {
+  const uint32_t per = (to + kThreads - 1) / kThreads, from = threadIdx.x * per, end = min(from + per, to);
+  Sum own{0, 0, 0};
+  for (uint32_t p = from; p < end; ++p) {
+    const uint64_t w = units_of(weight(sh.list[p]));
+    own = own + Sum{1, w >> 31, w & 0x7fffffffu};
+  }
+  Sum before;
+  block_sums(sh, own, true, before, total);
+  before = before + above;
+  const auto reached = make_reached(total);
+  if (own.count != 0 && reached(before + own) && !reached(before)) {               // one lane
+    for (uint32_t p = from; p < end; ++p) {
+      const uint64_t w = units_of(weight(sh.list[p]));
+      const Sum in{1, w >> 31, w & 0x7fffffffu};
+      before = before + in;
+      if (reached(before)) {
+        sh.found_bin = (int)p;
+        sh.found_in = in;
+        break;
+      }
     }
-    if (to > (uint32_t)kBins) fill_by_place(sh, 0, kBins, weigh);
-    whole = total.value();
   }
-  const double target = (double)top_p * whole;
-  for (from = 0;;) {
-    const Sum part = find_bin(sh, above, true, [=](const Sum& s) { return s.value() >= target; });
-    if (sh.found_bin >= 0) return from + kBins - 1 - sh.found_bin;
-    from += kBins;
-    if (from >= to) return to - 1;
-    above = above + part;
-    __syncthreads();
-    fill_by_place(sh, from, min(from + kBins, to), weigh);
-  }
+  __syncthreads();
+  chosen = sh.found_in;
+  return sh.found_bin < 0 ? to - 1 : (uint32_t)sh.found_bin;
 }
 
 // The list, sorted, to the cut.
@@ -582,40 +604,36 @@ __device__ __forceinline__ void cut_from_list(Shared& sh, const Plan& plan, cons
   if (limits.by_p && !(limits.top_p > 0.0f)) {
     last = 0;
   } else if (limits.by_p) {
-    last = place_of_top_p(sh, last + 1, limits.by_k ? Sum{0, 0, 0} : plan.above, limits.by_k ? -1.0 : plan.whole, limits.top_p, weigh);
+    const double top_p = (double)limits.top_p, whole = plan.whole;
+    const bool by_k = limits.by_k;
+    Sum chosen, total;
+    last = place_in_list(sh, last + 1, by_k ? Sum{0, 0, 0} : plan.above, [&](uint64_t x) { return weigh(score_of(entry_key(x))); },
+                         [=](const Sum& all) {
+                           const double target = top_p * (by_k ? all.value() : whole);
+                           return [=](const Sum& s) { return s.value() >= target; };
+                         }, chosen, total);
   }
   cut.key = entry_key(sh.list[last]);
   cut.last_tie = (uint32_t)sh.list[last];
 }
 
-// With top-k the list holds every node that may be chosen: histograms of its weights along the index, down to one.
+// With top-k the list holds every node that may be chosen: by index now.
 __device__ __forceinline__ void choose_from_list(Shared& sh, const Plan& plan, const Cut& cut, const RowLimits& limits, const Weigh& weigh, const SampleArgs& a, int64_t r) {
-  uint32_t lo = 0, hi = (uint32_t)a.n - 1;
-  Sum above{0, 0, 0}, total{0, 0, 0};
-  while (true) {
-    const int bits = lo < hi ? 32 - __clz(hi - lo) : 0;
-    const int shift = bits > 11 ? bits - 11 : 0;
-    clear_histogram(sh, true);
-    for (uint32_t p = threadIdx.x; p < plan.length; p += kThreads) {
-      const uint64_t x = sh.list[p];
-      const uint32_t at = (uint32_t)x;
-      if (at < lo || at > hi) continue;
-      const double e = kept_weight(entry_key(x), at, cut, limits.min_p, weigh);
-      if (e > 0.0) add_to(sh.hist, kBins - 1 - (int)((at - lo) >> shift), true, e);
-    }
-    __syncthreads();
-    if (total.count == 0) total = sum_of_bins(sh);
-    const uint32_t b = find_answer(sh, above, total, limits.u);
-    above = sh.found_above;
-    const Sum in = sh.found_in;
-    lo = lo + (b << shift);
-    hi = min(hi, lo + ((1u << shift) - 1u));
-    __syncthreads();
-    if (shift == 0) {
-      answer(a, r, lo, in, total);
-      return;
-    }
+  __syncthreads();
+  for (uint32_t p = threadIdx.x; p < plan.length; p += kThreads) {
+    const uint64_t x = sh.list[p];
+    sh.list[p] = (x << 32) | (x >> 32);        // index first
   }
+  sort_entries(sh, plan.length);
+  const double u = limits.u;
+  Sum chosen, total;
+  const uint32_t p = place_in_list(sh, plan.length, Sum{0, 0, 0},
+                                   [&](uint64_t x) { return kept_weight(~(uint32_t)x, (uint32_t)(x >> 32), cut, limits.min_p, weigh); },
+                                   [=](const Sum& all) {
+                                     const double target = u * all.value();
+                                     return [=](const Sum& s) { return s.value() > target || s.same_weight(all); };
+                                   }, chosen, total);
+  answer(a, r, (uint32_t)(sh.list[p] >> 32), chosen, total);
 }
 
 __device__ __forceinline__ bool answer_without_weights(uint32_t kmax, uint32_t first, const RowLimits& limits, const SampleArgs& a, int64_t r) {
@@ -898,7 +916,6 @@ __global__ __launch_bounds__(kThreads) void finish_rows_kernel(SplitArgs a) {
       if (e > 0.0) add_to(sh.hist, kBins - 1 - (int)((at + row.skew) / a.width), true, e);
     }
     __syncthreads();
-    total = sum_of_bins(sh);
     const uint32_t part = find_answer(sh, above, total, limits.u);
     above = sh.found_above;
     __syncthreads();
