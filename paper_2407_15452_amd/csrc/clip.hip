@@ -92,13 +92,19 @@ __device__ __forceinline__ double piece_squares(uint4 w) {
   }
   return s;
 }
+// In fp64: a factor far below 1 would lose its bits in fp32, where norms of 1e40 exist.  (16-bit formats: through fp32, which
+// moves a result only within 2^-24 of the middle between two of the format's numbers.)
 template <typename V>
-__device__ __forceinline__ uint4 piece_scaled(uint4 w, float factor) {
+__device__ __forceinline__ typename V::elem scaled(typename V::elem x, double factor) {
+  return V::put((float)((double)V::get(x) * factor));
+}
+template <typename V>
+__device__ __forceinline__ uint4 piece_scaled(uint4 w, double factor) {
   constexpr int per = 16 / (int)sizeof(typename V::elem);
   typename V::elem e[per];
   __builtin_memcpy(e, &w, 16);
 #pragma unroll
-  for (int k = 0; k < per; ++k) e[k] = V::put(V::get(e[k]) * factor);
+  for (int k = 0; k < per; ++k) e[k] = scaled<V>(e[k], factor);
   __builtin_memcpy(&w, e, 16);
   return w;
 }
@@ -134,7 +140,7 @@ __device__ double unit_squares(const Item& it, uint32_t unit) {
 }
 
 template <typename V>
-__device__ void unit_scaled(const Item& it, uint32_t unit, float factor, bool copy) {
+__device__ void unit_scaled(const Item& it, uint32_t unit, double factor, bool copy) {
   typedef typename V::elem elem;
   constexpr int per = 16 / (int)sizeof(elem);
   const elem* x = static_cast<const elem*>(it.data);
@@ -160,13 +166,13 @@ __device__ void unit_scaled(const Item& it, uint32_t unit, float factor, bool co
   } else {                                     // the two lie differently: element by element
     const int64_t from = head + (int64_t)unit * kUnit * per;
     const int64_t end = min(from + (int64_t)kUnit * per, tail);
-    for (int64_t i = from + threadIdx.x; i < end; i += kThreads) y[i] = copy ? x[i] : V::put(V::get(x[i]) * factor);
+    for (int64_t i = from + threadIdx.x; i < end; i += kThreads) y[i] = copy ? x[i] : scaled<V>(x[i], factor);
   }
   if (unit == 0) {
     const int64_t rest = head + (it.count - tail);
     if ((int64_t)threadIdx.x < rest) {
       const int64_t at = (int64_t)threadIdx.x < head ? (int64_t)threadIdx.x : tail + ((int64_t)threadIdx.x - head);
-      y[at] = copy ? x[at] : V::put(V::get(x[at]) * factor);
+      y[at] = copy ? x[at] : scaled<V>(x[at], factor);
     }
   }
 }
@@ -224,7 +230,7 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(Items list, Pass a) {
   if (blockIdx.x == 0 && threadIdx.x == 0) *a.norm_out = norm;
   // a norm that is no number, or infinite, says that some gradient is: nothing is scaled by it
   const bool reached = norm > a.max_norm && norm < INFINITY;
-  const float factor = reached ? (float)(a.max_norm / norm) : 1.0f;
+  const double factor = reached ? a.max_norm / norm : 1.0;
   for_units<TABLE>(list, a, gridDim.x - 1 - blockIdx.x, [&](const Item& it, uint32_t unit) {
     if (!reached && it.out == it.data) return;
     if (it.dtype == GS_F32) unit_scaled<F32Value>(it, unit, factor, !reached);

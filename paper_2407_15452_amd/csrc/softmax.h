@@ -12,7 +12,8 @@
 // probabilities, is the right operand of the second product without leaving the registers: the matrix instruction sums over
 // any numbering of its inner dimension, as long as both operands use the same one.  The left operand of the second product is
 // the streamed tile again, transposed on its way out of LDS (16-bit tables: ds_read_b64_tr_b16; fp32: one column per lane).
-//   forward: pairs kept, nodes streamed, running maximum and sum; gives the loss and sum_j p_ij c_j in one pass.
+//   forward: pairs kept, nodes streamed, running maximum and sum over the nodes but the context; gives the loss, 1 - p_it and
+//     sum_{j != t} p_ij c_j in one pass.
 //   table gradient: nodes kept, pairs streamed, p from the forward pass's log-sum; no atomics, each row of g_out has one owner.
 // Where the kept rows alone do not fill the chip the streamed ones are split, and a small kernel joins the parts in order.
 //
@@ -51,7 +52,7 @@ struct SoftmaxPlan {
   int64_t tiles_per_split, tiles_per_node_split;
   void* rows;
   int32_t* target;
-  float *lse2, *part_max, *part_acc;
+  float *lse2, *miss, *part_max, *part_acc;
   double* part_sum;
   size_t bytes;
 };
@@ -203,20 +204,19 @@ __device__ __forceinline__ acc16 step(vec4 a, vec4 b, acc16 c) {
 }
 
 // ---- the pairs' rows, copied for the table gradient --------------------------------------------------------------------
-// rows[i] = w_in[centers[i]], zero-padded to DP columns and to whole tiles.
+// rows[i] = w_in[centers[i]], zero-padded to DP columns and to whole tiles; zeros for pairs without gradient (target -1).
 template <typename E>
-__global__ __launch_bounds__(kThreads) void gather_pairs_kernel(const typename E::elem* w_in, int64_t num_in, int dim, int padded,
-                                                                const int32_t* centers, int64_t num_pairs, int64_t padded_pairs,
-                                                                typename E::elem* rows) {
+__global__ __launch_bounds__(kThreads) void gather_pairs_kernel(const typename E::elem* w_in, int dim, int padded,
+                                                                const int32_t* centers, const int32_t* target,
+                                                                int64_t padded_pairs, typename E::elem* rows) {
   constexpr int per = 16 / (int)sizeof(typename E::elem);
   const int pieces = padded / per;
   const int64_t total = padded_pairs * pieces;
   for (int64_t s = (int64_t)blockIdx.x * kThreads + threadIdx.x; s < total; s += (int64_t)gridDim.x * kThreads) {
     const int64_t i = s / pieces;
     const int p = (int)(s - i * pieces);
-    const int64_t c = i < num_pairs ? centers[i] : -1;
     uint4 v = make_uint4(0, 0, 0, 0);
-    if (c >= 0 && c < num_in && p * per < dim) v = reinterpret_cast<const uint4*>(w_in)[(c * dim + p * per) / per];
+    if (target[i] >= 0 && p * per < dim) v = reinterpret_cast<const uint4*>(w_in)[((int64_t)centers[i] * dim + p * per) / per];
     reinterpret_cast<uint4*>(rows)[s] = v;
   }
 }
@@ -232,8 +232,9 @@ struct StreamArgs {
   float scale2;              // scale * log2(e); scores: scale
   float out_scale;
   const float* bias;         // [nodes] or null
-  const float* lse2;         // [pairs, whole tiles] base-2 log-sums (table gradient)
-  const int32_t* target;     // [pairs, whole tiles] (table gradient)
+  const float* lse2;         // table gradient: [pairs, whole tiles] base-2 log-sums
+  const float* miss;         // .. 1 - p of the pair's context
+  const int32_t* target;     // .. that context, or -1; forward: contexts [pairs]
   int64_t kept_tiles;        // workgroups along the kept rows
   int32_t splits;
   int64_t tiles_per_split;
@@ -252,6 +253,7 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
   constexpr bool SECOND = MODE == kForward || MODE == kTableGrad;
   __shared__ __attribute__((aligned(1024))) char tile[2][TILE * ROWB];
   __shared__ float side[2][TILE];              // nodes streamed: bias * log2(e); pairs streamed: base-2 log-sums
+  __shared__ float side_miss[2][TILE];         // pairs streamed
   __shared__ int32_t side_target[2][TILE];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, l32 = lane & 31;
@@ -274,12 +276,15 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
   // ---- kept rows into registers
   vec4 kept[NB][KS];
   float kept_bias[NB];
+  int32_t kept_target[NB];                     // pairs kept: their contexts
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     int64_t row = kept_row0 + 32 * nb;
     bool live = row < a.kept_rows;
     kept_bias[nb] = 0.0f;
+    kept_target[nb] = -1;
     if constexpr (NODES_STREAMED) {
+      if (live) kept_target[nb] = a.target[row];
       row = live ? a.centers[row] : -1;
       live = row >= 0 && row < a.num_in;
     } else if constexpr (BIAS) {
@@ -296,7 +301,7 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
 
   // ---- staging: a wave's load number n fills the 64 pieces of chunk 4 n + wave of a tile
   float row_bias[S::kLoads];                   // nodes streamed, with bias: of the rows of the next tile to ask for
-  float side_value = 0.0f;
+  float side_value = 0.0f, miss_value = 0.0f;
   int32_t side_id = -1;
   auto slot_row = [&](int n) { return ((4 * n + wave) * 64 + lane) / PIECES; };
   auto has_chunk = [&](int n) { return S::kChunks % 4 == 0 || 4 * n + wave < S::kChunks; };
@@ -346,6 +351,7 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
       const int64_t row = t * TILE + tid;
       if constexpr (MODE == kTableGrad) {
         side_value = a.lse2[row];
+        miss_value = a.miss[row];
         side_id = a.target[row];
       } else if constexpr (NODES_STREAMED && BIAS) {
         side_value = row < a.streamed_rows ? a.bias[row] * kLog2e : -INFINITY;
@@ -356,7 +362,10 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
     if constexpr (MODE == kTableGrad || (NODES_STREAMED && BIAS)) {
       if (tid < TILE) {
         side[buf][tid] = side_value;
-        if constexpr (MODE == kTableGrad) side_target[buf][tid] = side_id;
+        if constexpr (MODE == kTableGrad) {
+          side_miss[buf][tid] = miss_value;
+          side_target[buf][tid] = side_id;
+        }
       }
     }
   };
@@ -444,6 +453,24 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
             for (int r = 0; r < 16; ++r)
               if (32 * jb + 8 * (r / 4) + r % 4 >= left) z[jb][nb][r] = -INFINITY;
       }
+      // The context takes no part here: its weight is 1 minus the others' sum, and joins at the end.  Where it has nearly all
+      // the weight, 1 - p would be lost in p's own rounding otherwise.
+      const uint32_t tile_row0 = (uint32_t)(t * TILE);
+      bool here = false;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) here = here || (uint32_t)kept_target[nb] - tile_row0 < (uint32_t)TILE;
+      if (__any(here)) {
+        rare();
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          const uint32_t at = (uint32_t)kept_target[nb] - tile_row0 - 4 * half;
+#pragma unroll
+          for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if (at == (uint32_t)(32 * jb + 8 * (r / 4) + r % 4)) z[jb][nb][r] = -INFINITY;
+        }
+      }
       bool moved = false;
       float keep[NB];
 #pragma unroll
@@ -495,7 +522,7 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
             const int64_t pair = pair0 + 8 * (r / 4) + r % 4;
             if (node < a.kept_rows && pair < a.streamed_rows)
               static_cast<float*>(a.out)[pair * a.kept_rows + node] =
-                  BIAS ? fmaf(z[jb][nb][r], a.scale2, kept_bias[nb]) : z[jb][nb][r] * a.scale2;
+                  !BIAS ? z[jb][nb][r] * a.scale2 : kept_bias[nb] == -INFINITY ? -INFINITY : fmaf(z[jb][nb][r], a.scale2, kept_bias[nb]);
           }
         }
       }
@@ -517,15 +544,17 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
       const int32_t wave_node0 = (int32_t)(kept_row0 - l32), t_of_lane = side_target[BUF][lane % TILE];
       if (__any(t_of_lane >= wave_node0 && t_of_lane - wave_node0 < 32 * NB)) {
         rare();
-        constexpr float one = E::kShift ? 16384.0f : 1.0f;
+        constexpr float one = (float)(1 << E::kShift);
 #pragma unroll
         for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const int32_t t_id = side_target[BUF][jb * 32 + 8 * (r / 4) + 4 * half + r % 4];
+            const int pair = jb * 32 + 8 * (r / 4) + 4 * half + r % 4;
+            const int32_t t_id = side_target[BUF][pair];
+            const float p = side_miss[BUF][pair] * -one;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
-              if (t_id == (int32_t)(kept_row0 + 32 * nb)) z[jb][nb][r] -= one;
+              if (t_id == (int32_t)(kept_row0 + 32 * nb)) z[jb][nb][r] = p;
           }
       }
     }
@@ -601,6 +630,8 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
           for (int q = 0; q < 4; ++q) {
             const int col = 32 * db + 8 * q + 4 * half;
             vec4 v = {out[db][nb][4 * q], out[db][nb][4 * q + 1], out[db][nb][4 * q + 2], out[db][nb][4 * q + 3]};
+            // a masked node has no gradient, whatever the pairs' rows hold
+            if (MODE == kTableGrad && BIAS && kept_bias[nb] == -INFINITY) v = (vec4)0.0f;
             if (MODE == kTableGrad && a.part_acc == nullptr) {
               if (col < a.dim) E::store4(static_cast<elem*>(a.out) + row * a.dim + col, v * a.out_scale);
             } else {
@@ -625,6 +656,7 @@ struct JoinArgs {
   const float* part_acc;
   float* loss;
   float* lse2;               // for the table gradient, to whole tiles: +infinity for a pair without gradient; or null
+  float* miss;               // .. 1 - p of its context
   int32_t* target;           // .. its context, or -1
   void* g_in;                // or null
 };
@@ -647,43 +679,9 @@ __global__ __launch_bounds__(kThreads) void join_pairs_kernel(JoinArgs a) {
   if (exists && (c < 0 || c >= a.num_in || t < -1 || t >= a.num_nodes)) t = -2;
   else if (t >= 0 && a.bias && a.bias[t] == -INFINITY) t = -3;
   const bool live = t >= 0;
-  // the splits' maxima and sums
-  float m = -INFINITY;
-  double sum = 0.0;
-  if (exists) {
-    for (int s = SLOTS > 1 ? member : 0; s < a.splits; s += SLOTS > 1 ? GROUP : 1) m = fmaxf(m, a.part_max[s * a.num_pairs + i]);
-    if constexpr (SLOTS > 1) {
-#pragma unroll
-      for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
-      if ((threadIdx.x & 63) == 0) part_m[threadIdx.x >> 6] = m;
-      __syncthreads();
-#pragma unroll
-      for (int w = 0; w < kThreads / 64; ++w) m = fmaxf(m, part_m[w]);
-    }
-    for (int s = SLOTS > 1 ? member : 0; s < a.splits; s += SLOTS > 1 ? GROUP : 1) {
-      const float pm = a.part_max[s * a.num_pairs + i];
-      const double ps = a.part_sum[s * a.num_pairs + i];
-      // a split of masked nodes alone has sum 0, whatever its maximum
-      sum += pm == -INFINITY && ps == 0.0 ? 0.0 : ps * exp2((double)pm - (double)m);
-    }
-    if constexpr (SLOTS > 1) {
-#pragma unroll
-      for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d, 64);
-      if ((threadIdx.x & 63) == 0) part_s[threadIdx.x >> 6] = sum;
-      __syncthreads();
-      sum = 0.0;
-#pragma unroll
-      for (int w = 0; w < kThreads / 64; ++w) sum += part_s[w];
-    }
-  }
-  const double total2 = (double)m + log2(sum) - (double)E::kForwardShift;  // base-2 log-sum
-  if (a.lse2 != nullptr && member == 0) {
-    a.lse2[i] = live ? (float)(total2 - (double)E::kShift) : INFINITY;
-    a.target[i] = live ? t : -1;
-  }
-  if (!exists) return;
+  // the context's row and score
   const bool column = 4 * quad < a.dim;        // the lanes beyond read nothing
-  vec4 to = (vec4)0.0f;                        // the context's row
+  vec4 to = (vec4)0.0f;
   double dot = 0.0;
   if (live && column) {
     const elem* h = static_cast<const elem*>(a.w_in) + c * a.dim + 4 * quad;
@@ -696,8 +694,50 @@ __global__ __launch_bounds__(kThreads) void join_pairs_kernel(JoinArgs a) {
   }
 #pragma unroll
   for (int d = QUADS / 2; d; d >>= 1) dot += __shfl_xor(dot, d, 64);
+  const double z2 = live ? ((double)a.scale * dot + (a.bias ? (double)a.bias[t] : 0.0)) * (1.0 / kLn2) : -INFINITY;    // base 2
+  // the splits' maxima and sums, of all nodes but the context; m: the largest of them and of z2
+  float m_others = -INFINITY;
+  double m = z2, others = 0.0;
+  if (exists) {
+    for (int s = SLOTS > 1 ? member : 0; s < a.splits; s += SLOTS > 1 ? GROUP : 1) m_others = fmaxf(m_others, a.part_max[s * a.num_pairs + i]);
+    if constexpr (SLOTS > 1) {
+#pragma unroll
+      for (int d = 32; d; d >>= 1) m_others = fmaxf(m_others, __shfl_xor(m_others, d, 64));
+      if ((threadIdx.x & 63) == 0) part_m[threadIdx.x >> 6] = m_others;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kThreads / 64; ++w) m_others = fmaxf(m_others, part_m[w]);
+    }
+    m = fmax(z2, (double)m_others);
+    for (int s = SLOTS > 1 ? member : 0; s < a.splits; s += SLOTS > 1 ? GROUP : 1) {
+      const float pm = a.part_max[s * a.num_pairs + i];
+      const double ps = a.part_sum[s * a.num_pairs + i];
+      // a split of masked nodes alone has sum 0, whatever its maximum
+      others += pm == -INFINITY && ps == 0.0 ? 0.0 : ps * exp2((double)pm - m);
+    }
+    if constexpr (SLOTS > 1) {
+#pragma unroll
+      for (int d = 32; d; d >>= 1) others += __shfl_xor(others, d, 64);
+      if ((threadIdx.x & 63) == 0) part_s[threadIdx.x >> 6] = others;
+      __syncthreads();
+      others = 0.0;
+#pragma unroll
+      for (int w = 0; w < kThreads / 64; ++w) others += part_s[w];
+    }
+  }
+  const double own = live ? exp2(z2 - m) * (double)(1 << E::kForwardShift) : 0.0;
+  const double sum = others + own;
+  const double total2 = m + log2(sum) - (double)E::kForwardShift;          // base-2 log-sum
+  const float miss = live ? (float)(others / sum) : 0.0f;
+  if (a.lse2 != nullptr && member == 0) {
+    a.lse2[i] = live ? (float)(total2 - (double)E::kShift) : INFINITY;
+    a.miss[i] = miss;
+    a.target[i] = live ? t : -1;
+  }
+  if (!exists) return;
   if (member == 0) {
-    double value = total2 * kLn2 - ((double)a.scale * dot + (live && a.bias ? (double)a.bias[t] : 0.0));
+    // a context that leads by far: its loss is of the others' size, not of the log-sum's rounding
+    double value = z2 >= (double)m_others ? log1p(others / own) : (total2 - z2) * kLn2;
     if (t == -1) value = 0.0;
     if (t == -2) value = NAN;
     if (t == -3) value = INFINITY;
@@ -711,7 +751,7 @@ __global__ __launch_bounds__(kThreads) void join_pairs_kernel(JoinArgs a) {
     for (int s = slot; s < a.splits; s += SLOTS) {
       const float pm = a.part_max[s * a.num_pairs + i];
       const bool empty = pm == -INFINITY && a.part_sum[s * a.num_pairs + i] == 0.0;           // masked nodes alone
-      const float w = empty ? 0.0f : (float)(exp2((double)pm - (double)m) * inverse);
+      const float w = empty ? 0.0f : (float)(exp2((double)pm - m) * inverse);
       g += w * *reinterpret_cast<const vec4*>(a.part_acc + (s * a.num_pairs + i) * a.padded + 4 * quad);
     }
   }
@@ -723,7 +763,7 @@ __global__ __launch_bounds__(kThreads) void join_pairs_kernel(JoinArgs a) {
     for (int k = 1; k < SLOTS; ++k) g += part_g[k * QUADS + quad];
   }
   if (!column) return;
-  if (live) g = (g - to) * a.out_scale;
+  if (live) g = (g - miss * to) * a.out_scale;
   E::store4(static_cast<elem*>(a.g_in) + i * a.dim + 4 * quad, g);
 }
 
@@ -805,6 +845,7 @@ SoftmaxPlan plan_softmax(void* ws, int64_t num_pairs, int64_t num_nodes, int32_t
     if (grad) p.rows = c.take<typename E::elem>((size_t)p.padded_pairs * p.padded);
     p.target = c.take<int32_t>(p.padded_pairs);
     p.lse2 = c.take<float>(p.padded_pairs);
+    p.miss = c.take<float>(p.padded_pairs);
     p.part_max = c.take<float>(part_rows);
     p.part_sum = c.take<double>(part_rows);
     p.part_acc = c.take<float>(acc_rows * p.padded);
@@ -857,6 +898,7 @@ static int32_t run_padded(const SoftmaxCall& q, const SoftmaxPlan& p, hipStream_
   a.part_max = p.part_max;
   a.part_sum = p.part_sum;
   a.part_acc = p.part_acc;
+  a.target = q.contexts;
   int32_t rc = q.g_in ? launch_stream<E, DP, kForward>(a, stream) : launch_stream<E, DP, kLossOnly>(a, stream);
   if (rc != GS_OK) return rc;
   const float out_scale = q.scale * q.grad_scale;
@@ -880,6 +922,7 @@ static int32_t run_padded(const SoftmaxCall& q, const SoftmaxPlan& p, hipStream_
   j.part_acc = p.part_acc;
   j.loss = q.loss;
   j.lse2 = q.g_out ? p.lse2 : nullptr;
+  j.miss = p.miss;
   j.target = p.target;
   j.g_in = q.g_in;
   constexpr int quads = DP <= 64 ? 16 : DP <= 128 ? 32 : 64;
@@ -889,13 +932,14 @@ static int32_t run_padded(const SoftmaxCall& q, const SoftmaxPlan& p, hipStream_
   if (!q.g_out) return GS_OK;
   elem* rows = static_cast<elem*>(p.rows);
   gather_pairs_kernel<E><<<blocks_for(p.padded_pairs * (DP / (16 / (int)sizeof(elem)))), kThreads, 0, stream>>>(
-      static_cast<const elem*>(q.w_in), q.num_in, q.dim, DP, q.centers, q.num_pairs, p.padded_pairs, rows);
+      static_cast<const elem*>(q.w_in), q.dim, DP, q.centers, p.target, p.padded_pairs, rows);
   GS_LAUNCH_CHECK();
   a.kept = q.w_out;
   a.streamed = rows;
   a.kept_rows = q.num_nodes;
   a.streamed_rows = q.num_pairs;
   a.lse2 = p.lse2;
+  a.miss = p.miss;
   a.target = p.target;
   a.kept_tiles = p.node_tiles;
   a.splits = p.node_splits;

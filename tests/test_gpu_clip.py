@@ -147,3 +147,15 @@ def test_graph_replays(gs):
         want = norm_of(grads)
         assert abs(norm.item() - want) <= 1e-14 * want
         check_scaled(outs, grads, min(1.0, 2.0 / want))
+
+
+@pytest.mark.parametrize("fmt", ["f32", "bf16"])
+def test_a_factor_below_the_least_float(gs, fmt):
+    """A norm of 1e40 clipped to 1e-4: the factor, 1e-44, is a float of three bits; the results, 1e-8, are ordinary."""
+    was = torch.full((10_000,), 1e38).to(DTYPES[fmt])
+    was[::2] *= -0.37
+    grads = [was.to(DEV)]
+    norm = norm_of(grads)
+    got = gs.gs_clip_grads(grads, 1e-4).item()
+    assert abs(got - norm) <= 1e-14 * norm
+    check_scaled(grads, [was], 1e-4 / norm)

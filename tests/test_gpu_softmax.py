@@ -294,3 +294,77 @@ def test_every_padding_of_a_row(gs, fmt, dim):
     got = gs.gs_scores(w_in.to(DEV), w_out.to(DEV), c.to(DEV)).cpu().double()
     h, w = w_in.double()[c.long()], w_out.double()
     assert torch.all((got - h @ w.T).abs() <= (dim + 4) * V * (h.abs() @ w.abs().T) + 4 * V * (h @ w.T).abs())
+
+
+@pytest.mark.parametrize("fmt", ["f32", "bf16", "f16"])
+def test_pairs_without_gradient_spoil_nothing(gs, fmt):
+    """Centre rows of NaN and infinity whose pair is left out, or has a masked context, move no row of g_out."""
+    w_in, w_out, _, t = make(90, 300, 64, fmt, rows=90)
+    c = torch.arange(90, dtype=torch.int32)
+    bias = torch.zeros(300)
+    bias[11] = -math.inf
+    t = torch.where(t == 11, t + 1, t)
+    t[5], t[40], t[41] = -1, -1, 11
+    d = [x.to(DEV) for x in (w_in, w_out, c, t)]
+    clean = gs.gs_softmax_loss(*d, bias=bias.to(DEV))
+    w_in[5], w_in[40], w_in[41] = math.nan, math.inf, math.nan
+    got = gs.gs_softmax_loss(w_in.to(DEV), *d[1:], bias=bias.to(DEV))
+    assert all(torch.equal(a, b) for a, b in zip(got, clean))
+
+
+@pytest.mark.parametrize("fmt", ["f32", "bf16"])
+def test_masked_nodes_stay_masked_beside_rows_that_hold_nan(gs, fmt):
+    w_in, w_out, c, t = make(40, 90, 64, fmt, rows=40)
+    c = torch.arange(40, dtype=torch.int32)
+    bias = torch.zeros(90)
+    bias[::3] = -math.inf
+    t = torch.where(t % 3 == 0, t + 1, t)
+    w_in[7], w_in[8, 3], c[9] = math.nan, math.inf, 40
+    d = [x.to(DEV) for x in (w_in, w_out, c, t)]
+    _, _, go = gs.gs_softmax_loss(*d, bias=bias.to(DEV))
+    assert torch.all(go[::3] == 0) and torch.isnan(go[1::3]).any()
+    z = gs.gs_scores(*d[:3], bias=bias.to(DEV))
+    assert torch.all(z[:, ::3] == -math.inf) and torch.isnan(z[[7, 9]][:, 1::3]).all()
+
+
+@pytest.mark.parametrize("fmt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n,nodes,dim", [(1, 900, 64), (70, 300, 64), (300, 2000, 128), (40, 1000, 256)])
+def test_pairs_that_are_nearly_certain(gs, fmt, n, nodes, dim):
+    """A context that leads by 5 to 60: loss and gradients keep the size of what the other nodes weigh.  1 - p enters unrounded
+    (but for 2^-24 of itself), so every bound of the file's head holds with |p - 1| in the place of p + 1, and the loss, the
+    logarithm of one plus the others' sum over the context's weight, moves by 1 - p times what the scores do.  binary16: other
+    probabilities below its normal numbers, scaled by 2^11 at least under their row's largest (2^14 under 1 for the table),
+    are off by half its least step, 2^-25."""
+    w_in, w_out, c, t = make(n, nodes, dim, fmt, rows=n, spread=1.0)
+    c = torch.arange(n, dtype=torch.int32)
+    lead = torch.linspace(5.0, 60.0, n)
+    rows = w_out[t.long()].float()
+    w_in = (rows * (lead / rows.square().sum(1))[:, None]).to(DTYPES[fmt])
+    f = 0.5
+    loss, g_in, g_out, *_, dz = reference(w_in, w_out, c, t, grad_scale=f)
+    h, w = w_in.double(), w_out.double()
+    z = h @ w.T
+    at = t.long()[:, None]
+    others = torch.softmax(z, 1).scatter(1, at, 0.0)
+    miss = others.sum(1)
+    apart = z.scatter(1, at, -math.inf)
+    loss = torch.log1p((apart - z.gather(1, at)).exp().sum(1))          # not as a difference of large numbers
+    hot = torch.zeros_like(others).scatter_(1, at, 1.0)
+    coef, size = others - hot * miss[:, None], others + hot * miss[:, None]
+    g_in, g_out = f * coef @ w, f * coef.T @ h
+    got, gi, go = (x.cpu() for x in gs.gs_softmax_loss(*(x.to(DEV) for x in (w_in, w_out, c, t)), grad_scale=f))
+    r = 2 * dz + 100 * V
+    assert torch.all((got.double() - loss).abs() <= miss * r + 4 * V * loss + 2.0 ** -126), float((got.double() - loss).abs().max())
+    alone = gs.gs_softmax_loss(*(x.to(DEV) for x in (w_in, w_out, c, t)), want_grad=False)[0].cpu()
+    assert torch.all((alone.double() - loss).abs() <= miss * r + 4 * V * loss + 2.0 ** -126)
+    u = torch.finfo(DTYPES[fmt]).eps / 2
+    r += u if fmt != "f32" else 0.0
+    least = 2.0 ** -25 if fmt == "f16" else 0.0
+    lost = 2.0 ** -126
+    low_in = least * 2.0 ** -11 * f * others.amax(1, keepdim=True) * w.abs().sum(0)
+    low_out = least * 2.0 ** -14 * f * h.abs().sum(0)
+    for have, want, terms, absolute, low in ((gi, g_in, nodes, f * size @ w.abs(), low_in + lost * (1 + w.abs().sum(0))),
+                                             (go, g_out, n, f * size.T @ h.abs(), low_out + lost * (1 + h.abs().sum(0)))):
+        bound = (r + terms * V + 4 * V) * absolute + low
+        bound = bound + u * (want.abs() + bound) + least
+        assert torch.all((have.double() - want).abs() <= bound), float(((have.double() - want).abs() - bound).max())
