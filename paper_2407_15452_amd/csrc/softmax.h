@@ -252,9 +252,9 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
   constexpr bool NODES_STREAMED = MODE == kLossOnly || MODE == kForward;
   constexpr bool SECOND = MODE == kForward || MODE == kTableGrad;
   __shared__ __attribute__((aligned(1024))) char tile[2][TILE * ROWB];
-  __shared__ float side[2][TILE];              // nodes streamed: bias * log2(e); pairs streamed: base-2 log-sums
-  __shared__ float side_miss[2][TILE];         // pairs streamed
-  __shared__ int32_t side_target[2][TILE];
+  __shared__ __attribute__((aligned(16))) float side[2][TILE];              // nodes streamed: bias * log2(e); pairs streamed: base-2 log-sums
+  __shared__ __attribute__((aligned(16))) float side_miss[2][TILE];         // pairs streamed
+  __shared__ __attribute__((aligned(16))) int32_t side_target[2][TILE];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, l32 = lane & 31;
   // workgroups of one split stream the same rows: they share an XCD (consecutive workgroups go round the eight of them)
@@ -548,13 +548,23 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
 #pragma unroll
         for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int pair = jb * 32 + 8 * (r / 4) + 4 * half + r % 4;
-            const int32_t t_id = side_target[BUF][pair];
-            const float p = side_miss[BUF][pair] * -one;
+          for (int q = 0; q < 4; ++q) {
+            const int pair = jb * 32 + 8 * q + 4 * half;
+            const int4 ids = *reinterpret_cast<const int4*>(&side_target[BUF][pair]);
+            const int32_t id[4] = {ids.x, ids.y, ids.z, ids.w};
+            bool hit = false;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
-              if (t_id == (int32_t)(kept_row0 + 32 * nb)) z[jb][nb][r] = p;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) hit = hit || id[e] == (int32_t)(kept_row0 + 32 * nb);
+            if (!__any(hit)) continue;
+            rare();
+            const vec4 p = *reinterpret_cast<const vec4*>(&side_miss[BUF][pair]) * -one;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (id[e] == (int32_t)(kept_row0 + 32 * nb)) z[jb][nb][4 * q + e] = p[e];
           }
       }
     }
