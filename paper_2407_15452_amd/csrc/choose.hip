@@ -82,15 +82,35 @@ struct RowLimits {
   }
 };
 
+// exp((s - top) / temperature) as 2^(n / 64) 2^r, r within 1/128: a table of 64 powers in LDS and the series of 2^r to r^5
+// (the next term is below 2^-54).  Half the instructions of exp(), which would bound the passes that weigh every score: about
+// 2^-51 (1 + |exponent|) of relative error, most of it the exponent's own rounding, as with exp().
+constexpr int kPowers = 64;
 struct Weigh {
-  float top;
-  double inverse;                              // of the temperature
+  double top, rate;                            // log2(e) / temperature
+  const double* powers;                        // 2^(j / 64)
+  __device__ __forceinline__ Weigh(float top_, float temperature, const double* powers_)
+      : top((double)top_), rate(fmax(1.4426950408889634074 / (double)temperature, 0x1p-900)), powers(powers_) {}
   __device__ __forceinline__ double operator()(float s) const {     // without branches: they would split every wave
-    const double d = (double)s - (double)top;                      // infinities: NaN for the greatest, -infinity for the others
-    const double e = exp(d * inverse);
-    return s == top ? 1.0 : d == -INFINITY ? 0.0 : e;
+    // infinities: NaN for the greatest, which fmin takes to 0, -infinity for the others
+    const double y = fmax(fmin(((double)s - top) * rate, 0.0), -2000.0);
+    const double t = fma(y, (double)kPowers, 0x1.8p52);              // its last bits: the nearest whole number
+    const double r = fma(t - 0x1.8p52, -1.0 / kPowers, y);
+    const int n = __double2loint(t);
+    const double power = powers[n & (kPowers - 1)];
+    constexpr double l = 0.69314718055994530942, l2 = l * l, l3 = l2 * l, l4 = l2 * l2, l5 = l4 * l;
+    double q = fma(r, l5 / 120, l4 / 24);
+    q = fma(r, q, l3 / 6);
+    q = fma(r, q, l2 / 2);
+    q = fma(r, q, l) * r;
+    return ldexp(fma(power, q, power), n >> 6);
   }
 };
+// by the first wave; a barrier follows before the first use
+__device__ __forceinline__ void fill_powers(double* powers) {
+  static_assert(kPowers == 64, "one per lane");
+  if (threadIdx.x < kPowers) powers[threadIdx.x] = exp2((double)threadIdx.x / kPowers);
+}
 
 // A sum of weights as integers: hi * 2^31 + lo, in units of 2^-62.
 struct Sum {
@@ -105,7 +125,14 @@ struct Sum {
 };
 __device__ __forceinline__ Sum operator+(const Sum& a, const Sum& b) { return Sum{a.count + b.count, a.hi + b.hi, a.lo + b.lo}; }
 __device__ __forceinline__ Sum operator-(const Sum& a, const Sum& b) { return Sum{a.count - b.count, a.hi - b.hi, a.lo - b.lo}; }
-__device__ __forceinline__ uint64_t units_of(double weight) { return (uint64_t)(weight * 0x1p62); }
+struct Units {
+  uint32_t hi, lo;
+};
+__device__ __forceinline__ Units units_of(double weight) {            // 1 at most; every step is exact
+  const double t = weight * 0x1p31;
+  const uint32_t hi = (uint32_t)t;
+  return Units{hi, (uint32_t)((t - (double)hi) * 0x1p31)};
+}
 
 struct Histogram {
   uint32_t count[kBins];
@@ -114,10 +141,10 @@ struct Histogram {
 __device__ __forceinline__ void add_to(Histogram& h, int b, bool weights, double weight) {
   atomicAdd(&h.count[b], 1u);
   if (!weights) return;
-  const uint64_t w = units_of(weight);
-  if (w == 0) return;
-  atomicAdd(&h.hi[b], (unsigned long long)(w >> 31));
-  atomicAdd(&h.lo[b], (unsigned long long)(w & 0x7fffffffu));
+  const Units w = units_of(weight);
+  if ((w.hi | w.lo) == 0) return;
+  atomicAdd(&h.hi[b], (unsigned long long)w.hi);
+  atomicAdd(&h.lo[b], (unsigned long long)w.lo);
 }
 
 // 2048 equal steps between the row's least and greatest finite score.  fp32: every operation is monotone, which is all that a
@@ -161,6 +188,7 @@ struct ListShared {
   uint64_t list[kListMost];                    // ~key in the high half, index in the low one: sorts by the order of the nodes
 };
 struct Shared : ListShared {
+  double powers[kPowers];
   Histogram hist;
   Sum wave_sum[kWaves];
   Sum found_above, found_in;
@@ -215,6 +243,18 @@ __device__ __forceinline__ void for_row(const Row<V>& row, uint32_t from, uint32
 #pragma unroll
       for (uint32_t k = 0; k < per; ++k)
         if (s[e][k] > -INFINITY) visit((p0 + e * threads) * per + k - row.skew, s[e][k]);
+  }
+}
+
+// The same a piece at a time, left-out elements too: visit(index of the first, scores).  What it computes for all of them before
+// it branches for one runs side by side.
+template <typename V, typename Visit>
+__device__ __forceinline__ void for_pieces(const Row<V>& row, uint32_t from, uint32_t to, uint32_t lane, uint32_t threads, Visit visit) {
+  constexpr uint32_t per = Row<V>::kPer;
+  for (uint32_t p = from + lane; p < to; p += threads) {
+    float s[per];
+    row.load(p, s);
+    visit(p * per - row.skew, s);
   }
 }
 
@@ -573,8 +613,8 @@ __device__ __forceinline__ uint32_t place_in_list(Shared& sh, uint32_t to, const
   const uint32_t per = (to + kThreads - 1) / kThreads, from = threadIdx.x * per, end = min(from + per, to);
   Sum own{0, 0, 0};
   for (uint32_t p = from; p < end; ++p) {
-    const uint64_t w = units_of(weight(sh.list[p]));
-    own = own + Sum{1, w >> 31, w & 0x7fffffffu};
+    const Units w = units_of(weight(sh.list[p]));
+    own = own + Sum{1, w.hi, w.lo};
   }
   Sum before;
   block_sums(sh, own, true, before, total);
@@ -582,8 +622,8 @@ __device__ __forceinline__ uint32_t place_in_list(Shared& sh, uint32_t to, const
   const auto reached = make_reached(total);
   if (own.count != 0 && reached(before + own) && !reached(before)) {               // one lane
     for (uint32_t p = from; p < end; ++p) {
-      const uint64_t w = units_of(weight(sh.list[p]));
-      const Sum in{1, w >> 31, w & 0x7fffffffu};
+      const Units w = units_of(weight(sh.list[p]));
+      const Sum in{1, w.hi, w.lo};
       before = before + in;
       if (reached(before)) {
         sh.found_bin = (int)p;
@@ -680,7 +720,22 @@ __device__ __forceinline__ Extreme extreme_of(const Row<V>& row, uint32_t from, 
 template <typename V>
 __device__ __forceinline__ void first_histogram(Histogram& hist, const Row<V>& row, uint32_t from, uint32_t to, const Steps& steps, bool weights, const Weigh& weigh) {
   if (weights)
-    for_row<1>(row, from, to, threadIdx.x, kThreads, [&](uint32_t, float s) { add_to(hist, steps(s), true, weigh(s)); });
+    for_pieces(row, from, to, threadIdx.x, kThreads, [&](uint32_t, const float* s) {
+      int bin[Row<V>::kPer];
+      Units w[Row<V>::kPer];
+#pragma unroll
+      for (uint32_t k = 0; k < Row<V>::kPer; ++k) {
+        bin[k] = steps(s[k]);
+        w[k] = units_of(weigh(s[k]));
+      }
+#pragma unroll
+      for (uint32_t k = 0; k < Row<V>::kPer; ++k)
+        if (s[k] > -INFINITY) {
+          atomicAdd(&hist.count[bin[k]], 1u);
+          atomicAdd(&hist.hi[bin[k]], (unsigned long long)w[k].hi);
+          atomicAdd(&hist.lo[bin[k]], (unsigned long long)w[k].lo);
+        }
+    });
   else
     for_row<kAhead>(row, from, to, threadIdx.x, kThreads, [&](uint32_t, float s) { atomicAdd(&hist.count[steps(s)], 1u); });
 }
@@ -692,9 +747,10 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
   const int64_t r = blockIdx.x;
   const Row<V> row(a.scores, r, a.n);
   const RowLimits limits(a, r);
+  fill_powers(sh.powers);
   const Extreme x = extreme_of(row, 0, row.pieces());
   if (answer_without_weights(x.kmax, x.first, limits, a, r)) return;
-  const Weigh weigh{score_of(x.kmax), 1.0 / (double)limits.temperature};
+  const Weigh weigh(score_of(x.kmax), limits.temperature, sh.powers);
   Cut cut{0, row.n};                           // every valid key lies above 0
   if (limits.by_k || limits.by_p) {
     clear_histogram(sh, true);
@@ -770,12 +826,14 @@ __global__ __launch_bounds__(kThreads) void extremes_kernel(SplitArgs a) {
 template <typename V>
 __global__ __launch_bounds__(kThreads) void first_histogram_kernel(SplitArgs a) {
   __shared__ Histogram hist;
+  __shared__ double powers[kPowers];
   const int64_t r = blockIdx.x / a.groups;
   const int g = (int)(blockIdx.x % a.groups);
   const RowLimits limits(a.s, r);
   const Extreme x = row_extreme(a, r);
   if (x.kmax == 0 || !(limits.temperature > 0.0f) || !(limits.by_k || limits.by_p)) return;
   const bool weights = !limits.by_k;
+  fill_powers(powers);
   for (int b = threadIdx.x; b < kBins; b += kThreads) {
     hist.count[b] = 0;
     hist.hi[b] = 0;
@@ -785,7 +843,7 @@ __global__ __launch_bounds__(kThreads) void first_histogram_kernel(SplitArgs a) 
   const Row<V> row(a.s.scores, r, a.s.n);
   uint32_t from, to;
   group_pieces(a, row, g, from, to);
-  first_histogram(hist, row, from, to, Steps(x.kmin, x.kmax), weights, Weigh{score_of(x.kmax), 1.0 / (double)limits.temperature});
+  first_histogram(hist, row, from, to, Steps(x.kmin, x.kmax), weights, Weigh(score_of(x.kmax), limits.temperature, powers));
   __syncthreads();
   Histogram& sum = a.first_hist[r];
   for (int b = threadIdx.x; b < kBins; b += kThreads) {
@@ -821,6 +879,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(SplitArgs a) {
 template <typename V>
 __global__ __launch_bounds__(kThreads) void collect_kernel(SplitArgs a) {
   __shared__ ListShared sh;
+  __shared__ double powers[kPowers];
   const int64_t r = blockIdx.x / a.groups;
   const int g = (int)(blockIdx.x % a.groups);
   const RowLimits limits(a.s, r);
@@ -828,6 +887,7 @@ __global__ __launch_bounds__(kThreads) void collect_kernel(SplitArgs a) {
   if (x.kmax == 0 || !(limits.temperature > 0.0f)) return;
   const Plan& plan = a.plans[r];
   if (plan.long_way) return;
+  fill_powers(powers);
   if (threadIdx.x == 0) sh.list_count = 0;
   __syncthreads();
   const float list_lo = score_of(plan.lo), list_hi = score_of(plan.hi);
@@ -840,22 +900,23 @@ __global__ __launch_bounds__(kThreads) void collect_kernel(SplitArgs a) {
     group_pieces(a, row, g, from, to);
     for_row<kAhead>(row, from, to, threadIdx.x, kThreads, to_list);
   } else {
-    const Weigh weigh{score_of(x.kmax), 1.0 / (double)limits.temperature};
+    const Weigh weigh(score_of(x.kmax), limits.temperature, powers);
     const float floor = plan.listed ? list_hi : -INFINITY;
     const uint32_t last = min(a.parts, (g + 1) * a.parts_per_group);
     const uint32_t span = a.width / Row<V>::kPer;
     for (uint32_t part = g * a.parts_per_group + (threadIdx.x >> 6); part < last; part += kWaves) {
       uint64_t hi = 0, lo = 0;
-      for_row<1>(row, min(part * span, row.pieces()), min((part + 1) * span, row.pieces()), threadIdx.x & 63, 64, [&](uint32_t at, float s) {
-        if (s <= floor) {
-          to_list(at, s);
-          return;
+      for_pieces(row, min(part * span, row.pieces()), min((part + 1) * span, row.pieces()), threadIdx.x & 63, 64, [&](uint32_t at, const float* s) {
+#pragma unroll
+        for (uint32_t k = 0; k < Row<V>::kPer; ++k) {
+          const double w = weigh(s[k]);
+          const Units units = units_of(w);
+          const bool kept = s[k] > floor && !(limits.min_p > 0.0 && w < limits.min_p);
+          hi += kept ? units.hi : 0;
+          lo += kept ? units.lo : 0;
         }
-        const double w = weigh(s);
-        if (limits.min_p > 0.0 && !(w >= limits.min_p)) return;
-        const uint64_t units = units_of(w);
-        hi += units >> 31;
-        lo += units & 0x7fffffffu;
+#pragma unroll
+        for (uint32_t k = 0; k < Row<V>::kPer; ++k) to_list(at + k, s[k]);
       });
 #pragma unroll
       for (int d = 32; d; d >>= 1) {
@@ -884,7 +945,9 @@ __global__ __launch_bounds__(kThreads) void finish_rows_kernel(SplitArgs a) {
   const RowLimits limits(a.s, r);
   const Extreme x = row_extreme(a, r);
   if (answer_without_weights(x.kmax, x.first, limits, a.s, r)) return;
-  const Weigh weigh{score_of(x.kmax), 1.0 / (double)limits.temperature};
+  fill_powers(sh.powers);
+  __syncthreads();
+  const Weigh weigh(score_of(x.kmax), limits.temperature, sh.powers);
   const Row<V> row(a.s.scores, r, a.s.n);
   const Plan plan = a.plans[r];
   Cut cut{0, row.n};
