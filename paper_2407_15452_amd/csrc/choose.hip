@@ -31,6 +31,7 @@ constexpr int kAhead = 4;                      // 16-byte loads per lane in flig
 constexpr int kListMost = 2 * kBins;           // elements of a row that may go to its list: room for two values of a 16-bit
                                                // format, which a step may hold, in rows of a million nodes
 constexpr int kSplitGroups = 2048;             // of one launch: eight per compute unit
+constexpr int kPartLeast = 2048;                // scores per part at least: what one histogram along the index takes
 constexpr int kSplitLeast = 8192;              // scores per workgroup at least
 
 struct SampleArgs {
@@ -210,52 +211,64 @@ struct Row {
     n = (uint32_t)n_;
   }
   __device__ __forceinline__ uint32_t pieces() const { return (n + skew + kPer - 1) / kPer; }
-  __device__ __forceinline__ void load(uint32_t piece, float* s) const {             // -infinity beyond the row
-    const uint32_t at = piece * kPer;
+  __device__ __forceinline__ bool inside(uint32_t piece) const { return (piece > 0 || skew == 0) && piece < (n + skew) / kPer; }
+  __device__ __forceinline__ void unpack(const uint4& w, float* s) const {
     elem e[kPer];
-    if (at >= skew && at + kPer <= n + skew) {
-      const uint4 w = *reinterpret_cast<const uint4*>(base + at);
-      __builtin_memcpy(e, &w, 16);
+    __builtin_memcpy(e, &w, 16);
 #pragma unroll
-      for (uint32_t k = 0; k < kPer; ++k) s[k] = V::get(e[k]);
+    for (uint32_t k = 0; k < kPer; ++k) s[k] = V::get(e[k]);
+  }
+  __device__ __forceinline__ void load(uint32_t piece, bool wanted, float* s) const {     // -infinity if it is not wanted
+    if (wanted && inside(piece)) {
+      unpack(reinterpret_cast<const uint4*>(base)[piece], s);
+    } else if (wanted) {
+      load_edge(piece, s);
     } else {
 #pragma unroll
-      for (uint32_t k = 0; k < kPer; ++k) s[k] = at + k >= skew && at + k < n + skew ? V::get(base[at + k]) : -INFINITY;
+      for (uint32_t k = 0; k < kPer; ++k) s[k] = -INFINITY;
     }
+  }
+  __device__ __forceinline__ void load_edge(uint32_t piece, float* s) const {        // -infinity beyond the row
+    const uint32_t at = piece * kPer;
+#pragma unroll
+    for (uint32_t k = 0; k < kPer; ++k) s[k] = at + k >= skew && at + k < n + skew ? V::get(base[at + k]) : -INFINITY;
   }
 };
-// visit(index, score) for the elements of the pieces from .. to that are not left out, by `threads` lanes of which this is
-// number `lane`
+// visit(index of the first, scores) for the pieces from .. to, left-out elements too, by `threads` lanes of which this is number
+// `lane`.  Pieces at the row's ends are a lane's of their own: a branch to them inside the loop would make every load wait for
+// the one before.  What a visit computes for all elements before it branches for one runs side by side.
 template <int AHEAD, typename V, typename Visit>
-__device__ __forceinline__ void for_row(const Row<V>& row, uint32_t from, uint32_t to, uint32_t lane, uint32_t threads, Visit visit) {
-  constexpr uint32_t per = Row<V>::kPer;
-  for (uint32_t p0 = from + lane; p0 < to; p0 += AHEAD * threads) {
-    float s[AHEAD][per];
-#pragma unroll
-    for (int e = 0; e < AHEAD; ++e) {
-      if (p0 + e * threads < to) row.load(p0 + e * threads, s[e]);
-      else
-#pragma unroll
-        for (uint32_t k = 0; k < per; ++k) s[e][k] = -INFINITY;
-    }
-#pragma unroll
-    for (int e = 0; e < AHEAD; ++e)
-#pragma unroll
-      for (uint32_t k = 0; k < per; ++k)
-        if (s[e][k] > -INFINITY) visit((p0 + e * threads) * per + k - row.skew, s[e][k]);
-  }
-}
-
-// The same a piece at a time, left-out elements too: visit(index of the first, scores).  What it computes for all of them before
-// it branches for one runs side by side.
-template <typename V, typename Visit>
 __device__ __forceinline__ void for_pieces(const Row<V>& row, uint32_t from, uint32_t to, uint32_t lane, uint32_t threads, Visit visit) {
   constexpr uint32_t per = Row<V>::kPer;
-  for (uint32_t p = from + lane; p < to; p += threads) {
-    float s[per];
-    row.load(p, s);
-    visit(p * per - row.skew, s);
+  const uint32_t first = max(from, row.skew ? 1u : 0u), last = min(to, (row.n + row.skew) / per);
+  const uint4* pieces = reinterpret_cast<const uint4*>(row.base);
+  for (uint32_t p0 = first + lane; p0 < last; p0 += AHEAD * threads) {
+    uint4 w[AHEAD];
+#pragma unroll
+    for (int e = 0; e < AHEAD; ++e) w[e] = pieces[min(p0 + e * threads, last - 1)];
+#pragma unroll
+    for (int e = 0; e < AHEAD; ++e) {
+      if (e > 0 && p0 + e * threads >= last) break;
+      float s[per];
+      row.unpack(w[e], s);
+      visit((p0 + e * threads) * per - row.skew, s);
+    }
   }
+  const uint32_t edge = lane == 0 ? 0 : row.pieces() - 1;
+  if (lane < 2 && (lane == 0 || edge > 0) && edge >= from && edge < to && !row.inside(edge)) {
+    float s[per];
+    row.load_edge(edge, s);
+    visit(edge * per - row.skew, s);
+  }
+}
+// visit(index, score) for those that are not left out
+template <int AHEAD, typename V, typename Visit>
+__device__ __forceinline__ void for_row(const Row<V>& row, uint32_t from, uint32_t to, uint32_t lane, uint32_t threads, Visit visit) {
+  for_pieces<AHEAD>(row, from, to, lane, threads, [&](uint32_t at, const float* s) {
+#pragma unroll
+    for (uint32_t k = 0; k < Row<V>::kPer; ++k)
+      if (s[k] > -INFINITY) visit(at + k, s[k]);
+  });
 }
 
 // Inclusive sums over the lanes of a wave, by moves inside and between the rows of 16 lanes (an add each, where a shuffle goes
@@ -686,7 +699,7 @@ __device__ __forceinline__ bool answer_without_weights(uint32_t kmax, uint32_t f
   return true;
 }
 
-// ---- least and greatest key, and the first index of the greatest
+// ---- least and greatest key, and the first index of the greatest (temperature 0)
 struct Extreme {
   uint32_t kmin, kmax, first, unused;
   __device__ __forceinline__ void with(uint32_t lo, uint32_t hi, uint32_t at) {
@@ -701,18 +714,32 @@ struct Extreme {
     for (int d = 32; d; d >>= 1) with(__shfl_xor(kmin, d, 64), __shfl_xor(kmax, d, 64), __shfl_xor(first, d, 64));
   }
 };
+// of the pieces from .. to, the same in every lane; the index only where it is asked for, by a second pass
 template <typename V>
-__device__ __forceinline__ Extreme extreme_of(const Row<V>& row, uint32_t from, uint32_t to) {           // the same in every lane
-  __shared__ Extreme wave_x[kWaves];
-  Extreme x{0xffffffffu, 0, 0xffffffffu, 0};
-  for_row<kAhead>(row, from, to, threadIdx.x, kThreads, [&](uint32_t at, float s) {
-    const uint32_t key = key_of(s);
-    x.with(key, key, at);
+__device__ __forceinline__ Extreme extreme_of(const Row<V>& row, uint32_t from, uint32_t to, bool want_first) {
+  __shared__ Extreme wave_x[2][kWaves];
+  float least = INFINITY, most = -INFINITY;
+  for_pieces<kAhead>(row, from, to, threadIdx.x, kThreads, [&](uint32_t, const float* s) {
+#pragma unroll
+    for (uint32_t k = 0; k < Row<V>::kPer; ++k) {
+      most = fmaxf(most, s[k]);                // a NaN is neither
+      least = fminf(least, s[k] > -INFINITY ? s[k] : INFINITY);
+    }
   });
-  x.over_wave();
-  if ((threadIdx.x & 63) == 0) wave_x[threadIdx.x >> 6] = x;
-  __syncthreads();
-  for (int w = 0; w < kWaves; ++w) x.with(wave_x[w].kmin, wave_x[w].kmax, wave_x[w].first);
+  Extreme x{key_of(least), key_of(most), 0xffffffffu, 0};
+  auto over_group = [&](int which) {
+    x.over_wave();
+    if ((threadIdx.x & 63) == 0) wave_x[which][threadIdx.x >> 6] = x;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) x.with(wave_x[which][w].kmin, wave_x[which][w].kmax, wave_x[which][w].first);
+  };
+  over_group(0);
+  if (want_first) {
+    for_row<kAhead>(row, from, to, threadIdx.x, kThreads, [&](uint32_t at, float s) {
+      if (key_of(s) == x.kmax) x.first = min(x.first, at);
+    });
+    over_group(1);
+  }
   return x;
 }
 
@@ -720,7 +747,7 @@ __device__ __forceinline__ Extreme extreme_of(const Row<V>& row, uint32_t from, 
 template <typename V>
 __device__ __forceinline__ void first_histogram(Histogram& hist, const Row<V>& row, uint32_t from, uint32_t to, const Steps& steps, bool weights, const Weigh& weigh) {
   if (weights)
-    for_pieces(row, from, to, threadIdx.x, kThreads, [&](uint32_t, const float* s) {
+    for_pieces<1>(row, from, to, threadIdx.x, kThreads, [&](uint32_t, const float* s) {
       int bin[Row<V>::kPer];
       Units w[Row<V>::kPer];
 #pragma unroll
@@ -748,7 +775,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
   const Row<V> row(a.scores, r, a.n);
   const RowLimits limits(a, r);
   fill_powers(sh.powers);
-  const Extreme x = extreme_of(row, 0, row.pieces());
+  const Extreme x = extreme_of(row, 0, row.pieces(), limits.temperature == 0.0f);
   if (answer_without_weights(x.kmax, x.first, limits, a, r)) return;
   const Weigh weigh(score_of(x.kmax), limits.temperature, sh.powers);
   Cut cut{0, row.n};                           // every valid key lies above 0
@@ -779,7 +806,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
 struct SplitArgs {
   SampleArgs s;
   int32_t groups;                              // workgroups per row
-  uint32_t parts;                              // of the positions of a row, `width` each (a multiple of 512: a 16-byte piece per lane), at most kBins
+  uint32_t parts;                              // of the positions of a row, `width` each, at most kBins
   uint32_t width, parts_per_group;
   Extreme* extremes;                           // [rows][groups]
   Histogram* first_hist;                       // [rows]
@@ -818,7 +845,7 @@ __global__ __launch_bounds__(kThreads) void extremes_kernel(SplitArgs a) {
   const Row<V> row(a.s.scores, r, a.s.n);
   uint32_t from, to;
   group_pieces(a, row, g, from, to);
-  const Extreme x = extreme_of(row, from, to);
+  const Extreme x = extreme_of(row, from, to, RowLimits(a.s, r).temperature == 0.0f);
   if (threadIdx.x == 0) a.extremes[blockIdx.x] = x;
 }
 
@@ -875,11 +902,13 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(SplitArgs a) {
 }
 
 // third pass: the list, gathered in LDS and handed over with one atomic per workgroup, and the weights above it by parts of the
-// row, one wave a part
+// row, one wave a part.  Few scores lie above a cut (one in six of normal ones at temperature 1, top_p 0.85): a wave gathers them
+// in LDS and weighs 64 at a time.
 template <typename V>
 __global__ __launch_bounds__(kThreads) void collect_kernel(SplitArgs a) {
   __shared__ ListShared sh;
   __shared__ double powers[kPowers];
+  __shared__ float sh_above[kWaves][64 * (1 + Row<V>::kPer)];
   const int64_t r = blockIdx.x / a.groups;
   const int g = (int)(blockIdx.x % a.groups);
   const RowLimits limits(a.s, r);
@@ -904,26 +933,42 @@ __global__ __launch_bounds__(kThreads) void collect_kernel(SplitArgs a) {
     const float floor = plan.listed ? list_hi : -INFINITY;
     const uint32_t last = min(a.parts, (g + 1) * a.parts_per_group);
     const uint32_t span = a.width / Row<V>::kPer;
-    for (uint32_t part = g * a.parts_per_group + (threadIdx.x >> 6); part < last; part += kWaves) {
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float* above = sh_above[wave];
+    for (uint32_t part = g * a.parts_per_group + wave; part < last; part += kWaves) {
       uint64_t hi = 0, lo = 0;
-      for_pieces(row, min(part * span, row.pieces()), min((part + 1) * span, row.pieces()), threadIdx.x & 63, 64, [&](uint32_t at, const float* s) {
+      auto weigh_one = [&](float s, bool valid) {
+        const double w = weigh(s);
+        const Units units = units_of(w);
+        const bool kept = valid && !(limits.min_p > 0.0 && w < limits.min_p);
+        hi += kept ? units.hi : 0;
+        lo += kept ? units.lo : 0;
+      };
+      const uint32_t from = min(part * span, row.pieces()), to = min((part + 1) * span, row.pieces());
+      uint32_t waiting = 0;                    // the same in every lane
+      for (uint32_t p0 = from; p0 < to; p0 += 64) {
+        float s[Row<V>::kPer];
+        row.load(p0 + lane, p0 + lane < to, s);
 #pragma unroll
         for (uint32_t k = 0; k < Row<V>::kPer; ++k) {
-          const double w = weigh(s[k]);
-          const Units units = units_of(w);
-          const bool kept = s[k] > floor && !(limits.min_p > 0.0 && w < limits.min_p);
-          hi += kept ? units.hi : 0;
-          lo += kept ? units.lo : 0;
+          const uint64_t lanes = __ballot(s[k] > floor);
+          if (s[k] > floor) above[waiting + __builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0))] = s[k];
+          waiting += (uint32_t)__popcll(lanes);
         }
 #pragma unroll
-        for (uint32_t k = 0; k < Row<V>::kPer; ++k) to_list(at + k, s[k]);
-      });
-#pragma unroll
-      for (int d = 32; d; d >>= 1) {
-        hi += (uint64_t)__shfl_xor((unsigned long long)hi, d, 64);
-        lo += (uint64_t)__shfl_xor((unsigned long long)lo, d, 64);
+        for (uint32_t k = 0; k < Row<V>::kPer; ++k) to_list((p0 + lane) * Row<V>::kPer + k - row.skew, s[k]);
+        wave_fence();
+        while (waiting >= 64) {
+          waiting -= 64;
+          weigh_one(above[waiting + lane], true);
+        }
+        wave_fence();
       }
-      if ((threadIdx.x & 63) == 0) {
+      if (waiting > 0) weigh_one(above[min(lane, waiting - 1)], lane < waiting);
+      wave_fence();
+      hi = wave_sums(hi);
+      lo = wave_sums(lo);
+      if (lane == 63) {
         a.part_hi[r * kBins + part] = hi;
         a.part_lo[r * kBins + part] = lo;
       }
@@ -1000,7 +1045,7 @@ SplitArgs plan_split(void* ws, int64_t rows, int64_t n, size_t& bytes) {
   p.groups = split_groups(rows, n);
   Carver c(ws);
   if (p.groups > 1) {
-    p.width = (uint32_t)(ceil_div(ceil_div(n + 7, kBins), 512) * 512);    // 7: the farthest a row begins behind a boundary
+    p.width = (uint32_t)(ceil_div(ceil_div(n + 7, kBins), kPartLeast) * kPartLeast);    // 7: the farthest a row begins behind a boundary
     p.parts = (uint32_t)ceil_div(n + 7, p.width);
     p.parts_per_group = (uint32_t)ceil_div(p.parts, p.groups);
     p.extremes = c.take<Extreme>((size_t)rows * p.groups);
