@@ -30,9 +30,10 @@ constexpr int kBins = 2048;
 constexpr int kAhead = 4;                      // 16-byte loads per lane in flight
 constexpr int kListMost = 2 * kBins;           // elements of a row that may go to its list: room for two values of a 16-bit
                                                // format, which a step may hold, in rows of a million nodes
-constexpr int kSplitGroups = 2048;             // of one launch: eight per compute unit
+constexpr int kSplitGroups = 2048;             // of one launch: eight per compute unit, where each has kSplitMany scores at least;
+constexpr int kSplitMany = 24576;              // half as many where not: a workgroup's histogram costs 40 KB of LDS and its sums
 constexpr int kPartLeast = 2048;                // scores per part at least: what one histogram along the index takes
-constexpr int kSplitLeast = 8192;              // scores per workgroup at least
+constexpr int kSplitLeast = 8192;              // scores per workgroup at least, of few rows
 
 struct SampleArgs {
   const void* scores;
@@ -1037,7 +1038,9 @@ __global__ __launch_bounds__(kThreads) void finish_rows_kernel(SplitArgs a) {
 // Split where a workgroup per row would leave compute units idle and rows are long enough for several.
 int32_t split_groups(int64_t rows, int64_t n) {
   if (rows >= 512 || n < 2 * kSplitLeast) return 1;
-  return (int32_t)std::max<int64_t>(1, std::min<int64_t>(kSplitGroups / rows, ceil_div(n, kSplitLeast)));
+  const int64_t many = std::min<int64_t>(kSplitGroups / rows, ceil_div(n, kSplitMany));
+  const int64_t few = std::min<int64_t>(kSplitGroups / 2 / rows, ceil_div(n, kSplitLeast));
+  return (int32_t)std::max<int64_t>(1, std::max(many, few));
 }
 
 SplitArgs plan_split(void* ws, int64_t rows, int64_t n, size_t& bytes) {
