@@ -188,6 +188,13 @@ __device__ __forceinline__ void wait_loads_and_barrier() {
   __syncthreads();
 }
 
+// what was asked of LDS is there; loads and stores may be under way
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // in a branch that few tiles take: keeps the compiler from doing its work for all of them and selecting
 __device__ __forceinline__ void rare() { asm volatile(""); }
 
@@ -291,6 +298,7 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
       kept_bias[nb] = live ? a.bias[row] * (MODE == kScores ? 1.0f : kLog2e) : -INFINITY;
       live = kept_bias[nb] != -INFINITY;
     }
+    if constexpr (MODE == kScores) continue;   // through LDS, below
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       const int at = (2 * ks + half) * S::kPerPiece;
@@ -314,6 +322,16 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
       }
     }
   };
+  int32_t row_center[S::kLoads];               // scores: the centres of those rows
+  auto fetch_centers = [&](int64_t t) {
+    if constexpr (MODE == kScores) {
+#pragma unroll
+      for (int n = 0; n < S::kLoads; ++n) {
+        const int64_t row = t * TILE + slot_row(n);
+        row_center[n] = has_chunk(n) && row < a.streamed_rows ? a.centers[row] : -1;
+      }
+    }
+  };
   constexpr int OUTSIDE = 1 << 30;
   const int streamed_bytes = (MODE == kTableGrad ? DP : a.dim) * (int)sizeof(elem);
   int place[S::kLoads];                        // in the tile's range
@@ -329,8 +347,7 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
 #pragma unroll
       for (int n = 0; n < S::kLoads; ++n) {
         if (!has_chunk(n)) continue;
-        const int64_t row = t * TILE + slot_row(n);
-        const int64_t c = row < a.streamed_rows ? a.centers[row] : -1;
+        const int64_t c = row_center[n];
         const bool known = c >= 0 && c < a.num_in;
         const elem* src = known && place[n] * S::kPerPiece < a.dim ? static_cast<const elem*>(a.streamed) + c * a.dim + place[n] * S::kPerPiece
                                                                  : reinterpret_cast<const elem*>(known ? zero_piece : nan_piece<E>);
@@ -398,7 +415,55 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
     read2 = (piece << 4) + (li & 1) * 8 + (4 * half + r) * ROWB;
   }
 
-  if (first < last) {
+  if constexpr (MODE == kScores) {
+    // The kept rows, 32 at a time, each into the registers of the wave that keeps them.  Read by that wave alone, 32 bytes of each
+    // of 32 rows per load, they come at 2.9 TB/s (fp32 rows of 256), in whole tiles at 4.
+    constexpr int STEPS = 4 * NB;
+    const int64_t row0 = kept_tile * S::kKept;
+    float step_bias[S::kLoads];
+    auto fetch_step = [&](int i) {
+      if constexpr (BIAS) {
+#pragma unroll
+        for (int n = 0; n < S::kLoads; ++n) {
+          const int64_t row = row0 + 32 * i + slot_row(n);
+          step_bias[n] = has_chunk(n) && row < a.kept_rows ? a.bias[row] : -INFINITY;
+        }
+      }
+    };
+    auto issue_step = [&](int i, int buf) {
+      const int64_t rows = min((int64_t)32, a.kept_rows - row0 - 32 * i);
+      const __amdgpu_buffer_rsrc_t range =
+          range_of(static_cast<const char*>(a.kept) + (row0 + 32 * i) * streamed_bytes, rows > 0 ? (int)rows * streamed_bytes : 0);
+#pragma unroll
+      for (int n = 0; n < S::kLoads; ++n) {
+        if (!has_chunk(n)) continue;
+        int at = place[n] * 16 < streamed_bytes ? slot_row(n) * streamed_bytes + place[n] * 16 : OUTSIDE;
+        if constexpr (BIAS) at = step_bias[n] != -INFINITY ? at : OUTSIDE;
+        load_piece_to_lds(range, at, &tile[buf][(4 * n + wave) * 1024]);
+      }
+    };
+    fetch_step(0);
+    issue_step(0, 0);
+    fetch_step(1);
+    if (first < last) fetch_centers(first);
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+      wait_loads_and_barrier();
+      if (i + 1 < STEPS) {
+        issue_step(i + 1, (i + 1) & 1);
+        if (i + 2 < STEPS) fetch_step(i + 2);
+      } else if (first < last) {               // STEPS is even: buffer 0 was read a step ago
+        issue(first, 0);
+        if (first + 1 < last) fetch_centers(first + 1);
+      }
+      if (wave == i / NB) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+          kept[i % NB][ks] = *reinterpret_cast<const vec4*>(tile[i & 1] + (read1 ^ ((ks & SWAP_KS) << 5)) + (ks & ~SWAP_KS) * 32);
+      }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  } else if (first < last) {
     fetch_bias(first);
     issue(first, 0);
     put_side(0);
@@ -409,10 +474,15 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
   auto take_tile = [&](auto which, int64_t t) {
     constexpr int BUF = decltype(which)::value;
     constexpr int JB = TILE / 32;
-    wait_loads_and_barrier();
+    // scores: each wave has waited for its loads in front of its stores, which need not be waited for
+    if constexpr (MODE == kScores) lds_barrier();
+    else wait_loads_and_barrier();
     if (t + 1 < last) {
       issue(t + 1, BUF ^ 1);
-      if (t + 2 < last) fetch_bias(t + 2);
+      if (t + 2 < last) {
+        fetch_bias(t + 2);
+        fetch_centers(t + 2);
+      }
     }
     const char* base = tile[BUF];
     acc16 z[JB][NB];
@@ -511,6 +581,7 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
         }
       }
     } else if constexpr (MODE == kScores) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
       for (int jb = 0; jb < JB; ++jb) {
         const int64_t pair0 = t * TILE + jb * 32 + 4 * half;
