@@ -154,9 +154,12 @@ struct Shape {
   static constexpr int kBlocks = DP / 32;                          // 32-column blocks of the second product
   // Registers: DP / 2 for the sums, DP / 4 (fp32: DP / 2) for the kept rows, 16 for each 32 streamed rows.  Two waves per SIMD, so
   // that one's exponentials run beside the other's matrix instructions, where 256 registers hold that.
-  static constexpr int kWaves = E::kWide && DP > 192 ? 1 : 2;
+  static constexpr int kWaves = MODE != kScores && E::kWide && DP > 192 ? 1 : 2;
   static constexpr int kTile = MODE == kScores || DP > (E::kWide ? 128 : 192) ? 32 : 64;
   static constexpr int kNB = MODE == kScores && !E::kWide && DP <= 128 ? 2 : 1;
+  // Scores take their kept rows through LDS where these are longer than 256 bytes: read by the wave that keeps them, 32 bytes of
+  // each of 32 rows per load, rows of 1 KB come at 2.9 TB/s (one centre, 1 M nodes), in whole tiles at 4; of 128 bytes at 5.0 and 4.1.
+  static constexpr bool kStaged = MODE == kScores && kRowBytes > 256;
   static constexpr int kKept = 32 * kNB * 4;                       // kept rows per workgroup
   static constexpr int kChunks = kTile * kPieces / 64;             // loads of a wave (1 KB) that make a tile
   static constexpr int kLoads = (kChunks + 3) / 4;                 // per wave
@@ -298,7 +301,7 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
       kept_bias[nb] = live ? a.bias[row] * (MODE == kScores ? 1.0f : kLog2e) : -INFINITY;
       live = kept_bias[nb] != -INFINITY;
     }
-    if constexpr (MODE == kScores) continue;   // through LDS, below
+    if constexpr (S::kStaged) continue;        // below
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       const int at = (2 * ks + half) * S::kPerPiece;
@@ -332,7 +335,7 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
       }
     }
   };
-  constexpr int OUTSIDE = 1 << 30;
+  constexpr int OUTSIDE = 1 << 30, FEW = 8;
   const int streamed_bytes = (MODE == kTableGrad ? DP : a.dim) * (int)sizeof(elem);
   int place[S::kLoads];                        // in the tile's range
 #pragma unroll
@@ -415,9 +418,8 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
     read2 = (piece << 4) + (li & 1) * 8 + (4 * half + r) * ROWB;
   }
 
-  if constexpr (MODE == kScores) {
-    // The kept rows, 32 at a time, each into the registers of the wave that keeps them.  Read by that wave alone, 32 bytes of each
-    // of 32 rows per load, they come at 2.9 TB/s (fp32 rows of 256), in whole tiles at 4.
+  if constexpr (S::kStaged) {
+    // the kept rows, 32 at a time, each into the registers of the wave that keeps them
     constexpr int STEPS = 4 * NB;
     const int64_t row0 = kept_tile * S::kKept;
     float step_bias[S::kLoads];
@@ -463,6 +465,13 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
       }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  } else if constexpr (MODE == kScores) {
+    if (first < last) {
+      fetch_centers(first);
+      issue(first, 0);
+      if (first + 1 < last) fetch_centers(first + 1);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   } else if (first < last) {
     fetch_bias(first);
     issue(first, 0);
@@ -486,6 +495,28 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
     }
     const char* base = tile[BUF];
     acc16 z[JB][NB];
+    if constexpr (MODE == kScores && E::kWide) {
+      // a few centres alone: their sums by ordinary arithmetic, a centre at a time (1/16 of a tile's matrix instructions each)
+      const int64_t left = a.streamed_rows - t * TILE;
+      if (left <= FEW) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        for (int row = 0; row < (int)left; ++row) {
+          float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            const vec4 v = *reinterpret_cast<const vec4*>(base + row * ROWB + ((((2 * ks) | half) ^ swap_of<SWAPPED>(row)) << 4));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] = fmaf(v[e], kept[0][ks][e], sum[e]);
+          }
+          float z1 = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          z1 += __shfl_xor(z1, 32, 64);
+          if (half == 0 && kept_row0 < a.kept_rows)
+            static_cast<float*>(a.out)[(t * TILE + row) * a.kept_rows + kept_row0] =
+                !BIAS ? z1 * a.scale2 : kept_bias[0] == -INFINITY ? -INFINITY : fmaf(z1, a.scale2, kept_bias[0]);
+        }
+        return;
+      }
+    }
     if constexpr (S::kWaves > 1) __builtin_amdgcn_s_setprio(1);         // of two waves the one with matrix work to issue goes first: 1 %
 #pragma unroll
     for (int jb = 0; jb < JB; ++jb) {
@@ -581,7 +612,8 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
         }
       }
     } else if constexpr (MODE == kScores) {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) asm volatile("s_waitcnt vmcnt(0)" : "+v"(z[0][nb]) : : "memory");      // behind the products
 #pragma unroll
       for (int jb = 0; jb < JB; ++jb) {
         const int64_t pair0 = t * TILE + jb * 32 + 4 * half;
