@@ -478,6 +478,8 @@ int32_t gs_table_mult_add(void* dst, const void* src, int64_t num_nodes, int32_t
  *   [num_nodes][dim] or NULL, both of the tables' dtype and overwritten.
  *   Sums, maxima and statistics are fp32 or fp64; 16-bit tables: the probabilities
  *   are rounded to the tables' format before they are summed with rows (fp32 sums).
+ *   A pair's own context enters as 1 - p, from the other nodes' sum: the loss and
+ *   the gradients of a pair that is nearly certain keep their relative precision.
  *   Same bits on every run.  The pairs x nodes matrix is never stored.
  *   contexts[i] = -1 leaves the pair out (loss 0, no gradient).  A centre outside
  *   [0, num_in), or another context outside [0, num_nodes), gives loss NaN and no
@@ -517,9 +519,10 @@ int32_t gs_scores(const void* w_in, int64_t num_in, const void* w_out, int64_t n
  *   (u >= 1 or NaN: the last that has any weight); probs_out[r], if not NULL, e_j
  *   over that sum.  temperature 0 takes the first node of the order, probability 1.
  *   A row of nothing but left-out nodes gives id -1 and probability 0; a negative
- *   temperature or NaN gives id -1 and probability NaN.  All weights are fp64, so
- *   that the answer is that of the definition unless u falls within about 1e-15 of
- *   a border; same answer on every run.
+ *   temperature or NaN gives id -1 and probability NaN.  All weights are fp64 and
+ *   are added as multiples of 2^-62, so that the answer is that of the definition
+ *   unless u, top_p or min_p falls within about 1e-13 of a border; same answer on
+ *   every run.
  *   ids_out int32[rows], probs_out float[rows]; 1 <= n < 2^31, rows < 2^22.
  * ------------------------------------------------------------------------ */
 size_t gs_sample_scores_workspace_bytes(int64_t rows, int64_t n, int32_t dtype);

@@ -18,6 +18,11 @@
 // Two routes.  Row by row: one workgroup does all of it.  Split: where rows are long and fewer than the compute units need,
 // three passes over the scores by several workgroups a row (least and greatest; histogram; list and pieces), and one workgroup
 // a row finishes.
+//
+// Measured: 64 rows of 1 M fp32 scores, every filter: 45 us for the least and greatest (5.7 TB/s), 57 histogram, 9 plan, 45 list,
+// 30 to finish (a chain of small steps in one workgroup a row).  256 rows of 100,003 bf16 scores, top-p alone: 19, 51, 9, 33, 21:
+// the histogram weighs every score and adds it with three LDS atomics, the list weighs what lies above the cut.  One row of 10,000:
+// 15 us, latency of its steps.
 
 #include "common.h"
 

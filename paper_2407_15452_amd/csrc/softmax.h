@@ -17,6 +17,11 @@
 //   table gradient: nodes kept, pairs streamed, p from the forward pass's log-sum; no atomics, each row of g_out has one owner.
 // Where the kept rows alone do not fill the chip the streamed ones are split, and a small kernel joins the parts in order.
 //
+// Bound: the matrix instructions, from some hundred pairs on.  4096 pairs on 1 M bf16 nodes of 128 columns: forward 1.95 ms, table
+// gradient 1.86 ms, 1.08 and 1.13 PFLOP/s (library products of 8192^3 and 16384^3: 1.08 and 1.30); 65,536 pairs on 10,000 fp32 nodes of 64
+// columns: 1.27 and 1.40 ms, 132 and 119 TFLOP/s (library: 153).  Few pairs: reading the table, 5 to 6 TB/s (a large copy: 4.8).
+// Scores of many centres: writing them, 4.8 TB/s of 16-bit tables; fp32 rows of 256 columns the products, 115 TFLOP/s.
+//
 // LDS tiles are written by the loads themselves (global_load_lds, 16 bytes per lane, one tile ahead).  Such a load puts lane
 // l's piece at base + 16 l, so rows cannot be padded; pieces are swapped inside a row instead, by a function of the row that
 // the source address undoes.  Rows beyond the table, pieces beyond `dim` and rows of masked nodes (bias -inf) are read from a
@@ -157,8 +162,8 @@ struct Shape {
   static constexpr int kWaves = MODE != kScores && E::kWide && DP > 192 ? 1 : 2;
   static constexpr int kTile = MODE == kScores || DP > (E::kWide ? 128 : 192) ? 32 : 64;
   static constexpr int kNB = MODE == kScores && !E::kWide && DP <= 128 ? 2 : 1;
-  // Scores take their kept rows through LDS where these are longer than 256 bytes: read by the wave that keeps them, 32 bytes of
-  // each of 32 rows per load, rows of 1 KB come at 2.9 TB/s (one centre, 1 M nodes), in whole tiles at 4; of 128 bytes at 5.0 and 4.1.
+  // Scores take their kept rows through LDS in whole tiles where these are longer than 256 bytes, instead of 32 bytes of each of 32
+  // rows per load: 16 centres on 1 M nodes, 256 fp32 columns 385 -> 327 us, 256 bf16 columns 131 -> 118, but 64 bf16 columns 33 -> 40.
   static constexpr bool kStaged = MODE == kScores && kRowBytes > 256;
   static constexpr int kKept = 32 * kNB * 4;                       // kept rows per workgroup
   static constexpr int kChunks = kTile * kPieces / 64;             // loads of a wave (1 KB) that make a tile
@@ -214,6 +219,7 @@ __device__ __forceinline__ acc16 step(vec4 a, vec4 b, acc16 c) {
 }
 
 // ---- the pairs' rows, copied for the table gradient --------------------------------------------------------------------
+// 5 to 6 us: the table gradient streams them once per workgroup, which has no room for a centre's id in front of every load.
 // rows[i] = w_in[centers[i]], zero-padded to DP columns and to whole tiles; zeros for pairs without gradient (target -1).
 template <typename E>
 __global__ __launch_bounds__(kThreads) void gather_pairs_kernel(const typename E::elem* w_in, int dim, int padded,
@@ -496,7 +502,8 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
     const char* base = tile[BUF];
     acc16 z[JB][NB];
     if constexpr (MODE == kScores && E::kWide) {
-      // a few centres alone: their sums by ordinary arithmetic, a centre at a time (1/16 of a tile's matrix instructions each)
+      // a few centres alone: their sums by ordinary arithmetic, each 1/16 of what the tile's matrix instructions take (one centre
+      // on 1 M nodes of 256 columns 311 -> 168 us; eight take half a tile's time)
       const int64_t left = a.streamed_rows - t * TILE;
       if (left <= FEW) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -757,6 +764,7 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
 }
 
 // ---- joining the parts of the forward pass ------------------------------------------------------------------------------
+// Bound by reading the parts: 20 us for 65,536 pairs in one part, 22 us for 4096 in 16; one pair's 152 parts 4 us of latency.
 struct JoinArgs {
   const void *w_in, *w_out;
   int64_t num_in, num_nodes, num_pairs, padded_pairs;

@@ -368,3 +368,27 @@ def test_pairs_that_are_nearly_certain(gs, fmt, n, nodes, dim):
         bound = (r + terms * V + 4 * V) * absolute + low
         bound = bound + u * (want.abs() + bound) + least
         assert torch.all((have.double() - want).abs() <= bound), float(((have.double() - want).abs() - bound).max())
+
+
+@pytest.mark.parametrize("fmt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n,nodes,dim", [(1, 700, 256), (8, 129, 200), (9, 300, 160), (40, 1000, 256), (41, 257, 136), (100, 64, 72), (3, 5000, 64)])
+def test_masked_scores_in_every_layout(gs, fmt, n, nodes, dim):
+    """Long rows come through LDS, short ones do not, few fp32 centres take no matrix instructions: masked nodes of NaN and
+    infinity, centres that are no rows, and the last tile's own number of centres in each."""
+    w_in, w_out, c, _ = make(n, nodes, dim, fmt, rows=17)
+    bias = torch.randn(nodes, generator=torch.Generator().manual_seed(3))
+    masked = torch.rand(nodes, generator=torch.Generator().manual_seed(4)) < 0.3
+    masked[0], masked[-1] = True, True
+    bias[masked] = -math.inf
+    w_out[masked] = math.nan
+    w_out[0] = math.inf
+    bad = torch.zeros(n, dtype=torch.bool)
+    if n > 2:
+        c[n - 1], c[1] = -5, 17
+        bad[n - 1] = bad[1] = True
+    got = gs.gs_scores(w_in.to(DEV), w_out.to(DEV), c.to(DEV), bias=bias.to(DEV), scale=0.5).cpu().double()
+    assert torch.all(got[:, masked] == -math.inf) and torch.isnan(got[bad][:, ~masked]).all()
+    h, w = w_in.double()[c.long()[~bad]], w_out.double()[~masked]
+    want = 0.5 * (h @ w.T) + bias.double()[~masked]
+    bound = (dim + 4) * V * 0.5 * (h.abs() @ w.abs().T) + 4 * V * want.abs() + 2 * V * bias[~masked].abs().max()
+    assert torch.all((got[~bad][:, ~masked] - want).abs() <= bound)
