@@ -154,6 +154,14 @@ __device__ __forceinline__ void add_to(Histogram& h, int b, bool weights, double
   atomicAdd(&h.lo[b], (unsigned long long)w.lo);
 }
 
+// a sum of weights, none if it is 0; counts the additions
+__device__ __forceinline__ void add_units(Histogram& h, int b, uint64_t hi, uint64_t lo) {
+  if ((hi | lo) == 0) return;
+  atomicAdd(&h.count[b], 1u);
+  atomicAdd(&h.hi[b], (unsigned long long)hi);
+  atomicAdd(&h.lo[b], (unsigned long long)lo);
+}
+
 // 2048 equal steps between the row's least and greatest finite score.  fp32: every operation is monotone, which is all that a
 // cut needs (this file is compiled without contraction: each pass has to find a score in the same step).  Halves, so that the
 // distance of two floats is one.
@@ -506,10 +514,34 @@ __device__ __forceinline__ void choose_index(Shared& sh, const Row<V>& row, uint
     const int shift = bits > 11 ? bits - 11 : 0;
     clear_histogram(sh, true);
     const uint32_t from = (lo + row.skew) / Row<V>::kPer, to = (hi + row.skew) / Row<V>::kPer + 1;
-    for_row<1>(row, from, to, threadIdx.x, kThreads, [&](uint32_t at, float s) {
-      if (at < lo || at > hi) return;
-      const double e = kept_weight(key_of(s), at, cut, limits.min_p, weigh);
-      if (e > 0.0) add_to(sh.hist, kBins - 1 - (int)((at - lo) >> shift), true, e);
+    for_pieces<1>(row, from, to, threadIdx.x, kThreads, [&](uint32_t at, const float* s) {
+      constexpr uint32_t per = Row<V>::kPer;
+      Units w[per];
+#pragma unroll
+      for (uint32_t k = 0; k < per; ++k) {
+        const uint32_t key = key_of(s[k]);
+        const double e = weigh(s[k]);
+        const bool kept = s[k] > -INFINITY && at + k >= lo && at + k <= hi && (key > cut.key || (key == cut.key && at + k <= cut.last_tie)) &&
+                          !(limits.min_p > 0.0 && !(e >= limits.min_p));
+        w[k] = units_of(kept ? e : 0.0);
+      }
+      if ((1u << shift) < per) {
+#pragma unroll
+        for (uint32_t k = 0; k < per; ++k) add_units(sh.hist, kBins - 1 - (int)((at + k - lo) >> shift), w[k].hi, w[k].lo);
+      } else {                                 // a piece reaches into two bins at most: neighbouring lanes would add to them one by one
+        const uint32_t b0 = (uint32_t)max((int32_t)at - (int32_t)lo, 0) >> shift;
+        uint64_t hi2[2] = {0, 0}, lo2[2] = {0, 0};
+#pragma unroll
+        for (uint32_t k = 0; k < per; ++k) {
+          const bool next = (at + k - lo) >> shift != b0;
+          hi2[0] += next ? 0 : w[k].hi;
+          lo2[0] += next ? 0 : w[k].lo;
+          hi2[1] += next ? w[k].hi : 0;
+          lo2[1] += next ? w[k].lo : 0;
+        }
+        add_units(sh.hist, kBins - 1 - (int)b0, hi2[0], lo2[0]);
+        add_units(sh.hist, kBins - 2 - (int)b0, hi2[1], lo2[1]);
+      }
     });
     __syncthreads();
     const uint32_t b = find_answer(sh, above, total, limits.u);
@@ -774,8 +806,11 @@ __device__ __forceinline__ void first_histogram(Histogram& hist, const Row<V>& r
 }
 
 // ---- row by row --------------------------------------------------------------------------------------------------------
+// Two workgroups per compute unit, as their LDS allows: held to 128 registers the seldom used ways spill, but 4096 rows of 10,000
+// take 250 instead of 389 us (every filter), one row as long as before.  finish_rows_kernel has 256 rows or fewer in most calls and
+// would lose 3 us.
 template <typename V>
-__global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs a) {
+__global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(SampleArgs a) {
   __shared__ Shared sh;
   const int64_t r = blockIdx.x;
   const Row<V> row(a.scores, r, a.n);

@@ -903,6 +903,27 @@ __global__ __launch_bounds__(kThreads) void join_nodes_kernel(const float* part_
   }
 }
 
+// The same from many parts of few nodes: a workgroup a row, its lanes share the parts (512 parts of 100 nodes one lane after the
+// other took 150 us).
+template <typename E>
+__global__ __launch_bounds__(kThreads) void join_many_kernel(const float* part_acc, int64_t num_nodes, int dim, int padded,
+                                                             int splits, float out_scale, typename E::elem* g_out) {
+  __shared__ vec4 part[kThreads];
+  const int quads = padded / 4, slots = kThreads / quads;
+  const int quad = threadIdx.x % quads, slot = threadIdx.x / quads;
+  const int64_t row = blockIdx.x;
+  vec4 g = (vec4)0.0f;
+  if (slot < slots) {
+#pragma unroll 4
+    for (int k = slot; k < splits; k += slots) g += *reinterpret_cast<const vec4*>(part_acc + (k * num_nodes + row) * padded + 4 * quad);
+  }
+  part[threadIdx.x] = g;
+  __syncthreads();
+  if (slot != 0 || 4 * quad >= dim) return;
+  for (int k = 1; k < slots; ++k) g += part[k * quads + quad];
+  E::store4(g_out + row * dim + 4 * quad, g * out_scale);
+}
+
 // no pairs: every gradient is zero
 __global__ __launch_bounds__(kThreads) void zero_pieces_kernel(uint4* to, int64_t pieces) {
   for (int64_t s = (int64_t)blockIdx.x * kThreads + threadIdx.x; s < pieces; s += (int64_t)gridDim.x * kThreads)
@@ -1070,6 +1091,12 @@ static int32_t run_padded(const SoftmaxCall& q, const SoftmaxPlan& p, hipStream_
   a.out = q.g_out;
   rc = launch_stream<E, DP, kTableGrad>(a, stream);
   if (rc != GS_OK || p.node_splits == 1) return rc;
+  if (p.node_splits > 8) {                     // 64 tiles of nodes at most
+    join_many_kernel<E><<<(unsigned)q.num_nodes, kThreads, 0, stream>>>(p.part_acc, q.num_nodes, q.dim, DP, p.node_splits, a.out_scale,
+                                                                       static_cast<elem*>(q.g_out));
+    GS_LAUNCH_CHECK();
+    return GS_OK;
+  }
   join_nodes_kernel<E><<<blocks_for(q.num_nodes * (q.dim / 4)), kThreads, 0, stream>>>(
       p.part_acc, q.num_nodes, q.dim, DP, p.node_splits, a.out_scale, static_cast<elem*>(q.g_out));
   GS_LAUNCH_CHECK();
