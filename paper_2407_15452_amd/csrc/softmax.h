@@ -22,10 +22,11 @@
 // columns: 1.27 and 1.40 ms, 132 and 119 TFLOP/s (library: 153).  Few pairs: reading the table, 5 to 6 TB/s (a large copy: 4.8).
 // Scores of many centres: writing them, 4.8 TB/s of 16-bit tables; fp32 rows of 256 columns the products, 115 TFLOP/s.
 //
-// LDS tiles are written by the loads themselves (global_load_lds, 16 bytes per lane, one tile ahead).  Such a load puts lane
+// LDS tiles are written by the loads themselves (16 bytes per lane, one tile ahead).  Such a load puts lane
 // l's piece at base + 16 l, so rows cannot be padded; pieces are swapped inside a row instead, by a function of the row that
-// the source address undoes.  Rows beyond the table, pieces beyond `dim` and rows of masked nodes (bias -inf) are read from a
-// piece of zeros: whatever a masked row holds, infinities and NaN included, it takes no part.
+// the source address undoes.  Rows beyond the table, pieces beyond `dim` and rows of masked nodes (bias -inf) are read as zeros,
+// from outside of a buffer load's range or from a piece of zeros: whatever a masked row holds, infinities and NaN included, it
+// takes no part.
 
 #pragma once
 

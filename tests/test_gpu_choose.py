@@ -234,3 +234,14 @@ def test_lists_of_more_than_one_histogram(gs, n, fmt):
     z = torch.round(z * 4) / 4                       # some hundred values
     check(gs, z, u, top_p=[0.5, 0.7, 0.9, 0.95, 0.99, 0.999])
     check(gs, z, u, top_k=[1500, 2500, 3500, 4000, 5000, 8000], top_p=[0.5, 0.7, 0.9, 0.95, 0.99, 0.999])
+
+
+@pytest.mark.parametrize("fmt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n", [8193, 12_001, 16_383])
+def test_long_rows_of_one_workgroup(gs, fmt, n):
+    """Bins of several neighbouring indices: the weights of a piece are added up before they go to a bin."""
+    z, u = rows_of(7, n, fmt, seed=11, masked=0.3)
+    u[0], u[1] = 0.0, float(np.nextafter(np.float32(1.0), np.float32(0.0)))
+    z[2, :-1] = -math.inf                                  # the last alone
+    check(gs, z, u)
+    check(gs, z, u, temperature=[0.5, 1.0, 2.0, 0.25, 1.5, 4.0, 0.7], min_p=[0.0, 0.01, 0.5, 1.0, 0.2, 0.001, 0.05])

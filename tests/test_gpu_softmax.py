@@ -392,3 +392,12 @@ def test_masked_scores_in_every_layout(gs, fmt, n, nodes, dim):
     want = 0.5 * (h @ w.T) + bias.double()[~masked]
     bound = (dim + 4) * V * 0.5 * (h.abs() @ w.abs().T) + 4 * V * want.abs() + 2 * V * bias[~masked].abs().max()
     assert torch.all((got[~bad][:, ~masked] - want).abs() <= bound)
+
+
+@pytest.mark.parametrize("fmt", ["f32", "bf16"])
+@pytest.mark.parametrize("n,nodes,dim", [(2000, 33, 24), (1500, 1, 72), (4000, 130, 200), (3000, 70, 96)])
+def test_many_pairs_on_few_nodes(gs, fmt, n, nodes, dim):
+    """The pairs are split into many parts, which lanes of a workgroup join."""
+    w_in, w_out, c, t = make(n, nodes, dim, fmt, rows=500)
+    t[::5] = -1
+    check(gs, w_in, w_out, c, t, fmt, grad_scale=1.0 / n)
