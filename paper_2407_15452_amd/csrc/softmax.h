@@ -58,7 +58,7 @@ struct SoftmaxPlan {
   int64_t tiles_per_split, tiles_per_node_split;
   void* rows;
   int32_t* target;
-  float *lse2, *miss, *part_max, *part_acc;
+  float *lse2, *miss, *part_max, *part_rounded, *part_acc;
   double* part_sum;
   size_t bytes;
 };
@@ -122,6 +122,9 @@ struct BF16 {
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((vec2){lo, hi}, bf2));
   }
+  static __device__ __forceinline__ float add_pair(uint32_t w, float sum) {
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf2, w), (bf2){(__bf16)1.0f, (__bf16)1.0f}, sum, false);
+  }
   static __device__ __forceinline__ acc16 mfma(vec4 a, vec4 b, acc16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
   }
@@ -139,6 +142,9 @@ struct F16 {
   static __device__ __forceinline__ float load(const uint16_t* p) { return __half2float(__ushort_as_half(*p)); }
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((vec2){lo, hi}, hf2));
+  }
+  static __device__ __forceinline__ float add_pair(uint32_t w, float sum) {
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(hf2, w), (hf2){(_Float16)1.0f, (_Float16)1.0f}, sum, false);
   }
   static __device__ __forceinline__ acc16 mfma(vec4 a, vec4 b, acc16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(hf8, a), __builtin_bit_cast(hf8, b), c, 0, 0, 0);
@@ -257,6 +263,7 @@ struct StreamArgs {
   int64_t tiles_per_split;
   float* part_max;           // forward: [splits][pairs]
   double* part_sum;          // forward: [splits][pairs]
+  float* part_rounded;       // .. of the probabilities as they are rounded to 16 bits
   float* part_acc;           // [splits][kept_rows][DP], or null (table gradient without splits)
   void* out;                 // table gradient without splits: g_out; scores: the scores
 };
@@ -268,6 +275,10 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
   constexpr int NB = S::kNB, TILE = S::kTile, ROWB = S::kRowBytes, PIECES = S::kPieces, KS = S::kSteps, DB = S::kBlocks, SWAPPED = S::kSwapped;
   constexpr bool NODES_STREAMED = MODE == kLossOnly || MODE == kForward;
   constexpr bool SECOND = MODE == kForward || MODE == kTableGrad;
+  // g_in is the sum of p_j (c_j - c_t).  Rows that share a large part leave little of it: the context's share, which the join takes
+  // off, has to be that of the same rounded probabilities: an instruction per two of them.  64 bf16 nodes whose columns are 24 +- 0.5:
+  // relative error of g_in 1.68e-3; 1.04e-2 with the unrounded probabilities' share; 1.66e-3 with fp32 probabilities.
+  constexpr bool ROUNDED = MODE == kForward && !E::kWide;
   __shared__ __attribute__((aligned(1024))) char tile[2][TILE * ROWB];
   __shared__ __attribute__((aligned(16))) float side[2][TILE];              // nodes streamed: bias * log2(e); pairs streamed: base-2 log-sums
   __shared__ __attribute__((aligned(16))) float side_miss[2][TILE];         // pairs streamed
@@ -406,10 +417,12 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
   }
   float run_max[NB];
   double run_sum[NB];                          // this half wave's streamed rows
+  float run_rounded[NB];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     run_max[nb] = -INFINITY;
     run_sum[nb] = 0.0;
+    run_rounded[nb] = 0.0f;
   }
 
   // lane's parts of the LDS addresses; the swap turns bits of them that a row's place leaves zero, what lies above is added
@@ -609,6 +622,7 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
             sum += z[jb][nb][r];
           }
         run_sum[nb] = run_sum[nb] * (double)keep[nb] + (double)sum;
+        if constexpr (ROUNDED) run_rounded[nb] *= keep[nb];
       }
       if constexpr (SECOND) {
         if (__any(moved)) {
@@ -704,8 +718,11 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                p[nb][e] = __uint_as_float(E::pack(z[jb][nb][8 * q2 + 2 * e], z[jb][nb][8 * q2 + 2 * e + 1]));
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t w = E::pack(z[jb][nb][8 * q2 + 2 * e], z[jb][nb][8 * q2 + 2 * e + 1]);
+                if constexpr (ROUNDED) run_rounded[nb] = E::add_pair(w, run_rounded[nb]);
+                p[nb][e] = __uint_as_float(w);
+              }
 #pragma unroll
             for (int db = 0; db < DB; ++db) {
               short4_t part[2];
@@ -743,6 +760,10 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
         a.part_sum[split * a.kept_rows + row] = sum;
       }
     }
+    if constexpr (ROUNDED) {
+      const float rounded = run_rounded[nb] + __shfl_xor(run_rounded[nb], 32, 64);
+      if (row < a.kept_rows && half == 0) a.part_rounded[split * a.kept_rows + row] = rounded;
+    }
     if constexpr (SECOND) {
       if (row < a.kept_rows) {
 #pragma unroll
@@ -775,6 +796,7 @@ struct JoinArgs {
   float scale, out_scale;
   const float* part_max;
   const double* part_sum;
+  const float* part_rounded;
   const float* part_acc;
   float* loss;
   float* lse2;               // for the table gradient, to whole tiles: +infinity for a pair without gradient; or null
@@ -874,7 +896,9 @@ __global__ __launch_bounds__(kThreads) void join_pairs_kernel(JoinArgs a) {
       const float pm = a.part_max[s * a.num_pairs + i];
       const bool empty = pm == -INFINITY && a.part_sum[s * a.num_pairs + i] == 0.0;           // masked nodes alone
       const float w = empty ? 0.0f : (float)(exp2((double)pm - m) * inverse);
-      g += w * *reinterpret_cast<const vec4*>(a.part_acc + (s * a.num_pairs + i) * a.padded + 4 * quad);
+      vec4 part = *reinterpret_cast<const vec4*>(a.part_acc + (s * a.num_pairs + i) * a.padded + 4 * quad);
+      if constexpr (!E::kWide) part -= a.part_rounded[s * a.num_pairs + i] * to;
+      g += w * part;
     }
   }
   if constexpr (SLOTS > 1) {
@@ -885,7 +909,10 @@ __global__ __launch_bounds__(kThreads) void join_pairs_kernel(JoinArgs a) {
     for (int k = 1; k < SLOTS; ++k) g += part_g[k * QUADS + quad];
   }
   if (!column) return;
-  if (live) g = (g - miss * to) * a.out_scale;
+  if (live) {
+    if constexpr (E::kWide) g -= miss * to;
+    g *= a.out_scale;
+  }
   E::store4(static_cast<elem*>(a.g_in) + i * a.dim + 4 * quad, g);
 }
 
@@ -991,6 +1018,7 @@ SoftmaxPlan plan_softmax(void* ws, int64_t num_pairs, int64_t num_nodes, int32_t
     p.miss = c.take<float>(p.padded_pairs);
     p.part_max = c.take<float>(part_rows);
     p.part_sum = c.take<double>(part_rows);
+    if (grad && !E::kWide) p.part_rounded = c.take<float>(part_rows);
     p.part_acc = c.take<float>(acc_rows * p.padded);
   }
   p.bytes = std::max<size_t>(c.used, 256);
@@ -1040,6 +1068,7 @@ static int32_t run_padded(const SoftmaxCall& q, const SoftmaxPlan& p, hipStream_
   a.tiles_per_split = p.tiles_per_split;
   a.part_max = p.part_max;
   a.part_sum = p.part_sum;
+  a.part_rounded = p.part_rounded;
   a.part_acc = p.part_acc;
   a.target = q.contexts;
   int32_t rc = q.g_in ? launch_stream<E, DP, kForward>(a, stream) : launch_stream<E, DP, kLossOnly>(a, stream);
@@ -1062,6 +1091,7 @@ static int32_t run_padded(const SoftmaxCall& q, const SoftmaxPlan& p, hipStream_
   j.out_scale = out_scale;
   j.part_max = p.part_max;
   j.part_sum = p.part_sum;
+  j.part_rounded = p.part_rounded;
   j.part_acc = p.part_acc;
   j.loss = q.loss;
   j.lse2 = q.g_out ? p.lse2 : nullptr;
