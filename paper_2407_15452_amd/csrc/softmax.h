@@ -108,6 +108,8 @@ struct F32 {
   static constexpr int kForwardShift = 0;
   static constexpr float kSlack = 8.0f;
   static constexpr uint32_t kNan = 0x7fc00000u;
+  // zero + 0 w, which is NaN if w holds infinity or NaN
+  static __device__ __forceinline__ float add_none(float w, float zero) { return fmaf(w, 0.0f, zero); }
   static __device__ __forceinline__ float load(const float* p) { return *p; }
   static __device__ __forceinline__ void store4(float* p, vec4 v) { *reinterpret_cast<vec4*>(p) = v; }
 };
@@ -124,6 +126,9 @@ struct BF16 {
   }
   static __device__ __forceinline__ float add_pair(uint32_t w, float sum) {
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf2, w), (bf2){(__bf16)1.0f, (__bf16)1.0f}, sum, false);
+  }
+  static __device__ __forceinline__ float add_none(float w, float zero) {
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf2, w), (bf2){(__bf16)0.0f, (__bf16)0.0f}, zero, false);
   }
   static __device__ __forceinline__ acc16 mfma(vec4 a, vec4 b, acc16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
@@ -145,6 +150,9 @@ struct F16 {
   }
   static __device__ __forceinline__ float add_pair(uint32_t w, float sum) {
     return __builtin_amdgcn_fdot2(__builtin_bit_cast(hf2, w), (hf2){(_Float16)1.0f, (_Float16)1.0f}, sum, false);
+  }
+  static __device__ __forceinline__ float add_none(float w, float zero) {
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(hf2, w), (hf2){(_Float16)0.0f, (_Float16)0.0f}, zero, false);
   }
   static __device__ __forceinline__ acc16 mfma(vec4 a, vec4 b, acc16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(hf8, a), __builtin_bit_cast(hf8, b), c, 0, 0, 0);
@@ -498,6 +506,22 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
     put_side(0);
     if (first + 1 < last) fetch_bias(first + 1);
   }
+  // Pairs without gradient are rows of zeros, whose probability is 0 by a log-sum of infinity: but not where a node's row holds
+  // infinities or NaN, which turn it into NaN.  A wave that keeps such a row sets those pairs' to 0 by name (what the others pay to
+  // know that they keep none: 1 % of a batch at most).
+  bool no_numbers = false;
+  if constexpr (MODE == kTableGrad) {
+    vec4 zero = (vec4)0.0f;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) zero[e] = E::add_none(kept[nb][ks][e], zero[e]);
+    const float sum = (zero[0] + zero[1]) + (zero[2] + zero[3]);
+    no_numbers = __any(sum != sum);
+  }
+
   // One tile.  The buffer is a constant of the code: its place is part of the LDS instructions then, and the lane's addresses
   // do not change over the loop.
   auto take_tile = [&](auto which, int64_t t) {
@@ -665,6 +689,21 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
               z[jb][nb][4 * q + e] = __builtin_amdgcn_exp2f(fmaf(z[jb][nb][4 * q + e], a.scale2, add));
             }
         }
+      if (__builtin_expect(no_numbers, 0)) {
+        rare();
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int4 ids = *reinterpret_cast<const int4*>(&side_target[BUF][jb * 32 + 8 * q + 4 * half]);
+            const int32_t id[4] = {ids.x, ids.y, ids.z, ids.w};
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (id[e] < 0) z[jb][nb][4 * q + e] = 0.0f;
+          }
+      }
       // does any pair of this tile have its context among this wave's nodes?
       const int32_t wave_node0 = (int32_t)(kept_row0 - l32), t_of_lane = side_target[BUF][lane % TILE];
       if (__any(t_of_lane >= wave_node0 && t_of_lane - wave_node0 < 32 * NB)) {
