@@ -583,20 +583,19 @@ def _out(t, shape, dtype, device, name):
 
 
 def gs_softmax_loss(w_in, w_out, centers, contexts, bias=None, scale: float = 1.0, grad_scale: float = 1.0,
-                    want_grad: bool = True, loss_out=None, g_in=None, g_out=None, ws=None):
-    """Softmax loss of every pair over all nodes; returns (loss [n] float32, g_in [n, dim], g_out [nodes, dim]),
-    the gradients None without want_grad (see gs.h)."""
+                    want_grad=True, loss_out=None, g_in=None, g_out=None, ws=None):
+    """Softmax loss of every pair over all nodes; returns (loss [n] float32, g_in [n, dim], g_out [nodes, dim]).
+    want_grad: True for both gradients, "in" or "out" for one alone, False for none; the others are None (see gs.h)."""
+    if isinstance(want_grad, str) and want_grad not in ("in", "out"):
+        raise ValueError('want_grad must be True, False, "in" or "out"')
     dtype = _two_tables(w_in, w_out, bias)
     (num_in, dim), num_nodes, n = w_in.shape, int(w_out.shape[0]), int(centers.numel())
     if int(contexts.numel()) != n:
         raise ValueError("centers and contexts must have the same length")
     dev = w_in.device
     loss_out = _out(loss_out, (n,), torch.float32, dev, "loss_out")
-    if want_grad:
-        g_in = _out(g_in, (n, dim), w_in.dtype, dev, "g_in")
-        g_out = _out(g_out, (num_nodes, dim), w_out.dtype, dev, "g_out")
-    else:
-        g_in = g_out = None
+    g_in = _out(g_in, (n, dim), w_in.dtype, dev, "g_in") if want_grad and want_grad != "out" else None
+    g_out = _out(g_out, (num_nodes, dim), w_out.dtype, dev, "g_out") if want_grad and want_grad != "in" else None
     if ws is None:
         ws = _workspace(gs_softmax_loss_workspace_bytes(n, num_nodes, dim, dtype, want_grad), dev)
     rc = lib().gs_softmax_loss(
