@@ -486,12 +486,15 @@ int32_t gs_table_mult_add(void* dst, const void* src, int64_t num_nodes, int32_t
  *   gradient; a masked context gives loss +infinity and no gradient.  Equal centres
  *   are separate rows of g_in; num_pairs = 0 writes zeros to g_out.
  *   dim a multiple of 4 (fp32) or 8 (16-bit) and at most 256; tables and gradients
- *   16-byte aligned; scale > 0.  Errors: GS_EINVAL otherwise.  Workspace:
- *   gs_softmax_loss_workspace_bytes (want_grad: whether g_in or g_out is given).
+ *   16-byte aligned; scale > 0.  Errors: GS_EINVAL otherwise; GS_EOVERFLOW for more
+ *   than 2^26 - 256 pairs, or more than 2^31 - 128 nodes, which no launch takes.
+ *   Workspace: gs_softmax_loss_workspace_bytes (want_grad: whether g_in or g_out is
+ *   given).
  *
  * gs_scores -- the same z, for answers: scores_out[i][j] = scale * <w_in[centers[i]],
  *   w_out[j]> + bias[j], float[num_centers][num_nodes]; -infinity for masked nodes,
- *   a row of NaN (but for masked nodes) for a centre that is no row.
+ *   a row of NaN (but for masked nodes) for a centre that is no row.  Errors as above
+ *   (GS_EOVERFLOW: the nodes alone).
  * ------------------------------------------------------------------------ */
 size_t gs_softmax_loss_workspace_bytes(int64_t num_pairs, int64_t num_nodes, int32_t dim, int32_t dtype,
                                        int32_t want_grad);

@@ -1078,7 +1078,8 @@ static int32_t run_padded(const SoftmaxCall& q, const SoftmaxPlan& p, hipStream_
   using elem = typename E::elem;
   constexpr int64_t most = ((int64_t)1 << 32) / kThreads;        // a launch takes fewer than 2^32 lanes
   if ((!q.loss || q.g_out) && p.node_tiles * p.node_splits >= most) return GS_EOVERFLOW;
-  if (q.loss && (p.pair_tiles * p.splits >= most || p.padded_pairs >= most)) return GS_EOVERFLOW;
+  // the join: four pairs a workgroup at least, but for few pairs in many parts
+  if (q.loss && (p.pair_tiles * p.splits >= most || p.padded_pairs / 4 >= most)) return GS_EOVERFLOW;
   auto blocks_for = [](int64_t items) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(items, kThreads), 256 * 16)); };
   StreamArgs a{};
   a.dim = q.dim;

@@ -1,4 +1,7 @@
-"""What the binding of the full-softmax operators refuses by itself, without a GPU."""
+"""What the full-softmax operators and their binding refuse, on the host: pointers are made up and never followed."""
+import ctypes as C
+import os
+
 import pytest
 import torch
 
@@ -12,3 +15,17 @@ def test_gradients_are_asked_for_by_name():
     for name in ("in", "out", True, False):
         with pytest.raises(TypeError):                       # the tensors are not on the GPU
             gs.gs_softmax_loss(f, f, ids, ids, want_grad=name)
+
+
+def test_more_pairs_than_a_launch_takes():
+    from paper_2407_15452_amd import binding, build
+    if not os.path.exists(binding.LIB_PATH):
+        build.build_lib()
+    at = [C.c_void_p(256 * i) for i in range(10)]
+    for dtype in (0, 1, 2):
+        for dim in (8, 64, 256):
+            for grads in ((at[7], at[8]), (None, at[8]), (at[7], None), (None, None)):
+                for pairs in ((1 << 26) - 255, 1 << 26, (1 << 31) - 1):
+                    assert binding.lib().gs_softmax_loss(
+                        at[1], C.c_int64(100), at[2], C.c_int64(50), C.c_int32(dim), C.c_int32(dtype), at[3], at[4], C.c_int64(pairs), None,
+                        C.c_float(1.0), at[6], *grads, C.c_float(1.0), at[9], C.c_size_t(1 << 62), None) == binding.GS_EOVERFLOW
