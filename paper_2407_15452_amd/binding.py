@@ -673,6 +673,8 @@ class GradList:
             o = None if self.outs is None else self.outs[i]
             if o is not None and (o.dtype != g.dtype or o.numel() != g.numel()):
                 raise TypeError("an output must have its gradient's size and dtype")
+            if g.device != self.device or (o is not None and o.device != self.device):
+                raise ValueError("gradients and outputs must be on one device")
             self.array[i] = TensorStruct(g.data_ptr(), None if o is None else _dev(o, None, "output").value, g.numel(), _table_dtype(g))
 
 

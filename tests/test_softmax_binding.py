@@ -29,3 +29,24 @@ def test_more_pairs_than_a_launch_takes():
                     assert binding.lib().gs_softmax_loss(
                         at[1], C.c_int64(100), at[2], C.c_int64(50), C.c_int32(dim), C.c_int32(dtype), at[3], at[4], C.c_int64(pairs), None,
                         C.c_float(1.0), at[6], *grads, C.c_float(1.0), at[9], C.c_size_t(1 << 62), None) == binding.GS_EOVERFLOW
+
+
+class Elsewhere(torch.Tensor):
+    """Says that it is on a GPU, of a number of its own."""
+    is_cuda = property(lambda self: True)
+    device = property(lambda self: torch.device("cuda", self.place))
+
+
+def on_gpu(place, n=4):
+    t = torch.zeros(n).as_subclass(Elsewhere)
+    t.place = place
+    return t
+
+
+def test_gradients_of_one_device():
+    from paper_2407_15452_amd import binding as gs
+    a, b, other = on_gpu(0), on_gpu(0), on_gpu(1)
+    assert gs.GradList([a, b], [None, on_gpu(0)]).device == torch.device("cuda", 0)
+    for grads, outs in (([a, other], None), ([a, b], [other, None]), ([a, b], [None, other])):
+        with pytest.raises(ValueError):
+            gs.GradList(grads, outs)
