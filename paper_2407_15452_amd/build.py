@@ -21,6 +21,7 @@ OBJ_DIR = os.path.join(_HERE, "_build")
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextra",
     "-munsafe-fp-atomics",
+    "-Werror=pass-failed",          # a kernel that cannot hold the occupancy it is bounded to
     # packed fp32 arithmetic is kept off for every kernel of this library
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]

@@ -430,7 +430,9 @@ __device__ __forceinline__ uint64_t ties_below(double above, double e, double ta
   return stay;
 }
 
-template <typename V>
+// WAVES: of the kernel that calls it, per SIMD.  One body for two kernels would take the registers of the one that may have more,
+// and the other one with it.
+template <int WAVES, typename V>
 __device__ __noinline__ void cut_the_long_way(Shared& sh, const Row<V>& row, uint32_t kmin, uint32_t kmax, const Weigh& weigh, const RowLimits& limits, Cut& cut) {
   const Steps steps(kmin, kmax);
   uint64_t ties = 0;
@@ -807,8 +809,8 @@ __device__ __forceinline__ void first_histogram(Histogram& hist, const Row<V>& r
 
 // ---- row by row --------------------------------------------------------------------------------------------------------
 // Two workgroups per compute unit, as their LDS allows: held to 128 registers the seldom used ways spill, but 4096 rows of 10,000
-// take 250 instead of 389 us (every filter), one row as long as before.  finish_rows_kernel has 256 rows or fewer in most calls and
-// would lose 3 us.
+// take 253 instead of 387 us (every filter) and 255 instead of 284 (none), one row as long as before.  finish_rows_kernel has 256 rows
+// or fewer in most calls and would lose 3 us.
 template <typename V>
 __global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(SampleArgs a) {
   __shared__ Shared sh;
@@ -827,7 +829,7 @@ __global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(SampleArgs a) 
     __syncthreads();
     const Plan plan = make_plan(sh, x.kmin, x.kmax, limits);
     if (plan.long_way) {
-      cut_the_long_way(sh, row, x.kmin, x.kmax, weigh, limits, cut);
+      cut_the_long_way<4>(sh, row, x.kmin, x.kmax, weigh, limits, cut);
     } else if (plan.listed) {
       const float lo = score_of(plan.lo), hi = score_of(plan.hi);
       for_row<kAhead>(row, 0, row.pieces(), threadIdx.x, kThreads, [&](uint32_t at, float s) {
@@ -1040,7 +1042,7 @@ __global__ __launch_bounds__(kThreads) void finish_rows_kernel(SplitArgs a) {
   uint32_t lo = 0, hi = row.n - 1;
   Sum above{0, 0, 0}, total{0, 0, 0};
   if (plan.long_way) {
-    cut_the_long_way(sh, row, x.kmin, x.kmax, weigh, limits, cut);
+    cut_the_long_way<2>(sh, row, x.kmin, x.kmax, weigh, limits, cut);
   } else {
     if (plan.listed) {
       for (uint32_t j = threadIdx.x; j < plan.length; j += kThreads) sh.list[j] = a.lists[r * kListMost + j];
