@@ -39,7 +39,7 @@ def train(w_in, w_out, centers, contexts, batch, steps, lr, max_norm):
         lo = k * batch % (centers.numel() - batch + 1)
         c, t = centers[lo:lo + batch].contiguous(), contexts[lo:lo + batch].contiguous()
         loss, _, _ = gs.gs_softmax_loss(w_in, w_out, c, t, grad_scale=1.0 / batch, g_in=g_in, g_out=g_out, ws=ws)
-        g_w.zero_().index_add_(0, c.long(), g_in)  # a row per pair: pairs of one centre add up
+        g_w.zero_().index_add_(0, c.long(), g_in)  # a row per pair: pairs of one centre add up (in an order that may differ from run to run)
         norms.append(gs.gs_clip_grads(grads, max_norm))
         gs.gs_table_mult_add(w_in, g_w, -lr)
         gs.gs_table_mult_add(w_out, g_out, -lr)

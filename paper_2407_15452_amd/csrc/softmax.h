@@ -13,14 +13,22 @@
 // any numbering of its inner dimension, as long as both operands use the same one.  The left operand of the second product is
 // the streamed tile again, transposed on its way out of LDS (16-bit tables: ds_read_b64_tr_b16; fp32: one column per lane).
 //   forward: pairs kept, nodes streamed, running maximum and sum over the nodes but the context; gives the loss, 1 - p_it and
-//     sum_{j != t} p_ij c_j in one pass.
+//     sum_{j != t} p_ij c_j in one pass (16-bit tables: also the sum of the probabilities as they are rounded).
 //   table gradient: nodes kept, pairs streamed, p from the forward pass's log-sum; no atomics, each row of g_out has one owner.
 // Where the kept rows alone do not fill the chip the streamed ones are split, and a small kernel joins the parts in order.
 //
-// Bound: the matrix instructions, from some hundred pairs on.  4096 pairs on 1 M bf16 nodes of 128 columns: forward 1.95 ms, table
-// gradient 1.86 ms, 1.08 and 1.13 PFLOP/s (library products of 8192^3 and 16384^3: 1.08 and 1.30); 65,536 pairs on 10,000 fp32 nodes of 64
-// columns: 1.27 and 1.40 ms, 132 and 119 TFLOP/s (library: 153).  Few pairs: reading the table, 5 to 6 TB/s (a large copy: 4.8).
-// Scores of many centres: writing them, 4.8 TB/s of 16-bit tables; fp32 rows of 256 columns the products, 115 TFLOP/s.
+// Precision: the second products of 16-bit tables take the probabilities rounded to the tables' format, as the matrix instructions
+// do; sums are fp32.  Probabilities in two parts of the format would cost a half more of these products.  The results are rounded
+// to the same format, which hides most of it: relative error of g_in 1.01 to 1.04 times that of fp32 probabilities, of g_out 1.02 to
+// 1.18 times (128 columns, 8 to 2000 pairs on 64 to 1000 nodes; g_out of 2000 pairs on 1000: bf16 1.78e-3 instead of 1.67e-3, fp16
+// 2.38e-4 instead of 2.08e-4), at most sqrt(2) times, of a single term; of 777 pairs on 20,000 nodes 1.00 and 1.03 times.
+//
+// Bound: the matrix instructions, from some hundred pairs on.  4096 pairs on 1 M bf16 nodes of 128 columns: forward 1.83 ms, table
+// gradient 1.76 ms, 1.15 and 1.19 PFLOP/s (library products of 8192^3 and 16384^3 on that card: 1.16 and 1.38); 65,536 pairs on
+// 10,000 fp32 nodes of 64 columns: 1.27 and 1.42 ms, 132 and 119 TFLOP/s (library: 153).  Few pairs, a tile of 64 computed whole: the
+// loss alone of 16 pairs on 1 M nodes of 128 columns reads bf16 tables at 5.4 TB/s (a large copy: 4.8) and fp32 ones at 2.0; with the
+// gradients 0.22 and 0.81 ms, a half and a quarter of the rate at which tables and gradients could be read and written.  Scores of
+// many centres: writing them, 4.8 TB/s of 16-bit tables; fp32 rows of 256 columns the products, 115 TFLOP/s.
 //
 // LDS tiles are written by the loads themselves (16 bytes per lane, one tile ahead).  Such a load puts lane
 // l's piece at base + 16 l, so rows cannot be padded; pieces are swapped inside a row instead, by a function of the row that
@@ -825,7 +833,8 @@ __global__ __launch_bounds__(kThreads, (Shape<E, DP, MODE>::kWaves)) void stream
 }
 
 // ---- joining the parts of the forward pass ------------------------------------------------------------------------------
-// Bound by reading the parts: 20 us for 65,536 pairs in one part, 22 us for 4096 in 16; one pair's 152 parts 4 us of latency.
+// Bound by reading the parts: 20 us for 65,536 pairs in one part, 22 us for 4096 in 16, 19 us for 777 in 72 (50 MB); one pair's 152
+// parts 4 us of latency.
 struct JoinArgs {
   const void *w_in, *w_out;
   int64_t num_in, num_nodes, num_pairs, padded_pairs;
