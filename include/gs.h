@@ -531,7 +531,8 @@ int32_t gs_scores(const void* w_in, int64_t num_in, const void* w_out, int64_t n
  *   of a border (3e-13 for a million nodes, 5e-10 for 2^31), or min_p within 6e-14 of
  *   itself of a weight.  A node whose e is below 2^-62 has no weight and is not chosen.
  *   Same answer on every run.
- *   ids_out int32[rows], probs_out float[rows]; 1 <= n < 2^31, rows < 2^22.
+ *   ids_out int32[rows], probs_out float[rows]; 1 <= n < 2^31, rows < 2^22
+ *   (GS_EOVERFLOW for more rows, GS_EINVAL otherwise).
  * ------------------------------------------------------------------------ */
 size_t gs_sample_scores_workspace_bytes(int64_t rows, int64_t n, int32_t dtype);
 int32_t gs_sample_scores(const void* scores, int64_t rows, int64_t n, int32_t dtype, const float* uniforms,
