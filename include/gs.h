@@ -564,6 +564,92 @@ size_t gs_clip_grads_workspace_bytes(int32_t num_tensors);
 int32_t gs_clip_grads(const gs_tensor* list, int32_t num_tensors, double max_norm, double* norm_out, void* ws,
                       size_t ws_bytes, void* stream);
 
+/* --------------------------------------------------------------------------
+ * 8-bit tables, for answers: a row is e4m3 values with a power of two for each block
+ * of 128 columns (the last block may be shorter).  One byte a value instead of two or
+ * four: a table of as many nodes again or three times as many is held and read for the
+ * same memory.  Training keeps its own rows; gs_quantize_rows makes the copy.
+ *   data    uint8[num_nodes][gs_q8_pitch(dim)]: e4m3 (the format with NaN and without
+ *           infinity), dim up to a multiple of 16 columns, zeros behind the row; 16-byte
+ *           aligned.
+ *   scales  uint8[num_nodes][gs_q8_scale_pitch(dim)]: e8m0 (byte = exponent + 127, 255 =
+ *           NaN), a block each: 1, 2 or a multiple of 4, zeros behind the row; 4-byte aligned.
+ *   dim at most GS_Q8_MAX_DIM.  Both helpers are host functions; 0 for no such dim.
+ *
+ * gs_quantize_rows -- rows of a table in that form.  In a block, a = max |x|: the scale
+ *   is the least power of two s with a <= 448 s, at least 2^-127, and a value x becomes
+ *   the e4m3 nearest to x / s (ties to even), one rounding: at most half a step, 2^-4 of
+ *   a value above 2^-6 s, 2^-10 s below.  A block with infinity or NaN in it gets the
+ *   scale NaN and zeros.
+ *   table [num_nodes][dim] of dtype GS_F32 | GS_BF16 | GS_F16, 16-byte aligned; dim a
+ *   multiple of 4 (fp32) or 8 (16-bit).
+ *   ids  int32[n]: only rows ids[i] of the table are written to rows ids[i] of the copy
+ *   (the rows that a step has changed; ids outside [0, num_nodes) are skipped, equal ones
+ *   are fine), all others stay as they are; NULL: every row, with n = num_nodes.
+ *   count_dev: NULL, or int64[1] on the device: only the first min(n, *count_dev) ids, as
+ *   gs_unique_ids writes it (with ids alone).
+ *
+ * gs_scores_q8 -- gs_scores from 8-bit tables: scores_out[i][j] = scale * <row centers[i] of
+ *   the one table, row j of the other> + bias[j], of the values that their bytes stand for.
+ *   Sums are fp32.  scores_out [num_centers][num_nodes] of dtype GS_F32 | GS_BF16 | GS_F16
+ *   (one rounding, from fp32), aligned to its element.  bias, masked nodes and centres that
+ *   are no row as for gs_scores; a scale NaN makes the scores of its row NaN.
+ *   Same bits on every run.  Errors: GS_EINVAL, GS_EOVERFLOW for more than 2^21 - 32
+ *   centres.
+ * ------------------------------------------------------------------------ */
+enum { GS_Q8_MAX_DIM = 8192 };
+int32_t gs_q8_pitch(int32_t dim);
+int32_t gs_q8_scale_pitch(int32_t dim);
+int32_t gs_quantize_rows(const void* table, int64_t num_nodes, int32_t dim, int32_t dtype, const int32_t* ids, int64_t n,
+                         const int64_t* count_dev, void* q_out, void* scales_out, void* stream);
+size_t gs_scores_q8_workspace_bytes(int64_t num_centers, int64_t num_nodes, int32_t dim);
+int32_t gs_scores_q8(const void* q_in, const void* scales_in, int64_t num_in, const void* q_out, const void* scales_out,
+                     int64_t num_nodes, int32_t dim, const int32_t* centers, int64_t num_centers, const float* bias,
+                     float scale, void* scores_out, int32_t dtype, void* ws, size_t ws_bytes, void* stream);
+
+/* --------------------------------------------------------------------------
+ * gs_beam_select -- the best continuations of walks, as a beam search takes them: row
+ *   r = g * beams + b of scores is walk b of group g, with the log-probability logp[r] so far.
+ *   Candidate (b, j) has   p = logp[r] + s_rj - log sum_i exp(s_ri)      in fp64,
+ *   and of each group's the `width` first are taken, in this order: larger p; lower b; larger
+ *   score; lower j.
+ *   scores [groups * beams][n] of dtype GS_F32 | GS_BF16 | GS_F16, aligned to its element;
+ *   -infinity and NaN leave a node out (of the sum too); where +infinity is among a row's
+ *   scores, the nodes that have it share its probability.  logp float[groups * beams]:
+ *   -infinity or NaN: there is no such walk, its scores are not looked at.
+ *   ended  uint8[groups * beams] or NULL: a walk that has ended (not 0) is one candidate, itself:
+ *   node -1 and p = logp[r]; its scores are not looked at.
+ *   parents_out, nodes_out int32[groups][width], logp_out float[groups][width] (p, rounded
+ *   once): b, j and p.  Where a group has fewer candidates: -1, -1 and -infinity.
+ *   p is that of the definition to 2e-14 (1 + |p| + log n): candidates of different walks nearer
+ *   than that may change places.  Same answer on every run, and for equal rows.
+ *   1 <= n < 2^31, 1 <= beams, width <= 256, groups * beams < 2^22.  Errors: GS_EINVAL,
+ *   GS_EOVERFLOW for more rows.
+ *
+ * gs_beam_reorder -- what is kept for each walk follows the choice: row g * width + k of
+ *   `out` becomes row g * beams + parents[g][k] of `data`, for each state of the list, a HOST
+ *   array (read during the call).  A parent outside [0, beams) leaves its row as it is.
+ *   out == NULL (or == data): in place, with width == beams; rows that stay are not moved.
+ *   append_at >= 0: nodes[g][k] is then written at this byte of the row, as int32 (walks of
+ *   int32[len]: 4 * position; -1, behind a walk that has ended, as gs_random_walk writes it);
+ *   a multiple of 4, as row_bytes and both addresses are then.  -1: nothing is.
+ *   data [groups * beams][row_bytes], out [groups * width][row_bytes]; no state may overlap
+ *   another's out, nor its own out its data otherwise.  beams, width at most 256,
+ *   groups * max(beams, width) < 2^22 (GS_EOVERFLOW), row_bytes >= 0 below 2^40.
+ * ------------------------------------------------------------------------ */
+size_t gs_beam_select_workspace_bytes(int64_t groups, int32_t beams, int64_t n, int32_t width, int32_t dtype);
+int32_t gs_beam_select(const void* scores, int64_t groups, int32_t beams, int64_t n, int32_t dtype, const float* logp,
+                       const uint8_t* ended, int32_t width, int32_t* parents_out, int32_t* nodes_out, float* logp_out, void* ws,
+                       size_t ws_bytes, void* stream);
+typedef struct {
+  void* data;
+  void* out;           /* or NULL: in place                 */
+  int64_t row_bytes;
+  int64_t append_at;   /* byte of a row, or -1              */
+} gs_state;
+int32_t gs_beam_reorder(const gs_state* list, int32_t num_states, int64_t groups, int32_t beams, int32_t width,
+                        const int32_t* parents, const int32_t* nodes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -37,6 +37,8 @@ EXPORTS = (
     "gs_softmax_loss_workspace_bytes", "gs_softmax_loss", "gs_scores_workspace_bytes", "gs_scores",
     "gs_sample_scores_workspace_bytes", "gs_sample_scores",
     "gs_clip_grads_workspace_bytes", "gs_clip_grads",
+    "gs_q8_pitch", "gs_q8_scale_pitch", "gs_quantize_rows", "gs_scores_q8_workspace_bytes", "gs_scores_q8",
+    "gs_beam_select_workspace_bytes", "gs_beam_select", "gs_beam_reorder",
 )
 
 
@@ -62,6 +64,10 @@ class AliasStruct(C.Structure):
 
 class TensorStruct(C.Structure):
     _fields_ = [("data", C.c_void_p), ("out", C.c_void_p), ("count", C.c_int64), ("dtype", C.c_int32)]
+
+
+class StateStruct(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("out", C.c_void_p), ("row_bytes", C.c_int64), ("append_at", C.c_int64)]
 
 
 _lib = None
@@ -694,3 +700,150 @@ def gs_clip_grads(grads, max_norm: float, norm_out=None, ws=None):
                              C.c_size_t(ws.numel()), _stream())
     _check(rc, "gs_clip_grads")
     return norm_out
+
+
+GS_Q8_MAX_DIM = 8192
+
+
+def _one_device(dev, **tensors):
+    """All of a call's tensors on its device, which is the current one: streams and workspaces are of that."""
+    for name, t in tensors.items():
+        if isinstance(t, torch.Tensor) and t.device != dev:
+            raise ValueError(f"{name} must be on {dev}, not on {t.device}")
+    if dev.type == "cuda" and dev.index != torch.cuda.current_device():
+        raise ValueError(f"{dev} must be the current device")
+
+
+class Table8:
+    """Rows of 8-bit values for answers: data float8_e4m3fn [rows, pitch], scales float8_e8m0fnu [rows, scale pitch], a scale for
+    each block of 128 of the `dim` columns (see gs.h).  ``Table8.empty`` makes room for one."""
+
+    def __init__(self, data: torch.Tensor, scales: torch.Tensor, dim: int):
+        _dev(data, torch.float8_e4m3fn, "data")
+        _dev(scales, torch.float8_e8m0fnu, "scales")
+        pitch, scale_pitch = self.pitches(dim)
+        if data.dim() != 2 or data.shape[1] != pitch or tuple(scales.shape) != (data.shape[0], scale_pitch):
+            raise ValueError(f"rows of {dim} columns are data [rows, {pitch}] and scales [rows, {scale_pitch}]")
+        if data.device != scales.device:
+            raise ValueError("data and scales must be on one device")
+        self.data, self.scales, self.dim, self.num_nodes, self.device = data, scales, int(dim), int(data.shape[0]), data.device
+
+    @staticmethod
+    def pitches(dim: int):
+        if not 1 <= dim <= GS_Q8_MAX_DIM:
+            raise ValueError(f"dim must be from 1 to {GS_Q8_MAX_DIM}")
+        blocks = -(-dim // 128)
+        return -(-dim // 16) * 16, blocks if blocks <= 2 else -(-blocks // 4) * 4
+
+    @classmethod
+    def empty(cls, num_nodes: int, dim: int, device):
+        pitch, scale_pitch = cls.pitches(dim)
+        return cls(torch.empty(num_nodes, pitch, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn),
+                   torch.empty(num_nodes, scale_pitch, dtype=torch.uint8, device=device).view(torch.float8_e8m0fnu), dim)
+
+
+def gs_quantize_rows(table, ids=None, count=None, out=None) -> Table8:
+    """table [nodes, dim] as a Table8: all of it, or (with ids int32 [n], and out) the rows ids, the others as they are."""
+    if table.dim() != 2:
+        raise ValueError("table must be [nodes, dim]")
+    dtype = _table_dtype(table)
+    num_nodes, dim = int(table.shape[0]), int(table.shape[1])
+    _one_device(table.device, out=None if out is None else out.data, ids=ids, count=count)
+    if out is None:
+        if ids is not None:
+            raise ValueError("rows by their ids are written to an existing copy: pass out")
+        out = Table8.empty(num_nodes, dim, table.device)
+    if out.num_nodes != num_nodes or out.dim != dim:
+        raise ValueError(f"out must have {num_nodes} rows of {dim} columns")
+    n = num_nodes if ids is None else int(ids.numel())
+    rc = lib().gs_quantize_rows(_dev(table, None, "table"), C.c_int64(num_nodes), C.c_int32(dim), C.c_int32(dtype),
+                                _dev(ids, torch.int32, "ids"), C.c_int64(n), _dev(count, torch.int64, "count"), _dev(out.data),
+                                _dev(out.scales), _stream())
+    _check(rc, "gs_quantize_rows")
+    return out
+
+
+def gs_scores_q8_workspace_bytes(num_centers: int, num_nodes: int, dim: int) -> int:
+    return int(lib().gs_scores_q8_workspace_bytes(C.c_int64(num_centers), C.c_int64(num_nodes), C.c_int32(dim)))
+
+
+def gs_scores_q8(t_in: Table8, t_out: Table8, centers, bias=None, scale: float = 1.0, dtype=torch.float32, out=None, ws=None):
+    """[n, nodes] of dtype (float32, bfloat16, float16): scale * <row centers[i] of t_in, row j of t_out> + bias[j]."""
+    if t_in.dim != t_out.dim:
+        raise ValueError("t_in and t_out must have the same dim")
+    if bias is not None and tuple(bias.shape) != (t_out.num_nodes,):
+        raise ValueError("bias must have one value per row of t_out")
+    n, dev = int(centers.numel()), t_in.device
+    _one_device(dev, t_out=t_out.data, centers=centers, bias=bias, out=out, ws=ws)
+    out = _out(out, (n, t_out.num_nodes), dtype, dev, "out")
+    if ws is None:
+        ws = _workspace(gs_scores_q8_workspace_bytes(n, t_out.num_nodes, t_out.dim), dev)
+    rc = lib().gs_scores_q8(
+        _dev(t_in.data), _dev(t_in.scales), C.c_int64(t_in.num_nodes), _dev(t_out.data), _dev(t_out.scales), C.c_int64(t_out.num_nodes),
+        C.c_int32(t_out.dim), _dev(centers, torch.int32, "centers"), C.c_int64(n), _dev(bias, torch.float32, "bias"), C.c_float(scale),
+        _dev(out, None, "out"), C.c_int32(_table_dtype(out)), _dev(ws), C.c_size_t(ws.numel()), _stream())
+    _check(rc, "gs_scores_q8")
+    return out
+
+
+def gs_beam_select_workspace_bytes(groups: int, beams: int, n: int, width: int, dtype: int = GS_F32) -> int:
+    return int(lib().gs_beam_select_workspace_bytes(C.c_int64(groups), C.c_int32(beams), C.c_int64(n), C.c_int32(width), C.c_int32(dtype)))
+
+
+def gs_beam_select(scores, logp, beams: int, width: int, ended=None, parents_out=None, nodes_out=None, logp_out=None, ws=None):
+    """The `width` best continuations of each group of `beams` walks, from scores [groups * beams, n] and logp float32
+    [groups * beams]; ended: bool or uint8 [groups * beams].  Returns (parents, nodes int32, logp float32), [groups, width] each."""
+    if scores.dim() != 2 or beams < 1 or scores.shape[0] % beams != 0:
+        raise ValueError("scores must be [groups * beams, n]")
+    dtype = _table_dtype(scores)
+    rows, n, dev = int(scores.shape[0]), int(scores.shape[1]), scores.device
+    groups = rows // beams
+    for name, t in (("logp", logp), ("ended", ended)):
+        if t is not None and tuple(t.shape) != (rows,):
+            raise ValueError(f"{name} must have one value per row of scores")
+    if ended is not None and ended.dtype == torch.bool:
+        ended = ended.view(torch.uint8)
+    _one_device(dev, logp=logp, ended=ended, parents_out=parents_out, nodes_out=nodes_out, logp_out=logp_out, ws=ws)
+    parents_out = _out(parents_out, (groups, width), torch.int32, dev, "parents_out")
+    nodes_out = _out(nodes_out, (groups, width), torch.int32, dev, "nodes_out")
+    logp_out = _out(logp_out, (groups, width), torch.float32, dev, "logp_out")
+    if ws is None:
+        ws = _workspace(gs_beam_select_workspace_bytes(groups, beams, n, width, dtype), dev)
+    rc = lib().gs_beam_select(
+        _dev(scores, None, "scores"), C.c_int64(groups), C.c_int32(beams), C.c_int64(n), C.c_int32(dtype), _dev(logp, torch.float32, "logp"),
+        _dev(ended, torch.uint8, "ended"), C.c_int32(width), _dev(parents_out), _dev(nodes_out), _dev(logp_out), _dev(ws),
+        C.c_size_t(ws.numel()), _stream())
+    _check(rc, "gs_beam_select")
+    return parents_out, nodes_out, logp_out
+
+
+def gs_beam_reorder(states, parents, beams: int, outs=None, nodes=None, columns=None):
+    """Row g * width + k of each output becomes row g * beams + parents[g, k] of its state; a parent that is none leaves the row as it
+    is.  states: tensors [groups * beams, ...] of any type; outs: tensors [groups * width, ...], or None (also one of them): in
+    place.  columns: for each state None, or the column of an int32 state [rows, columns] at which nodes[g, k] is written."""
+    if parents.dim() != 2:
+        raise ValueError("parents must be [groups, width]")
+    groups, width = int(parents.shape[0]), int(parents.shape[1])
+    if nodes is not None and nodes.shape != parents.shape:
+        raise ValueError("nodes must have the shape of parents")
+    states, outs = list(states), [None] * len(states) if outs is None else list(outs)
+    columns = [None] * len(states) if columns is None else list(columns)
+    if len(outs) != len(states) or len(columns) != len(states):
+        raise ValueError("one output and one column per state")
+    _one_device(parents.device, nodes=nodes, **{f"states[{i}]": x for i, x in enumerate(states)}, **{f"outs[{i}]": x for i, x in enumerate(outs)})
+    array = (StateStruct * len(states))()
+    for i, (x, out, column) in enumerate(zip(states, outs, columns)):
+        data = _dev(x, None, "state")
+        if x.dim() < 1 or x.shape[0] != groups * beams:
+            raise ValueError(f"a state must have {groups * beams} rows")
+        if out is not None and (out.dtype != x.dtype or tuple(out.shape) != (groups * width, *x.shape[1:])):
+            raise ValueError("an output must have its state's type and rows")
+        if out is None and beams != width:
+            raise ValueError("in place there are as many walks as before: pass outs")
+        row_bytes = x[0].numel() * x.element_size() if groups else 0
+        if column is not None and (x.dim() != 2 or x.dtype != torch.int32 or not 0 <= column < x.shape[1] or nodes is None):
+            raise ValueError("nodes are written to a column of an int32 state [rows, columns]")
+        array[i] = StateStruct(data, None if out is None else _dev(out, None, "output"), row_bytes, -1 if column is None else 4 * column)
+    rc = lib().gs_beam_reorder(array, C.c_int32(len(states)), C.c_int64(groups), C.c_int32(beams), C.c_int32(width),
+                               _dev(parents, torch.int32, "parents"), _dev(nodes, torch.int32, "nodes"), _stream())
+    _check(rc, "gs_beam_reorder")
