@@ -594,8 +594,8 @@ int32_t gs_clip_grads(const gs_tensor* list, int32_t num_tensors, double max_nor
  *   Sums are fp32.  scores_out [num_centers][num_nodes] of dtype GS_F32 | GS_BF16 | GS_F16
  *   (one rounding, from fp32), aligned to its element.  bias, masked nodes and centres that
  *   are no row as for gs_scores; a scale NaN makes the scores of its row NaN.
- *   Same bits on every run.  Errors: GS_EINVAL, GS_EOVERFLOW for more than 2^21 - 32
- *   centres.
+ *   Same bits on every run.  Errors: GS_EINVAL, GS_EOVERFLOW for 2^21 centres and
+ *   more, or more tiles of 128 x 128 scores than a launch takes (2^31).
  * ------------------------------------------------------------------------ */
 enum { GS_Q8_MAX_DIM = 8192 };
 int32_t gs_q8_pitch(int32_t dim);
