@@ -47,13 +47,7 @@ struct OutF32 {
   static constexpr bool kExact = true;         // bf16 products of converted values
   static __device__ __forceinline__ void store4(float* p, const float* v) { __builtin_memcpy(p, v, 16); }
   static __device__ __forceinline__ void store(float* p, float v) { *p = v; }
-  // a lane's node j of rows i .. i + 3
-  static __device__ __forceinline__ void store_rows(float* out, int64_t i, int64_t j, const float* v, int64_t rows, int64_t n, int) {
-    if (j >= n) return;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (i + k < rows) out[(i + k) * n + j] = v[k];
-  }
+  static __device__ __forceinline__ void put4(float* p, const float* v) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
 };
 template <typename H>
 struct OutHalf {
@@ -65,20 +59,8 @@ struct OutHalf {
     __builtin_memcpy(p, w, 8);
   }
   static __device__ __forceinline__ void store(uint16_t* p, float v) { *p = (uint16_t)round(v); }
-  // Neighbouring lanes exchange: of two rows, the even lane writes both nodes of the first, the odd one of the second.
-  static __device__ __forceinline__ void store_rows(uint16_t* out, int64_t i, int64_t j, const float* v, int64_t rows, int64_t n, int lane) {
-    const bool odd = lane & 1;
-#pragma unroll
-    for (int k = 0; k < 4; k += 2) {
-      const float mine = odd ? v[k + 1] : v[k], give = odd ? v[k] : v[k + 1];
-      const float got = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, give), 0xb1, 0xf, 0xf, true));   // lane ^ 1
-      const int64_t row = i + k + (odd ? 1 : 0), first = j - (odd ? 1 : 0);
-      const uint32_t w = odd ? round(got) | round(mine) << 16 : round(mine) | round(got) << 16;
-      if (row >= rows) continue;
-      uint16_t* p = out + row * n + first;
-      if (first + 1 < n) __builtin_memcpy(p, &w, 4);
-      else if (first < n) *p = (uint16_t)w;
-    }
+  static __device__ __forceinline__ void put4(uint16_t* p, const float* v) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(round(v[0]) | round(v[1]) << 16, round(v[2]) | round(v[3]) << 16);
   }
 };
 struct ToBf16 {
@@ -180,11 +162,11 @@ __global__ __launch_bounds__(kThreads) void scores_kernel(ScoresArgs a) {
 
 // ---- many centres: tiles of both through LDS ---------------------------------
 // Centres are copied first: rows of whole blocks, zeros behind, so that no load looks at an id; a centre that is no row has the scale
-// NaN.  A workgroup computes TM x TN scores; a step is a block of 128 columns of TM + TN rows, which the loads write to LDS
-// themselves, a step ahead.  Such a load puts lane l's 16 bytes at base + 16 l, so rows cannot be padded: the eight pieces of a
-// row's 128 bytes are exchanged among each other by the row's number instead, which keeps reads of a piece of 32 rows off each
-// other's banks.  Here centres are the left operand: a lane holds one node's scores of 16 centres, neighbouring lanes
-// neighbouring nodes, and 32 lanes write 128 bytes of an fp32 row or 64 of a 16-bit one.
+// NaN.  A workgroup computes TN x TC scores in steps of 64 columns, half a block: the loads write rows' 64 bytes to LDS themselves,
+// three steps ahead.  Such a load puts lane l's 16 bytes at base + 16 l, so rows cannot be padded: the four pieces of a row are exchanged
+// among each other by a quarter of the row's number instead, so that 16 rows' pieces of a read lie in different banks (four rows
+// make 256 bytes, all 64 banks).  One barrier a step.
+// The scores go out through LDS as well, as pieces of 16 bytes of whole rows.
 
 struct Copied {                                // of the centres, in the workspace
   uint8_t* q;                                  // [padded centres][128 * blocks]
@@ -218,183 +200,209 @@ __global__ __launch_bounds__(64) void copy_centers_kernel(ScoresArgs a, Copied t
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t range_of(const void* base, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00027000);
 }
+template <int LOADS>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(LOADS < 64, "the counter's range");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LOADS) : "memory");
+}
+__device__ __forceinline__ void meet() {
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 constexpr int kOutside = 1 << 30;              // of every range: read as zeros
+constexpr int kStep = 64;                      // columns
+constexpr int kStages = 4;                     // steps in LDS
 
-template <typename O, int MB, int NB, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(ScoresArgs a, Copied in, int64_t tiles_m, int64_t tiles_n) {
-  constexpr int TM = 32 * MB * WM, TN = 32 * NB * WN, kWaves = WM * WN;
-  constexpr int kChunks = (TM + TN) / 8, kLoads = kChunks / kWaves;      // of 1 KB: eight rows
-  static_assert(kChunks % kWaves == 0 && (TM / 8) % kLoads == 0, "a wave's chunks are of one operand");
-  __shared__ __attribute__((aligned(16))) uint8_t stage_m[2][TM * kBlock], stage_n[2][TN * kBlock];
-  __shared__ __attribute__((aligned(16))) int32_t tops[TM];
+template <typename O, int NA, int NC, int WA, int WC>
+__global__ __launch_bounds__(64 * WA * WC, 2) void tile_kernel(ScoresArgs a, Copied in, int64_t tiles_c, int64_t tiles_n) {
+  typedef typename O::elem elem;
+  constexpr int S = kStages, TN = 32 * NA * WA, TC = 32 * NC * WC, kWaves = WA * WC;
+  constexpr int kLoads = (TN + TC) / 16 / kWaves;                        // of 1 KB: sixteen rows
+  constexpr int kPer = 16 / (int)sizeof(elem), kRowBytes = TN * (int)sizeof(elem) + 16, kRound = 32 * WC;   // of scores in LDS
+  constexpr int kStageBytes = S * (TN + TC) * kStep, kBytes = kStageBytes > kRound * kRowBytes ? kStageBytes : kRound * kRowBytes;
+  static_assert((TN / 16) % kLoads == 0 && kLoads * 16 * kWaves == TN + TC, "a wave's loads are of one operand");
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kBytes];
+  __shared__ __attribute__((aligned(16))) int32_t side_top[TN];
+  __shared__ __attribute__((aligned(16))) float side_bias[TN];
+  uint8_t* const lds_c = lds + S * TN * kStep;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), at = lane & 31, half = lane >> 5;
-  const int wm = wave / WN, wn = wave % WN;
+  const int wa = wave % WA, wc = wave / WA;
 
   // Consecutive workgroups go round the eight XCDs: each of them gets neighbouring tiles, eight of nodes at a time, so that what 32
   // compute units read at once is in their L2.
-  const int64_t tiles = tiles_m * tiles_n, per = (tiles + 7) / 8;
+  const int64_t tiles = tiles_c * tiles_n, per = (tiles + 7) / 8;
   const int64_t t = (int64_t)(blockIdx.x % 8) * per + blockIdx.x / 8;
   if (blockIdx.x / 8 >= per || t >= tiles) return;
-  const int64_t group = t / (8 * tiles_m), left = min((int64_t)8, tiles_n - 8 * group), in_group = t - group * 8 * tiles_m;
-  const int64_t m0 = in_group / left * TM, n0 = (8 * group + in_group % left) * TN;
+  const int64_t group = t / (8 * tiles_c), left = min((int64_t)8, tiles_n - 8 * group), in_group = t - group * 8 * tiles_c;
+  const int64_t c0 = in_group / left * TC, n0 = (8 * group + in_group % left) * TN;
+  const int nodes = (int)min((int64_t)TN, a.num_nodes - n0);
 
-  const bool of_centers = wave * kLoads < TM / 8;
-  const int64_t rows = of_centers ? (int64_t)TM : min((int64_t)TN, a.num_nodes - n0);
-  const int pitch = of_centers ? in.pitch : a.pitch;
-  const __amdgpu_buffer_rsrc_t range = range_of(of_centers ? in.q + m0 * in.pitch : a.q_out + n0 * a.pitch, (int)rows * pitch);
-  // the rows of a wave's loads are eight apart: one place in the row, and one exchange
-  const int piece = ((lane & 7) ^ (lane >> 3)) * 16, first_row = wave * kLoads * 8 - (of_centers ? 0 : TM);
-  const int place = (first_row + (lane >> 3)) * pitch + piece;
-  auto issue = [&](int block, int buf) {
-    const int from = block * kBlock + piece < pitch ? place + block * kBlock : kOutside;
-#pragma unroll
-    for (int n = 0; n < kLoads; ++n)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(range, (__attribute__((address_space(3))) void*)((of_centers ? stage_m[buf] : stage_n[buf]) + first_row * kBlock + n * 1024), 16,
-                                               from + n * 8 * pitch, 0, 0, 0);
+  const bool of_nodes = wave * kLoads < TN / 16;
+  const int first_row = wave * kLoads * 16 - (of_nodes ? 0 : TN), pitch = of_nodes ? a.pitch : in.pitch;
+  const __amdgpu_buffer_rsrc_t range = range_of(of_nodes ? a.q_out + n0 * a.pitch : in.q + c0 * in.pitch, (of_nodes ? nodes : TC) * pitch);
+  uint8_t* const to = (of_nodes ? lds : lds_c) + first_row * kStep;
+  const int to_next = (of_nodes ? TN : TC) * kStep;
+  const int piece = ((lane & 3) ^ (lane >> 4)) * 16, row_at = (first_row + (lane >> 2)) * pitch;
+  auto issue = [&](int step, int buf, int n) {
+    const int col = step * kStep + piece;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(range, (__attribute__((address_space(3))) void*)(to + buf * to_next + n * 1024), 16,
+                                             col < pitch ? row_at + col + n * 16 * pitch : kOutside, 0, 0, 0);
   };
-  issue(0, 0);
-
-  const uint8_t *scales_m = in.scales + m0 * in.scale_pitch, *scales_n = a.scales_out + n0 * a.scale_pitch;
-  int scale_n[NB];
-  const int scale_m = (wm * MB * 32 + at) * in.scale_pitch;
 #pragma unroll
-  for (int n = 0; n < NB; ++n) scale_n[n] = min((wn * NB + n) * 32 + at, (int)min(a.num_nodes - n0, (int64_t)TN) - 1) * a.scale_pitch;
-  auto of_nodes = [&](int n, int block) {      // the scales of four blocks from `block` on
-    const uint8_t* p = scales_n + scale_n[n];
+  for (int s = 0; s < S - 1; ++s)
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) issue(s, s, n);
+
+  // ---- scales: of a lane's rows, four blocks at a time
+  const uint8_t *scales_c = in.scales + c0 * in.scale_pitch, *scales_n = a.scales_out + n0 * a.scale_pitch;
+  int scale_n[NA];
+  const int scale_c = (wc * NC * 32 + at) * in.scale_pitch;
+#pragma unroll
+  for (int m = 0; m < NA; ++m) scale_n[m] = min((wa * NA + m) * 32 + at, nodes - 1) * a.scale_pitch;
+  auto four = [&](int m, int block) {
+    const uint8_t* p = scales_n + scale_n[m];
     if (a.scale_pitch >= 4) return *reinterpret_cast<const uint32_t*>(p + block);
     return (uint32_t)p[0] | (a.scale_pitch == 2 ? (uint32_t)p[1] << 8 : 0u);
   };
-  int top_m[MB], top_n[NB];
+  int top_n[NA], top_c[NC];
   if (O::kExact) {
 #pragma unroll
-    for (int m = 0; m < MB; ++m) top_m[m] = in.top[m0 + (wm * MB + m) * 32 + at];
+    for (int n = 0; n < NC; ++n) top_c[n] = in.top[c0 + (wc * NC + n) * 32 + at];
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      top_n[n] = 0;
+    for (int m = 0; m < NA; ++m) {
+      top_n[m] = 0;
       for (int b = 0; b < a.blocks; b += 4) {
-        const uint32_t w = of_nodes(n, b);
+        const uint32_t w = four(m, b);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int byte = (int)((w >> (8 * k)) & 255u);
-          top_n[n] = max(top_n[n], byte == 255 ? 0 : byte);
+          top_n[m] = max(top_n[m], byte == 255 ? 0 : byte);
         }
       }
+      if (wc == 0 && half == 0) side_top[(wa * NA + m) * 32 + at] = top_n[m];
     }
-    for (int i = tid; i < TM; i += 64 * kWaves) tops[i] = in.top[m0 + i];
   }
-
-  // reads: piece 4 s + 2 half + j of a row
-  int at_m[2][2], at_n[2][2];
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const int in_row = ((4 * (c >> 1) + 2 * half + (c & 1)) ^ (at & 7)) * 16;
-    at_m[c >> 1][c & 1] = (wm * MB * 32 + at) * kBlock + in_row;
-    at_n[c >> 1][c & 1] = (wn * NB * 32 + at) * kBlock + in_row;
-  }
-  acc16 acc[MB][NB];
-#pragma unroll
-  for (int m = 0; m < MB; ++m)
-#pragma unroll
-    for (int n = 0; n < NB; ++n) acc[m][n] = acc16{};
-  uint32_t sm[MB], sn[NB], next_m[MB], next_n[NB];      // the scales of four blocks, and of the next four
+  if (a.bias)
+    for (int i = tid; i < nodes; i += 64 * kWaves) side_bias[i] = a.bias[n0 + i];
+  uint32_t sn[NA], sc[NC], next_n[NA], next_c[NC];
   auto fetch_scales = [&](int block) {
 #pragma unroll
-    for (int m = 0; m < MB; ++m) next_m[m] = *reinterpret_cast<const uint32_t*>(scales_m + scale_m + m * 32 * in.scale_pitch + block);
+    for (int n = 0; n < NC; ++n) next_c[n] = *reinterpret_cast<const uint32_t*>(scales_c + scale_c + n * 32 * in.scale_pitch + block);
 #pragma unroll
-    for (int n = 0; n < NB; ++n) next_n[n] = of_nodes(n, block);
+    for (int m = 0; m < NA; ++m) next_n[m] = four(m, block);
   };
   fetch_scales(0);
 
-  auto step = [&](int block, int buf) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
+  // ---- products: pieces 2 half and 2 half + 1 of a row
+  const int in_row = ((2 * half) ^ ((at >> 2) & 3)) * 16;
+  const int at_n[2] = {(wa * NA * 32 + at) * kStep + in_row, (wa * NA * 32 + at) * kStep + (in_row ^ 16)};
+  const int at_c[2] = {(wc * NC * 32 + at) * kStep + in_row, (wc * NC * 32 + at) * kStep + (in_row ^ 16)};
+  acc16 acc[NA][NC];
+#pragma unroll
+  for (int m = 0; m < NA; ++m)
+#pragma unroll
+    for (int n = 0; n < NC; ++n) acc[m][n] = acc16{};
+  auto pair = [&](const uint8_t* base, const int* place, int more) {
+    const uint4 p = *reinterpret_cast<const uint4*>(base + place[0] + more), q = *reinterpret_cast<const uint4*>(base + place[1] + more);
+    return int8v{(int)p.x, (int)p.y, (int)p.z, (int)p.w, (int)q.x, (int)q.y, (int)q.z, (int)q.w};
+  };
+  auto step = [&](int k) {
+    const int buf = k % S;
+    wait_loads<(S - 2) * kLoads>();            // this step's rows; those of later ones may be under way
+    meet();
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) issue(k + S - 1, (k + S - 1) % S, n);      // where the step before was read
+    int8v x[NA], y[NC];
+#pragma unroll
+    for (int n = 0; n < NC; ++n) y[n] = pair(lds_c + buf * TC * kStep, at_c, n * 32 * kStep);
+#pragma unroll
+    for (int m = 0; m < NA; ++m) x[m] = pair(lds + buf * TN * kStep, at_n, m * 32 * kStep);
+    if (O::kExact) {
+      float fx[NA], fy[NC];
+#pragma unroll
+      for (int m = 0; m < NA; ++m) fx[m] = relative((int)(sn[m] & 255u), top_n[m]);
+#pragma unroll
+      for (int n = 0; n < NC; ++n) fy[n] = relative((int)(sc[n] & 255u), top_c[n]);
+#pragma unroll
+      for (int w = 0; w < 8; w += 2) {
+        bf8 u[NA], v[NC];
+#pragma unroll
+        for (int n = 0; n < NC; ++n) v[n] = widen(y[n][w], y[n][w + 1], fy[n]);
+#pragma unroll
+        for (int m = 0; m < NA; ++m) {
+          u[m] = widen(x[m][w], x[m][w + 1], fx[m]);
+#pragma unroll
+          for (int n = 0; n < NC; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u[m], v[n], acc[m][n], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int m = 0; m < NA; ++m)
+#pragma unroll
+        for (int n = 0; n < NC; ++n)
+          acc[m][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x[m], y[n], acc[m][n], 0, 0, 0, (int)sn[m], 0, (int)sc[n]);
+    }
+  };
+  static_assert(kBlock == 2 * kStep, "two steps a block");
+  for (int block = 0; block < a.blocks; ++block) {
     if ((block & 3) == 0) {
 #pragma unroll
-      for (int m = 0; m < MB; ++m) sm[m] = next_m[m];
+      for (int m = 0; m < NA; ++m) sn[m] = next_n[m];
 #pragma unroll
-      for (int n = 0; n < NB; ++n) sn[n] = next_n[n];
+      for (int n = 0; n < NC; ++n) sc[n] = next_c[n];
       if (block + 4 < a.blocks) fetch_scales(block + 4);
     }
-    if (block + 1 < a.blocks) issue(block + 1, buf ^ 1);
-    __builtin_amdgcn_sched_barrier(0);
-    auto read = [&](const uint8_t* p) {
-      const uint4 w = *reinterpret_cast<const uint4*>(p);
-      return w;
-    };
+    step(2 * block);
+    step(2 * block + 1);
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      if (s > 0) __builtin_amdgcn_sched_barrier(0);
-      int8v x[MB], y[NB];
+    for (int m = 0; m < NA; ++m) sn[m] >>= 8;
 #pragma unroll
-      for (int m = 0; m < MB; ++m) {
-        const uint4 p = read(stage_m[buf] + at_m[s][0] + m * 32 * kBlock), q = read(stage_m[buf] + at_m[s][1] + m * 32 * kBlock);
-        x[m] = int8v{(int)p.x, (int)p.y, (int)p.z, (int)p.w, (int)q.x, (int)q.y, (int)q.z, (int)q.w};
-      }
-#pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        const uint4 p = read(stage_n[buf] + at_n[s][0] + n * 32 * kBlock), q = read(stage_n[buf] + at_n[s][1] + n * 32 * kBlock);
-        y[n] = int8v{(int)p.x, (int)p.y, (int)p.z, (int)p.w, (int)q.x, (int)q.y, (int)q.z, (int)q.w};
-      }
-      if (O::kExact) {
-#pragma unroll
-        for (int k = 0; k < 8; k += 2) {
-          bf8 u[MB], v[NB];
-#pragma unroll
-          for (int m = 0; m < MB; ++m) u[m] = widen(x[m][k], x[m][k + 1], relative((int)(sm[m] & 255u), top_m[m]));
-#pragma unroll
-          for (int n = 0; n < NB; ++n) v[n] = widen(y[n][k], y[n][k + 1], relative((int)(sn[n] & 255u), top_n[n]));
-#pragma unroll
-          for (int m = 0; m < MB; ++m)
-#pragma unroll
-            for (int n = 0; n < NB; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u[m], v[n], acc[m][n], 0, 0, 0);
-        }
-      } else {
-#pragma unroll
-        for (int m = 0; m < MB; ++m)
-#pragma unroll
-          for (int n = 0; n < NB; ++n)
-            acc[m][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x[m], y[n], acc[m][n], 0, 0, 0, (int)sm[m], 0, (int)sn[n]);
-      }
-    }
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int m = 0; m < MB; ++m) sm[m] >>= 8;
-#pragma unroll
-    for (int n = 0; n < NB; ++n) sn[n] >>= 8;
-  };
-  int block = 0;
-  for (; block + 2 <= a.blocks; block += 2) {
-    step(block, 0);
-    step(block + 1, 1);
+    for (int n = 0; n < NC; ++n) sc[n] >>= 8;
   }
-  if (block < a.blocks) step(block, 0);
 
-  // ---- scores: register 4 g + k of a block is centre 8 g + 4 half + k, a lane's node is n0 + ... + at
-  typedef typename O::elem elem;
+  // ---- scores: register 4 g + k of a block is node 8 g + 4 half + k, a lane's centre is ... + at
   elem* out = static_cast<elem*>(a.out);
-  const int64_t row0 = m0 + wm * MB * 32 + 4 * half;
 #pragma unroll
-  for (int n = 0; n < NB; ++n) {
-    const int64_t j = n0 + (wn * NB + n) * 32 + at;
-    const float bias = a.bias && j < a.num_nodes ? a.bias[j] : 0.0f;
-    const bool masked = bias == -INFINITY;
+  for (int n = 0; n < NC; ++n) {
+    wait_loads<0>();                           // also what was asked for beyond the last step: it lands where the scores go
+    meet();
 #pragma unroll
-    for (int m = 0; m < MB; ++m)
+    for (int m = 0; m < NA; ++m)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        float v[4];
+        const int j = (wa * NA + m) * 32 + 8 * g + 4 * half;
+        float v[4], bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         int top[4] = {0, 0, 0, 0};
-        if (O::kExact) __builtin_memcpy(top, &tops[(wm * MB + m) * 32 + 8 * g + 4 * half], 16);
+        if (O::kExact) __builtin_memcpy(top, &side_top[j], 16);
+        if (a.bias) __builtin_memcpy(bias, &side_bias[j], 16);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           float z = acc[m][n][4 * g + k];
-          if (O::kExact) z = ldexpf(z, top[k] + top_n[n] - 254);
-          z = a.scale * z + bias;
-          v[k] = masked ? -INFINITY : z;
+          if (O::kExact) z = ldexpf(z, top[k] + top_c[n] - 254);
+          z = a.scale * z + bias[k];
+          v[k] = bias[k] == -INFINITY ? -INFINITY : z;
         }
-        const int64_t i = row0 + m * 32 + 8 * g;
-        O::store_rows(out, i, j, v, a.num_centers, a.num_nodes, lane);
+        O::put4(reinterpret_cast<elem*>(lds + (wc * 32 + at) * kRowBytes) + j, v);
       }
+    wait_loads<0>();
+    meet();
+    constexpr int kLanes = TN / kPer;          // of a row
+    for (int p = tid; p < kRound * kLanes; p += 64 * kWaves) {
+      const int r = p / kLanes, j = (p - r * kLanes) * kPer;
+      const int64_t i = c0 + (r / 32 * NC + n) * 32 + r % 32;
+      const uint4 w = *reinterpret_cast<const uint4*>(lds + r * kRowBytes + j * (int)sizeof(elem));
+      if (i >= a.num_centers || j >= nodes) continue;
+      elem* row = out + i * a.num_nodes + n0 + j;
+      if (j + kPer <= nodes) {
+        __builtin_memcpy(row, &w, 16);
+      } else {
+        elem e[kPer];
+        __builtin_memcpy(e, &w, 16);
+#pragma unroll
+        for (int k = 0; k < kPer; ++k)
+          if (j + k < nodes) row[k] = e[k];
+      }
+    }
   }
 }
 
@@ -435,11 +443,11 @@ ScoresPlan plan_scores(void* ws, int64_t num_centers, int32_t dim) {
   return p;
 }
 
-template <typename O, int MB, int NB, int WM, int WN>
+template <typename O, int NA, int NC, int WA, int WC>
 int32_t run_tiles(const ScoresArgs& a, const Copied& in, hipStream_t s) {
-  const int64_t m = ceil_div(a.num_centers, 32 * MB * WM), n = ceil_div(a.num_nodes, 32 * NB * WN);
-  if (ceil_div(m * n, 8) * 8 > (int64_t)INT32_MAX) return GS_EOVERFLOW;
-  tile_kernel<O, MB, NB, WM, WN><<<dim3((unsigned)(ceil_div(m * n, 8) * 8)), 64 * WM * WN, 0, s>>>(a, in, m, n);
+  const int64_t c = ceil_div(a.num_centers, 32 * NC * WC), n = ceil_div(a.num_nodes, 32 * NA * WA);
+  if (ceil_div(c * n, 8) * 8 > (int64_t)INT32_MAX) return GS_EOVERFLOW;
+  tile_kernel<O, NA, NC, WA, WC><<<dim3((unsigned)(ceil_div(c * n, 8) * 8)), 64 * WA * WC, 0, s>>>(a, in, c, n);
   GS_LAUNCH_CHECK();
   return GS_OK;
 }
@@ -453,7 +461,8 @@ int32_t run_scores(const ScoresArgs& a, const ScoresPlan& p, hipStream_t s) {
   }
   copy_centers_kernel<<<dim3((unsigned)p.padded), 64, 0, s>>>(a, p.in);
   GS_LAUNCH_CHECK();
-  return run_tiles<O, 2, 2, 2, 2>(a, p.in, s);
+  if (a.num_centers <= 128) return run_tiles<O, 2, 2, 2, 2>(a, p.in, s);
+  return run_tiles<O, 4, 2, 2, 4>(a, p.in, s);
 }
 
 }  // namespace
