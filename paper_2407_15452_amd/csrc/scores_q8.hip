@@ -17,6 +17,7 @@
 #include "common.h"
 
 #include <cmath>
+#include <type_traits>
 
 namespace gs {
 namespace {
@@ -209,6 +210,17 @@ __device__ __forceinline__ void meet() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
+// 16 bytes of a row of scores; rows begin at any element.  One store: types of their own, not a copy of bytes, which the compiler
+// takes apart where parts of it are stored elsewhere too.
+typedef uint32_t of_words __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t of_halves __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ void put_piece(float* to, const uint4& w) { *reinterpret_cast<of_words*>(to) = (of_words){w.x, w.y, w.z, w.w}; }
+__device__ __forceinline__ void put_piece(uint16_t* to, const uint4& w) { *reinterpret_cast<of_halves*>(to) = (of_halves){w.x, w.y, w.z, w.w}; }
+// 16 bytes of LDS from any element on
+__device__ __forceinline__ uint4 read_loose(const uint8_t* from) {
+  const of_halves w = *reinterpret_cast<const of_halves*>(from);
+  return make_uint4(w.x, w.y, w.z, w.w);
+}
 constexpr int kOutside = 1 << 30;              // of every range: read as zeros
 constexpr int kStep = 64;                      // columns
 constexpr int kStages = 4;                     // steps in LDS
@@ -387,22 +399,298 @@ __global__ __launch_bounds__(64 * WA * WC, 2) void tile_kernel(ScoresArgs a, Cop
     wait_loads<0>();
     meet();
     constexpr int kLanes = TN / kPer;          // of a row
-    for (int p = tid; p < kRound * kLanes; p += 64 * kWaves) {
-      const int r = p / kLanes, j = (p - r * kLanes) * kPer;
-      const int64_t i = c0 + (r / 32 * NC + n) * 32 + r % 32;
-      const uint4 w = *reinterpret_cast<const uint4*>(lds + r * kRowBytes + j * (int)sizeof(elem));
-      if (i >= a.num_centers || j >= nodes) continue;
-      elem* row = out + i * a.num_nodes + n0 + j;
-      if (j + kPer <= nodes) {
-        __builtin_memcpy(row, &w, 16);
-      } else {
-        elem e[kPer];
-        __builtin_memcpy(e, &w, 16);
-#pragma unroll
-        for (int k = 0; k < kPer; ++k)
-          if (j + k < nodes) row[k] = e[k];
+    if (nodes == TN) {
+      for (int p = tid; p < kRound * kLanes; p += 64 * kWaves) {
+        const int r = p / kLanes, j = (p - r * kLanes) * kPer;
+        const int64_t i = c0 + (r / 32 * NC + n) * 32 + r % 32;
+        const uint4 w = *reinterpret_cast<const uint4*>(lds + r * kRowBytes + j * (int)sizeof(elem));
+        if (i < a.num_centers) put_piece(out + i * a.num_nodes + n0 + j, w);
+      }
+    } else {
+      for (int p = tid; p < kRound * TN; p += 64 * kWaves) {
+        const int r = p / TN, j = p - r * TN;
+        const int64_t i = c0 + (r / 32 * NC + n) * 32 + r % 32;
+        if (i < a.num_centers && j < nodes) out[i * a.num_nodes + n0 + j] = reinterpret_cast<const elem*>(lds + r * kRowBytes)[j];
       }
     }
+  }
+}
+
+// ---- narrow rows: centres kept in registers, nodes streamed ---------------------
+// One or two blocks (256 columns): the scores are more bytes than the rows, and writing them is the work.  Four waves keep 32 * KC
+// centres each, as the right operand; a fifth asks for the nodes' rows, 64 at a time and three tiles ahead, with their scales and
+// biases, into LDS, and is the only one that waits for memory: the others' stores are never waited for.  One barrier a tile.  A
+// workgroup has a range of neighbouring nodes: what it writes of a row grows along the row, so that lines that two tiles share
+// meet in L2.  A wave turns 16 centres' scores in LDS of its own and writes them as pieces of 16 bytes of whole rows.
+
+template <typename O, int BL, bool CARRY>
+struct Strip {
+  static constexpr int kWaves = 4, kThreads = 64 * (kWaves + 1);                    // and the one that loads
+  static constexpr int kSize = (int)sizeof(typename O::elem);
+  static constexpr int kNodes = 64, kSlots = BL == 1 && !CARRY ? 4 : 3, kAhead = kSlots - 1;
+  static constexpr int kRows = kNodes * kBlock * BL, kSlotBytes = kRows + 512;      // rows, scales, biases
+  static constexpr int kLoads = kRows / 1024 + 2;
+  static constexpr int kPer = 16 / kSize, kLanes = kNodes / kPer;                   // of a row of scores
+  static constexpr int kRowBytes = kNodes * kSize + (CARRY ? 128 : 0) + 16;
+  static constexpr int kTurn = BL == 1 || CARRY ? 32 : 16;                          // rows that a wave turns at once
+};
+
+template <typename O, int BL, int KC, bool CARRY>
+__global__ __launch_bounds__(320, 2) void strip_kernel(ScoresArgs a, int64_t groups_c, int64_t ranges, int64_t tiles_per_range) {
+  typedef Strip<O, BL, CARRY> S;
+  static_assert(!CARRY || KC == 1, "a wave keeps what is left of each of its rows");
+  typedef typename O::elem elem;
+  __shared__ __attribute__((aligned(16))) uint8_t slots[S::kSlots][S::kSlotBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t turn[S::kWaves][S::kTurn * S::kRowBytes];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), at = lane & 31, half = lane >> 5;
+  // XCD x has an eighth of the nodes.  Its workgroups take tiles in turn; with CARRY each has a range of neighbouring ones.
+  const int64_t all_tiles = (a.num_nodes + S::kNodes - 1) / S::kNodes, xcd = blockIdx.x % 8, u = blockIdx.x / 8, group = u % groups_c;
+  const int64_t of_xcd = min((xcd + 1) * tiles_per_range, all_tiles);      // the end of its tiles
+  const int64_t chunk = (tiles_per_range + ranges - 1) / ranges, every = CARRY ? 1 : ranges;
+  const int64_t first = xcd * tiles_per_range + u / groups_c * (CARRY ? chunk : 1), last = CARRY ? min(first + chunk, of_xcd) : of_xcd;
+  if (first >= last) return;
+
+  if (wave == S::kWaves) {                     // the wave that loads
+    const int row = (lane >> 3) * a.pitch, piece = ((lane & 7) ^ (lane >> 4)) * 16;
+    auto issue = [&](int64_t t) {
+      uint8_t* slot = slots[(t - first) / every % S::kSlots];
+      const int64_t n0 = t * S::kNodes;
+      const int nodes = (int)max((int64_t)0, min((int64_t)S::kNodes, a.num_nodes - n0));
+      const int64_t from = t < last ? n0 : 0;  // beyond the range: nothing, but as many loads
+      const int rows = t < last ? nodes : 0;
+      const __amdgpu_buffer_rsrc_t q = range_of(a.q_out + from * a.pitch, rows * a.pitch);
+#pragma unroll
+      for (int b = 0; b < BL; ++b)
+#pragma unroll
+        for (int c = 0; c < S::kNodes / 8; ++c) {
+          const int col = b * kBlock + (piece ^ (c & 1 ? 64 : 0));
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(q, (__attribute__((address_space(3))) void*)(slot + b * S::kNodes * kBlock + c * 1024), 16,
+                                                   col < a.pitch ? row + c * 8 * a.pitch + col : kOutside, 0, 0, 0);
+        }
+      // whole words of scales: the last one's bytes beyond the table lie in a word that the table has a part of
+      const __amdgpu_buffer_rsrc_t e = range_of(a.scales_out + from * BL, (rows * BL + 3) / 4 * 4);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(e, (__attribute__((address_space(3))) void*)(slot + S::kRows), 4, lane * 4, 0, 0, 0);
+      const __amdgpu_buffer_rsrc_t f = range_of(a.bias ? static_cast<const void*>(a.bias + from) : a.q_out, a.bias ? rows * 4 : 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(f, (__attribute__((address_space(3))) void*)(slot + S::kRows + 256), 4, lane * 4, 0, 0, 0);
+    };
+    for (int s = 0; s < S::kAhead; ++s) issue(first + s * every);
+    for (int64_t t = first; t < last; t += every) {
+      wait_loads<(S::kAhead - 1) * S::kLoads>();
+      meet();
+      issue(t + S::kAhead * every);                    // where the tile before was read
+    }
+    wait_loads<0>();                           // nothing may land in LDS after the workgroup
+    return;
+  }
+
+  // ---- centres: pieces 4 s + 2 half, + 1 of a block's eight
+  const int64_t c0 = (group * S::kWaves + wave) * 32 * KC;
+  int8v kept[O::kExact ? 1 : KC][BL * 2];
+  bf8 wide[O::kExact ? KC : 1][BL * 8];
+  int top_c[KC], scale_c[KC][BL];
+#pragma unroll
+  for (int n = 0; n < KC; ++n) {
+    const int64_t i = c0 + n * 32 + at, id = i < a.num_centers ? (int64_t)a.centers[i] : -1;
+    const bool there = id >= 0 && id < a.num_in;
+    const uint8_t *h = a.q_in + (there ? id : 0) * a.pitch, *e = a.scales_in + (there ? id : 0) * BL;
+    top_c[n] = 0;
+#pragma unroll
+    for (int b = 0; b < BL; ++b) {
+      scale_c[n][b] = there ? e[b] : 255;
+      top_c[n] = max(top_c[n], scale_c[n][b] == 255 ? 0 : scale_c[n][b]);
+    }
+#pragma unroll
+    for (int k = 0; k < BL * 2; ++k) {
+      const int8v x = load32(h, (k >> 1) * kBlock + (k & 1) * 64 + half * 32, a.pitch);
+      if (O::kExact) {
+#pragma unroll
+        for (int w = 0; w < 8; w += 2) wide[n][k * 4 + w / 2] = widen(x[w], x[w + 1], relative(scale_c[n][k >> 1], top_c[n]));
+      } else {
+        kept[n][k] = x;
+      }
+    }
+  }
+
+  float factor_c[KC];
+  bool near_c = true;
+#pragma unroll
+  for (int n = 0; n < KC; ++n) {
+    factor_c[n] = __uint_as_float((uint32_t)top_c[n] << 23) * a.scale;
+    near_c = near_c && top_c[n] - 27u <= 173u && factor_c[n] >= 0x1p-126f && factor_c[n] <= 0x1p126f;
+  }
+  near_c = __ballot(near_c) == ~0ull;
+  uint8_t* const mine = turn[wave];
+  const int rows = (int)min((int64_t)32 * KC, a.num_centers - c0);      // may be none, or fewer
+  elem* const out = static_cast<elem*>(a.out);
+  // pieces of the nodes: by half the row's number
+  int at_n[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) at_n[c] = at * kBlock + (((4 * (c >> 1) + 2 * half + (c & 1)) ^ ((at >> 1) & 7)) * 16);
+  for (int64_t t = first; t < last; t += every) {
+    meet();
+    const uint8_t* slot = slots[(t - first) / every % S::kSlots];
+    const uint8_t* side = slot + S::kRows;
+    const int64_t n0 = t * S::kNodes;
+    const int nodes = (int)min((int64_t)S::kNodes, a.num_nodes - n0);
+    acc16 acc[2][KC];
+    int byte[2][BL], top[2];
+    bool near = true;
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+#pragma unroll
+      for (int n = 0; n < KC; ++n) acc[m][n] = acc16{};
+      top[m] = 0;
+#pragma unroll
+      for (int b = 0; b < BL; ++b) {
+        byte[m][b] = side[(m * 32 + at) * BL + b];
+        top[m] = max(top[m], byte[m][b]);
+      }
+      near = near && top[m] - 27u <= 173u;
+    }
+#pragma unroll
+    for (int k = 0; k < BL * 2; ++k) {
+      int8v x[2];
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const uint8_t* from = slot + (k >> 1) * S::kNodes * kBlock + m * 32 * kBlock;
+        const uint4 p = *reinterpret_cast<const uint4*>(from + at_n[(k & 1) * 2]), q = *reinterpret_cast<const uint4*>(from + at_n[(k & 1) * 2 + 1]);
+        x[m] = int8v{(int)p.x, (int)p.y, (int)p.z, (int)p.w, (int)q.x, (int)q.y, (int)q.z, (int)q.w};
+      }
+      if (O::kExact) {
+#pragma unroll
+        for (int w = 0; w < 8; w += 2)
+#pragma unroll
+          for (int m = 0; m < 2; ++m) {
+            const bf8 u = widen(x[m][w], x[m][w + 1], relative(byte[m][k >> 1], top[m]));
+#pragma unroll
+            for (int n = 0; n < KC; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u, wide[n][k * 4 + w / 2], acc[m][n], 0, 0, 0);
+          }
+      } else {
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int n = 0; n < KC; ++n)
+            acc[m][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x[m], kept[n][k], acc[m][n], 0, 0, 0, byte[m][k >> 1], 0, scale_c[n][k >> 1]);
+      }
+    }
+    // Register 4 g + k of a block is node 8 g + 4 half + k, a lane's centre is ... + at.  The powers are factors where no product leaves
+    // the normal numbers (the sums lie within 2^-18 and 2^27), which is always but for rows of 1e-30 or 1e21, and rows of NaN.
+    const bool factors = !O::kExact || (__ballot(near) == ~0ull && near_c);
+    auto finish = [&](auto by_factors, auto with_bias) {
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int j = m * 32 + 8 * g + 4 * half;
+          float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+          uint32_t power[4] = {0, 0, 0, 0};
+          if constexpr (decltype(with_bias)::value) __builtin_memcpy(bias, side + 256 + 4 * j, 16);
+          if constexpr (O::kExact) {
+            uint32_t w[BL];
+            __builtin_memcpy(w, side + j * BL, 4 * BL);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              power[k] = BL == 1 ? (w[0] >> (8 * k)) & 255u : max((w[k * BL / 4] >> (8 * (k * BL % 4))) & 255u, (w[k * BL / 4] >> (8 * (k * BL % 4 + 1))) & 255u);
+          }
+#pragma unroll
+          for (int n = 0; n < KC; ++n)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              float z = acc[m][n][4 * g + k];
+              if constexpr (!O::kExact) {
+                z = fmaf(z, a.scale, bias[k]);
+              } else if constexpr (decltype(by_factors)::value) {
+                z = fmaf(z * __uint_as_float(power[k] << 23), factor_c[n], bias[k]);
+              } else {
+                z = fmaf(ldexpf(z, (int)power[k] + top_c[n] - 254), a.scale, bias[k]);
+              }
+              if constexpr (decltype(with_bias)::value) z = bias[k] == -INFINITY ? -INFINITY : z;
+              acc[m][n][4 * g + k] = z;
+            }
+        }
+    };
+    if (factors) {
+      if (a.bias) finish(std::true_type{}, std::true_type{});
+      else finish(std::true_type{}, std::false_type{});
+    } else {
+      if (a.bias) finish(std::false_type{}, std::true_type{});
+      else finish(std::false_type{}, std::false_type{});
+    }
+#pragma unroll
+    for (int n = 0; n < KC; ++n)
+#pragma unroll
+      for (int r = 0; r < 32 / S::kTurn; ++r) {
+        wave_fence();
+        if (S::kTurn == 32 || at / S::kTurn == r) {
+          elem* to = reinterpret_cast<elem*>(mine + at % S::kTurn * S::kRowBytes + (CARRY ? 128 : 0));
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const float v[4] = {acc[m][n][4 * g], acc[m][n][4 * g + 1], acc[m][n][4 * g + 2], acc[m][n][4 * g + 3]};
+              O::put4(to + m * 32 + 8 * g + 4 * half, v);
+            }
+        }
+        wave_fence();
+        if constexpr (CARRY) {
+          // A row's buffer: the last line's worth of the tile before, then this tile.  From the line on that holds the tile's first
+          // node, 64 scores go out as whole lines; what lies behind goes with the next tile.
+          const int row = lane / S::kLanes, piece = lane % S::kLanes * 16;
+          const uint8_t* from = mine + row * S::kRowBytes + 128 + piece;
+          elem* node = out + (c0 + row) * a.num_nodes + n0;
+          constexpr int kStep = 64 / S::kLanes;        // rows of a store
+          if (t > first && t + 1 < last) {
+#pragma unroll
+            for (int p = 0; p < 32 / kStep; ++p) {
+              const int back = (int)(reinterpret_cast<uintptr_t>(node) & 127);
+              if (row < rows - p * kStep)
+                *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(node) - back + piece) = read_loose(from + p * kStep * S::kRowBytes - back);
+              node += kStep * a.num_nodes;
+              asm("" : "+v"(node));
+            }
+          } else {
+#pragma unroll 1
+            for (int p = 0; p < 32 / kStep; ++p, node += kStep * a.num_nodes) {
+              const int back = (int)(reinterpret_cast<uintptr_t>(node) & 127);
+              for (int more = 0; more < (t + 1 < last ? 1 : 2); ++more) {       // the last tile: to its end
+                const int at0 = (piece + more * 64 * S::kSize - back) / S::kSize;      // of the piece, among the tile's nodes
+                if (row >= rows - p * kStep || at0 >= nodes) continue;
+                const uint4 w = read_loose(from + p * kStep * S::kRowBytes + more * 64 * S::kSize - back);
+                elem e[S::kPer];
+                __builtin_memcpy(e, &w, 16);
+#pragma unroll
+                for (int k = 0; k < S::kPer; ++k)
+                  if ((t > first || at0 + k >= 0) && at0 + k < (t + 1 < last ? S::kNodes : nodes)) node[at0 + k] = e[k];
+              }
+            }
+          }
+          wave_fence();
+          uint4 kept_back[4];
+#pragma unroll
+          for (int p = 0; p < 4; ++p) kept_back[p] = *reinterpret_cast<const uint4*>(mine + (p * 8 + lane / 8) * S::kRowBytes + S::kNodes * S::kSize + lane % 8 * 16);
+#pragma unroll
+          for (int p = 0; p < 4; ++p) *reinterpret_cast<uint4*>(mine + (p * 8 + lane / 8) * S::kRowBytes + lane % 8 * 16) = kept_back[p];
+          continue;
+        }
+        const int row0 = n * 32 + r * S::kTurn;
+        if (nodes == S::kNodes) {
+          const int row = lane / S::kLanes;
+          elem* to = out + (c0 + row0 + row) * a.num_nodes + n0 + lane % S::kLanes * S::kPer;
+          const uint8_t* from = mine + row * S::kRowBytes + lane % S::kLanes * 16;
+#pragma unroll
+          for (int p = 0; p < S::kTurn * S::kLanes / 64; ++p) {
+            constexpr int kStep = 64 / S::kLanes;      // rows of a store
+            if (row < rows - row0 - p * kStep) put_piece(to, *reinterpret_cast<const uint4*>(from + p * kStep * S::kRowBytes));
+            to += kStep * a.num_nodes;
+            asm("" : "+v"(to));                // one address at a time: kept for all of them they would not fit the registers
+          }
+        } else if (lane < nodes) {
+          elem* to = out + (c0 + row0) * a.num_nodes + n0 + lane;
+#pragma unroll 1
+          for (int row = 0; row < min(S::kTurn, rows - row0); ++row, to += a.num_nodes)
+            *to = reinterpret_cast<const elem*>(mine + row * S::kRowBytes)[lane];
+        }
+      }
   }
 }
 
@@ -431,7 +719,7 @@ ScoresPlan plan_scores(void* ws, int64_t num_centers, int32_t dim) {
   ScoresPlan p{};
   p.few = num_centers <= kFew;
   p.bytes = 256;
-  if (p.few) return p;
+  if (p.few || dim <= 2 * kBlock) return p;
   p.padded = ceil_div(num_centers, 256) * 256;
   const int blocks = (int)ceil_div(dim, kBlock);
   p.in.pitch = blocks * kBlock, p.in.scale_pitch = (blocks + 3) / 4 * 4;
@@ -452,6 +740,37 @@ int32_t run_tiles(const ScoresArgs& a, const Copied& in, hipStream_t s) {
   return GS_OK;
 }
 
+template <typename O, int BL, int KC, bool CARRY>
+int32_t run_strip(const ScoresArgs& a, int64_t per_xcd, int64_t groups, int64_t ranges, hipStream_t s) {
+  if (groups * ranges * 8 > (int64_t)INT32_MAX) return GS_EOVERFLOW;
+  strip_kernel<O, BL, KC, CARRY><<<dim3((unsigned)(groups * ranges * 8)), Strip<O, BL, CARRY>::kThreads, 0, s>>>(a, groups, ranges, per_xcd);
+  GS_LAUNCH_CHECK();
+  return GS_OK;
+}
+
+// Rows of one or two blocks.
+template <typename O>
+int32_t run_strips(const ScoresArgs& a, hipStream_t s) {
+  const bool two = a.blocks == 2, wide = a.num_centers > 128 && !(two && O::kExact);      // 64 centres a wave, where registers hold them
+  const int64_t per_xcd = ceil_div(ceil_div(a.num_nodes, 64), 8);
+  auto ranges = [&](int64_t groups, int64_t workgroups, int64_t least) {   // of an XCD, of so many tiles at least
+    return std::max<int64_t>(1, std::min(ceil_div(workgroups, groups * 8), per_xcd / least));
+  };
+  const int64_t groups = ceil_div(a.num_centers, wide ? 256 : 128), rows = ceil_div(a.num_centers, 128);
+  // Rows of scores that begin inside lines: long ranges keep the ends of their lines for the next tile.  256 centres on 1,000,003 nodes
+  // of 128 columns: 335 -> 275 us (fp32 scores), 190 -> 161 (bf16); shorter ranges lose more at their own ends (40 on 300,001: 17 -> 27).
+  const bool lines = a.num_nodes * (int64_t)sizeof(typename O::elem) % 128 == 0 && aligned(a.out, 128);
+  const int64_t few = ranges(rows, 256, 1);
+  if (!two && !lines && per_xcd / few >= 48) return run_strip<O, 1, 1, true>(a, per_xcd, rows, few, s);
+  const int64_t r = ranges(groups, wide ? 256 : 512, 8);      // one workgroup of 64 centres a wave fits a compute unit's registers
+  if (two) {
+    if constexpr (!O::kExact)
+      if (wide) return run_strip<O, 2, 2, false>(a, per_xcd, groups, r, s);
+    return run_strip<O, 2, 1, false>(a, per_xcd, groups, r, s);
+  }
+  return wide ? run_strip<O, 1, 2, false>(a, per_xcd, groups, r, s) : run_strip<O, 1, 1, false>(a, per_xcd, groups, r, s);
+}
+
 template <typename O>
 int32_t run_scores(const ScoresArgs& a, const ScoresPlan& p, hipStream_t s) {
   if (p.few) {
@@ -459,6 +778,7 @@ int32_t run_scores(const ScoresArgs& a, const ScoresPlan& p, hipStream_t s) {
     GS_LAUNCH_CHECK();
     return GS_OK;
   }
+  if (a.blocks <= 2) return run_strips<O>(a, s);
   copy_centers_kernel<<<dim3((unsigned)p.padded), 64, 0, s>>>(a, p.in);
   GS_LAUNCH_CHECK();
   if (a.num_centers <= 128) return run_tiles<O, 2, 2, 2, 2>(a, p.in, s);

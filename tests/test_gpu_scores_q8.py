@@ -72,6 +72,23 @@ def test_scores(gs, centers, nodes, dim, dtype):
     check(gs, t_in, t_out, ids, dtype=dtype, scale=0.5 if dim == 200 else 1.0)
 
 
+@pytest.mark.parametrize("dtype", list(TORCH))
+@pytest.mark.parametrize("centers,nodes,dim", [(33, 800_003, 16), (64, 790_001, 128), (600, 172_543, 100), (130, 400_007, 64), (130, 400_064, 64), (700, 30_016, 256)])
+def test_many_nodes(gs, centers, nodes, dim, dtype):
+    """Long ranges of nodes for each workgroup, in rows that begin inside and on lines of 128 bytes; an output that begins elsewhere."""
+    t_in, t_out = table(gs, 300, dim, 1), table(gs, nodes, dim, 2)
+    gen = torch.Generator().manual_seed(3)
+    ids = torch.randint(0, 300, (centers,), generator=gen, dtype=torch.int32).to(DEV)
+    ids[centers // 3] = -1
+    bias = torch.randn(nodes, generator=gen).masked_fill(torch.rand(nodes, generator=gen) < 0.1, -INF).to(DEV)
+    check(gs, t_in, t_out, ids, bias=bias, dtype=dtype)
+    room = torch.full((centers * nodes + 100,), 9.0, dtype=TORCH[dtype], device=DEV)
+    out = room[37:37 + centers * nodes].view(centers, nodes)
+    gs.gs_scores_q8(t_in, t_out, ids, dtype=TORCH[dtype], out=out)
+    assert torch.equal(out.nan_to_num(7.0), gs.gs_scores_q8(t_in, t_out, ids, dtype=TORCH[dtype]).nan_to_num(7.0))
+    assert bool((room[:37] == 9).all()) and bool((room[-63:] == 9).all())
+
+
 @pytest.mark.parametrize("centers", [1, 5, 40, 130, 300])
 @pytest.mark.parametrize("dim", [64, 200, 1024])
 def test_masks_and_centres_that_are_no_rows(gs, centers, dim):
