@@ -27,7 +27,6 @@ typedef float acc16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 
-constexpr int kThreads = 256;
 constexpr int kBlock = 128;
 
 struct ScoresArgs {
@@ -43,10 +42,17 @@ struct ScoresArgs {
   void* out;
 };
 
+// Pieces of rows of scores, which begin at any element.  One store each: types of their own, not copies of bytes, which the compiler
+// takes apart where parts of them are stored elsewhere too.
+typedef uint32_t of_words __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t of_halves __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t of_two_halves __attribute__((ext_vector_type(2), aligned(2)));
 struct OutF32 {
   typedef float elem;
   static constexpr bool kExact = true;         // bf16 products of converted values
-  static __device__ __forceinline__ void store4(float* p, const float* v) { __builtin_memcpy(p, v, 16); }
+  static __device__ __forceinline__ void store4(float* p, const float* v) {
+    *reinterpret_cast<of_words*>(p) = (of_words){__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+  }
   static __device__ __forceinline__ void store(float* p, float v) { *p = v; }
   static __device__ __forceinline__ void put4(float* p, const float* v) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
 };
@@ -56,8 +62,7 @@ struct OutHalf {
   static constexpr bool kExact = false;
   static __device__ __forceinline__ uint32_t round(float v) { return H::round_any(v); }
   static __device__ __forceinline__ void store4(uint16_t* p, const float* v) {
-    const uint32_t w[2] = {round(v[0]) | round(v[1]) << 16, round(v[2]) | round(v[3]) << 16};
-    __builtin_memcpy(p, w, 8);
+    *reinterpret_cast<of_two_halves*>(p) = (of_two_halves){round(v[0]) | round(v[1]) << 16, round(v[2]) | round(v[3]) << 16};
   }
   static __device__ __forceinline__ void store(uint16_t* p, float v) { *p = (uint16_t)round(v); }
   static __device__ __forceinline__ void put4(uint16_t* p, const float* v) {
@@ -71,20 +76,26 @@ struct ToF16 {
   static __device__ __forceinline__ uint32_t round_any(float v) { return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)v); }
 };
 
-// 32 bytes of a row from `col` on, zeros from `pitch` on
-__device__ __forceinline__ int8v load32(const uint8_t* row, int col, int pitch) {
-  const uint4 none = make_uint4(0, 0, 0, 0);
-  const uint4 a = col < pitch ? *reinterpret_cast<const uint4*>(row + col) : none;
-  const uint4 b = col + 16 < pitch ? *reinterpret_cast<const uint4*>(row + col + 16) : none;
+typedef uint32_t word4 __attribute__((ext_vector_type(4)));
+__device__ word4 zero_piece[1];                // never written: what pieces that are none are read as
+
+// 32 bytes of a row from `col` on, zeros from `pitch` on, or all of them; the address is chosen, not the value, which would be loaded
+// in words
+__device__ __forceinline__ int8v load32(const uint8_t* row, int col, int pitch, bool there = true) {
+  const word4 a = *(there && col < pitch ? reinterpret_cast<const word4*>(row + col) : zero_piece);
+  const word4 b = *(there && col + 16 < pitch ? reinterpret_cast<const word4*>(row + col + 16) : zero_piece);
+  return int8v{(int)a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, (int)b.y, (int)b.z, (int)b.w};
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t range_of(const void* base, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00027000);
+}
+constexpr int kOutside = 1 << 30;              // of every range: read as zeros
+__device__ __forceinline__ int8v load32(__amdgpu_buffer_rsrc_t range, int row, int col, int pitch) {
+  const word4 a = __builtin_bit_cast(word4, __builtin_amdgcn_raw_buffer_load_b128(range, col < pitch ? row + col : kOutside, 0, 0));
+  const word4 b = __builtin_bit_cast(word4, __builtin_amdgcn_raw_buffer_load_b128(range, col + 16 < pitch ? row + col + 16 : kOutside, 0, 0));
   return int8v{(int)a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, (int)b.y, (int)b.z, (int)b.w};
 }
 
-// The largest power of a row's blocks, as its byte; blocks of NaN aside.
-__device__ __forceinline__ int top_scale(const uint8_t* scales, int blocks) {
-  int top = 0;
-  for (int b = 0; b < blocks; ++b) top = max(top, scales[b] == 255 ? 0 : (int)scales[b]);
-  return top;
-}
 // 2^(byte - top) for the conversion, which looks at the exponent alone; NaN stays
 __device__ __forceinline__ float relative(int byte, int top) {
   return __uint_as_float((uint32_t)(byte == 255 ? 255 : max(byte - top + 127, 1)) << 23);
@@ -102,64 +113,145 @@ __device__ __forceinline__ bf8 widen(int lo, int hi, float scale) {
   return x.all;
 }
 
-// A wave: 32 nodes and 32 centres.
-template <typename O>
-__global__ __launch_bounds__(kThreads) void scores_kernel(ScoresArgs a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = lane & 31, half = lane >> 5;
-  const int64_t first = ((int64_t)blockIdx.x * 4 + wave) * 32;
-  if (first >= a.num_nodes) return;
-  const int64_t i = (int64_t)blockIdx.y * 32 + at;
-  const int64_t id = i < a.num_centers ? (int64_t)a.centers[i] : -1;
+template <int LOADS>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(LOADS < 64, "the counter's range");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LOADS) : "memory");
+}
+__device__ __forceinline__ void meet() {
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+// ---- few centres: rows of nodes straight into registers -----------------------
+// Up to 32 centres: reading the nodes' rows is the work.  A wave takes 32 nodes and a block at a time, and asks for the next one's bytes
+// before it multiplies; SPLIT waves share the blocks of a tile, and add up through LDS.  Workgroups take tiles in turn.
+// fp32 scores: values go into the bf16 instruction times their powers of two, which is exact while these are of 2^-117 to 2^119; other
+// powers (and blocks of zeros, which have the least) multiply the block's sums instead.
+
+template <typename O, int SPLIT>
+__global__ __launch_bounds__(256, 4) void few_kernel(ScoresArgs a, int64_t turns) {
+  constexpr int kTiles = 4 / SPLIT;            // of a workgroup at once
+  __shared__ float others[2][SPLIT > 1 ? kTiles * (SPLIT - 1) : 1][16][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = lane & 31, half = lane >> 5;
+  const int part = wave % SPLIT, sub = wave / SPLIT;
+  const bool asked = at < a.num_centers;
+  const int64_t id = asked ? (int64_t)a.centers[at] : -1;
   const bool there = id >= 0 && id < a.num_in;
-  const int64_t row_in = there ? id : 0, row_out = min(first + at, a.num_nodes - 1);
-  const uint8_t *h = a.q_in + row_in * a.pitch, *c = a.q_out + row_out * a.pitch;
-  const uint8_t *hs = a.scales_in + row_in * a.scale_pitch, *cs = a.scales_out + row_out * a.scale_pitch;
+  const uint8_t *h = a.q_in + (there ? id : 0) * a.pitch, *hs = a.scales_in + (there ? id : 0) * a.scale_pitch;
+  const int steps = (a.blocks + SPLIT - 1) / SPLIT;                      // of a tile
+  const bool keep = steps == 1;                                          // the centres' block is the same for every tile
+
+  struct Stage {
+    int8v x[2], y[2];
+    int node_power, center_power;
+  } st[2];
+  auto load_centers = [&](Stage& to, int block) {
+    const int col = block * kBlock + half * 64;
+    to.center_power = !asked ? 127 : !there ? 255 : block < a.blocks ? (int)hs[block] : 127;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) to.y[s] = load32(h, col + 32 * s, a.pitch, there);
+  };
+  auto load = [&](Stage& to, int64_t turn, int k) {
+    const int block = part + SPLIT * k, col = block * kBlock + half * 64;
+    const int64_t first = (turn * kTiles + sub) * 32;
+    const int nodes = (int)max((int64_t)0, min((int64_t)32, a.num_nodes - first));
+    const int64_t from = nodes > 0 ? first : 0;
+    const __amdgpu_buffer_rsrc_t rows = range_of(a.q_out + from * a.pitch, nodes * a.pitch);
+    const __amdgpu_buffer_rsrc_t powers = range_of(a.scales_out + from * a.scale_pitch, nodes * a.scale_pitch);
+    to.node_power = __builtin_amdgcn_raw_buffer_load_b8(powers, block < a.blocks ? at * a.scale_pitch + block : kOutside, 0, 0);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) to.x[s] = load32(rows, at * a.pitch, col + 32 * s, a.pitch);
+    if (!keep) load_centers(to, block);
+  };
   acc16 acc = {};
-  const int top_in = O::kExact ? top_scale(hs, a.blocks) : 0, top_out = O::kExact ? top_scale(cs, a.blocks) : 0;
-  for (int b = 0; b < a.blocks; ++b) {
-    const int col = b * kBlock + half * 64;
-    const int se = hs[b], sf = cs[b];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const int8v x = load32(c, col + 32 * s, a.pitch), y = load32(h, col + 32 * s, a.pitch);
-      if (O::kExact) {
-        const float fx = relative(sf, top_out), fy = relative(se, top_in);
-#pragma unroll
-        for (int k = 0; k < 8; k += 2)
-          acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(x[k], x[k + 1], fx), widen(y[k], y[k + 1], fy), acc, 0, 0, 0);
-      } else {
-        acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, acc, 0, 0, 0, sf, 0, se);
-      }
-    }
+  int64_t turn = blockIdx.x;
+  int k = 0, flip = 0;
+  if (keep) {
+    load_centers(st[0], part);
+    st[1].y[0] = st[0].y[0], st[1].y[1] = st[0].y[1], st[1].center_power = st[0].center_power;
   }
-  if (O::kExact)
+  auto finish = [&]() {
+    if (SPLIT > 1) {
+      if (part > 0)
 #pragma unroll
-    for (int t = 0; t < 16; ++t)
-      acc[t] = ldexpf(acc[t], top_in - 254 + __shfl(top_out, 8 * (t / 4) + 4 * half + t % 4, 64));
-  if (i >= a.num_centers) return;
-  typename O::elem* out = static_cast<typename O::elem*>(a.out) + i * a.num_nodes;
+        for (int t = 0; t < 16; ++t) others[flip][sub * (SPLIT - 1) + part - 1][t][lane] = acc[t];
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      meet();
+      if (part == 0)
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    const int64_t j = first + 8 * t + 4 * half;
-    float v[4];
+        for (int o = 0; o < SPLIT - 1; ++o)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      v[k] = there ? a.scale * acc[4 * t + k] : NAN;
-      if (a.bias && j + k < a.num_nodes) {
-        const float bias = a.bias[j + k];
-        v[k] = bias == -INFINITY ? -INFINITY : v[k] + bias;
+          for (int t = 0; t < 16; ++t) acc[t] += others[flip][sub * (SPLIT - 1) + o][t][lane];
+      flip ^= 1;                               // the other half is free: part 0 was done with it before it came here
+    }
+    const int64_t first = (turn * kTiles + sub) * 32;
+    if (part == 0 && asked) {
+      typename O::elem* out = static_cast<typename O::elem*>(a.out) + at * a.num_nodes + first + 4 * half;
+      const float* biases = a.bias ? a.bias + first + 4 * half : nullptr;
+      if (first + 32 <= a.num_nodes) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = a.scale * acc[4 * g + e];
+          if (a.bias) {
+            const of_words w = *reinterpret_cast<const of_words*>(biases + 8 * g);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(w[e]) == -INFINITY ? -INFINITY : v[e] + __uint_as_float(w[e]);
+          }
+          O::store4(out + 8 * g, v);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int j = 8 * (e / 4) + e % 4;
+          if (first + 4 * half + j >= a.num_nodes) continue;
+          const float z = a.scale * acc[e], bias = a.bias ? biases[j] : 0.0f;
+          O::store(out + j, bias == -INFINITY ? -INFINITY : z + bias);
+        }
       }
     }
-    if (j + 4 <= a.num_nodes) {
-      O::store4(out + j, v);
+    acc = acc16{};
+  };
+  // one step: asks for the next, multiplies this one's; false after the last
+  auto step = [&](Stage& now, Stage& next) {
+    int64_t next_turn = turn;
+    int next_k = k + 1;
+    if (next_k == steps) next_k = 0, next_turn += gridDim.x;
+    if (next_turn < turns) load(next, next_turn, next_k);
+    if (O::kExact) {
+      auto easy = [](int byte) { return byte == 255 || (unsigned)(byte - 10) <= 236u; };
+      const bool by_values = __ballot(easy(now.node_power) && easy(now.center_power)) == ~0ull;
+      const float fx = by_values ? __uint_as_float((uint32_t)now.node_power << 23) : relative(now.node_power, now.node_power);
+      const float fy = by_values ? __uint_as_float((uint32_t)now.center_power << 23) : relative(now.center_power, now.center_power);
+      acc16 sum = {};
+      if (by_values) sum = acc;
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int w = 0; w < 8; w += 2)
+          sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(now.x[s][w], now.x[s][w + 1], fx), widen(now.y[s][w], now.y[s][w + 1], fy), sum, 0, 0, 0);
+      if (by_values) {
+        acc = sum;
+      } else {
+#pragma unroll
+        for (int t = 0; t < 16; ++t)
+          acc[t] += ldexpf(sum[t], now.center_power - 254 + __shfl(now.node_power, 8 * (t / 4) + 4 * half + t % 4, 64));
+      }
     } else {
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (j + k < a.num_nodes) O::store(out + j + k, v[k]);
+      for (int s = 0; s < 2; ++s)
+        acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(now.x[s], now.y[s], acc, 0, 0, 0, now.node_power, 0, now.center_power);
     }
+    if (k + 1 == steps) finish();
+    turn = next_turn, k = next_k;
+    return turn < turns;
+  };
+  if (turn >= turns) return;
+  load(st[0], turn, 0);
+  while (step(st[0], st[1]) && step(st[1], st[0])) {
   }
 }
-
 
 // ---- many centres: tiles of both through LDS ---------------------------------
 // Centres are copied first: rows of whole blocks, zeros behind, so that no load looks at an id; a centre that is no row has the scale
@@ -198,22 +290,6 @@ __global__ __launch_bounds__(64) void copy_centers_kernel(ScoresArgs a, Copied t
   if (lane == 0) to.top[i] = top;
 }
 
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t range_of(const void* base, int bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00027000);
-}
-template <int LOADS>
-__device__ __forceinline__ void wait_loads() {
-  static_assert(LOADS < 64, "the counter's range");
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LOADS) : "memory");
-}
-__device__ __forceinline__ void meet() {
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-// 16 bytes of a row of scores; rows begin at any element.  One store: types of their own, not a copy of bytes, which the compiler
-// takes apart where parts of it are stored elsewhere too.
-typedef uint32_t of_words __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint32_t of_halves __attribute__((ext_vector_type(4), aligned(2)));
 __device__ __forceinline__ void put_piece(float* to, const uint4& w) { *reinterpret_cast<of_words*>(to) = (of_words){w.x, w.y, w.z, w.w}; }
 __device__ __forceinline__ void put_piece(uint16_t* to, const uint4& w) { *reinterpret_cast<of_halves*>(to) = (of_halves){w.x, w.y, w.z, w.w}; }
 // 16 bytes of LDS from any element on
@@ -221,7 +297,6 @@ __device__ __forceinline__ uint4 read_loose(const uint8_t* from) {
   const of_halves w = *reinterpret_cast<const of_halves*>(from);
   return make_uint4(w.x, w.y, w.z, w.w);
 }
-constexpr int kOutside = 1 << 30;              // of every range: read as zeros
 constexpr int kStep = 64;                      // columns
 constexpr int kStages = 4;                     // steps in LDS
 
@@ -774,7 +849,12 @@ int32_t run_strips(const ScoresArgs& a, hipStream_t s) {
 template <typename O>
 int32_t run_scores(const ScoresArgs& a, const ScoresPlan& p, hipStream_t s) {
   if (p.few) {
-    scores_kernel<O><<<dim3((unsigned)ceil_div(a.num_nodes, 128), (unsigned)ceil_div(a.num_centers, 32)), kThreads, 0, s>>>(a);
+    const int split = a.blocks >= 3 ? 4 : a.blocks;
+    const int64_t turns = ceil_div(a.num_nodes, 32 * (4 / split));
+    const dim3 grid((unsigned)std::min<int64_t>(turns, 1024));
+    if (split == 1) few_kernel<O, 1><<<grid, 256, 0, s>>>(a, turns);
+    if (split == 2) few_kernel<O, 2><<<grid, 256, 0, s>>>(a, turns);
+    if (split == 4) few_kernel<O, 4><<<grid, 256, 0, s>>>(a, turns);
     GS_LAUNCH_CHECK();
     return GS_OK;
   }
