@@ -19,10 +19,11 @@ namespace {
 
 constexpr int kMostWidth = 256;
 constexpr int kPartThreads = 256;
-constexpr int kJoinThreads = 512;
-constexpr int kPartList = 1024;                // scores that may reach the bound
+constexpr int kPartList = 2048;                // scores that may reach the bound
 constexpr int kJoinList = 2048;
-static_assert(kPartThreads >= kMostWidth && kJoinThreads >= kMostWidth, "a lane each for the bound");
+constexpr int kBins = 1024;
+constexpr int kCounted = 128;                  // of a list at most, where places are counted; longer ones are sorted
+static_assert(kPartThreads >= kMostWidth, "a lane each for the bound");
 
 struct SelectArgs {
   const void* scores;
@@ -32,9 +33,8 @@ struct SelectArgs {
   const uint8_t* ended;                        // or null
   int32_t parts;                               // of a row
   int64_t part_len;
-  uint64_t* keys;                              // [rows][parts][width]: a part's best, in order
-  int32_t* counts;                             // [rows][parts]: how many these are
-  float* tops;                                 // largest score
+  uint64_t* keys;                              // [rows][parts][width]: a part's best, in order, and zeros
+  float* tops;                                 // [rows][parts]: largest score
   double* sums;                                // of exp(s - top)
   int32_t *parents, *nodes;
   float* logp_out;
@@ -59,130 +59,301 @@ __device__ __forceinline__ uint64_t wave_most(uint64_t v) {
   return v;
 }
 
-// The width-th largest of a value of each lane, 0 if there are fewer than `width` above 0: a lower bound of the width-th largest
-// of all, if each lane's value is one of them.
+// The width-th largest of a value of each lane of a wave; 0 if there are fewer than `width` above 0.  Bit by bit: the largest value that
+// `width` lanes reach; one vector instruction each.
+template <typename K>
+__device__ __forceinline__ K wave_bound(K mine, int width) {
+  K found = 0;
+#pragma unroll
+  for (int bit = 8 * (int)sizeof(K) - 1; bit >= 0; --bit) {
+    const bool reached = (int)__popcll(__ballot(mine >= (found | (K)1 << bit))) >= width;
+    found |= (K)reached << bit;
+  }
+  return found;
+}
+// The same of a workgroup, or of 64 of its values, the largest of the lanes alike; `all`: a value for each lane.  Where each value is
+// one of many, a lower bound of the width-th largest of all.
 template <int THREADS, typename K>
-__device__ __forceinline__ K bound_of(K own, int width, K* all, K* bound) {
+__device__ __forceinline__ K bound_of(K own, int width, K* all) {
+  static_assert(THREADS >= kMostWidth, "the width-th of them");
+  const int lane = threadIdx.x & 63;
   all[threadIdx.x] = own;
-  if (threadIdx.x == 0) *bound = 0;
+  __syncthreads();
+  if (width <= 32) {                           // every wave for itself
+    K mine = all[lane];
+#pragma unroll
+    for (int w = 1; w < THREADS / 64; ++w) mine = max(mine, all[w * 64 + lane]);
+    return wave_bound(mine, width);
+  }
+  // of 256 values; a lane's own one is the largest of the lanes alike
+  __shared__ K bound;
+  if (threadIdx.x == 0) bound = 0;
+  K mine = 0;
+  if (threadIdx.x < 256)
+#pragma unroll
+    for (int w = 0; w < THREADS / 256; ++w) mine = max(mine, all[w * 256 + threadIdx.x]);
+  __syncthreads();
+  if (threadIdx.x < 256) all[threadIdx.x] = mine;
   __syncthreads();
   int before = 0;
-  for (int t = 0; t < THREADS; ++t) before += all[t] > own || (all[t] == own && t < (int)threadIdx.x);
-  if (before == width - 1) *bound = own;
+  if (threadIdx.x < 256)
+#pragma unroll 16
+    for (int t = 0; t < 256; ++t) before += all[t] > mine || (all[t] == mine && t < (int)threadIdx.x);
+  if (threadIdx.x < 256 && before == width - 1) bound = mine;
   __syncthreads();
-  return *bound;
+  return bound;
 }
 
+// Puts n values (more than 1, room for the next power of two) in falling order, by THREADS lanes: bitonic.  `key` gives a place for an index, `swap`
+// exchanges two; a barrier precedes.
+template <int THREADS, typename Before, typename Swap>
+__device__ __forceinline__ void sort_list(int n, Before before, Swap swap) {
+  for (int size = 2; size <= n; size <<= 1)
+    for (int step = size >> 1; step > 0; step >>= 1) {
+      for (int i = threadIdx.x; i < n / 2; i += THREADS) {
+        const int lo = 2 * i - (i & (step - 1)), hi = lo + step;
+        const bool falling = (lo & size) == 0;
+        if (falling ? before(hi, lo) : before(lo, hi)) swap(lo, hi);
+      }
+      __syncthreads();
+    }
+}
+__device__ __forceinline__ int power_of_two(int n) { return n <= 1 ? 1 : 1 << (32 - __clz(n - 1)); }
+
+// exp(s - top) as 2^(n / 64) 2^r, r within 1/128: a table of 64 powers, and the series of 2^r to r^4 (the next term is below 4e-14 of
+// it).  A copy of the table for each lane of a half wave, so that no two lanes of a read meet in a bank.
+// 2^(j / 64), each to the nearest
+__device__ const double power_table[kPowers] = {
+    0x1.0000000000000p+0, 0x1.02c9a3e778061p+0, 0x1.059b0d3158574p+0, 0x1.0874518759bc8p+0,
+    0x1.0b5586cf9890fp+0, 0x1.0e3ec32d3d1a2p+0, 0x1.11301d0125b51p+0, 0x1.1429aaea92de0p+0,
+    0x1.172b83c7d517bp+0, 0x1.1a35beb6fcb75p+0, 0x1.1d4873168b9aap+0, 0x1.2063b88628cd6p+0,
+    0x1.2387a6e756238p+0, 0x1.26b4565e27cddp+0, 0x1.29e9df51fdee1p+0, 0x1.2d285a6e4030bp+0,
+    0x1.306fe0a31b715p+0, 0x1.33c08b26416ffp+0, 0x1.371a7373aa9cbp+0, 0x1.3a7db34e59ff7p+0,
+    0x1.3dea64c123422p+0, 0x1.4160a21f72e2ap+0, 0x1.44e086061892dp+0, 0x1.486a2b5c13cd0p+0,
+    0x1.4bfdad5362a27p+0, 0x1.4f9b2769d2ca7p+0, 0x1.5342b569d4f82p+0, 0x1.56f4736b527dap+0,
+    0x1.5ab07dd485429p+0, 0x1.5e76f15ad2148p+0, 0x1.6247eb03a5585p+0, 0x1.6623882552225p+0,
+    0x1.6a09e667f3bcdp+0, 0x1.6dfb23c651a2fp+0, 0x1.71f75e8ec5f74p+0, 0x1.75feb564267c9p+0,
+    0x1.7a11473eb0187p+0, 0x1.7e2f336cf4e62p+0, 0x1.82589994cce13p+0, 0x1.868d99b4492edp+0,
+    0x1.8ace5422aa0dbp+0, 0x1.8f1ae99157736p+0, 0x1.93737b0cdc5e5p+0, 0x1.97d829fde4e50p+0,
+    0x1.9c49182a3f090p+0, 0x1.a0c667b5de565p+0, 0x1.a5503b23e255dp+0, 0x1.a9e6b5579fdbfp+0,
+    0x1.ae89f995ad3adp+0, 0x1.b33a2b84f15fbp+0, 0x1.b7f76f2fb5e47p+0, 0x1.bcc1e904bc1d2p+0,
+    0x1.c199bdd85529cp+0, 0x1.c67f12e57d14bp+0, 0x1.cb720dcef9069p+0, 0x1.d072d4a07897cp+0,
+    0x1.d5818dcfba487p+0, 0x1.da9e603db3285p+0, 0x1.dfc97337b9b5fp+0, 0x1.e502ee78b3ff6p+0,
+    0x1.ea4afa2a490dap+0, 0x1.efa1bee615a27p+0, 0x1.f50765b6e4540p+0, 0x1.fa7c1819e90d8p+0,
+};
+constexpr int kCopies = 32;
+struct Powers {
+  double of[kPowers][kCopies];
+  // by kPartThreads lanes, a quarter of a power's copies each; a barrier follows before the first use
+  static __device__ __forceinline__ double mine() { return power_table[threadIdx.x / 4]; }
+  __device__ __forceinline__ void fill(double p) {
+    static_assert(kPartThreads == 4 * kPowers && kCopies % 8 == 0, "a quarter each");
+#pragma unroll
+    for (int c = 0; c < kCopies / 4; ++c) of[threadIdx.x / 4][threadIdx.x % 4 * (kCopies / 4) + c] = p;
+  }
+};
+struct WeighBelow {
+  double top;
+  const double* powers;
+  __device__ __forceinline__ WeighBelow(float top_, const Powers& p) : top((double)top_), powers(&p.of[0][threadIdx.x % kCopies]) {}
+  // a score left out (-infinity or NaN) weighs 2^-1000, which no sum of weights up to 1 notices
+  __device__ __forceinline__ double operator()(float s) const {
+    const double y = fmax(((double)s - top) * (kPowers * 1.4426950408889634074), -1000.0 * kPowers);      // in steps of the table
+    const double t = y + 0x1.8p52;             // its last bits: the nearest whole number
+    const double r = y - (t - 0x1.8p52);
+    const int n = __double2loint(t);
+    const double power = powers[(n & (kPowers - 1)) * kCopies];
+    constexpr double l = 0.69314718055994530942 / kPowers, l2 = l * l, l3 = l2 * l, l4 = l2 * l2;
+    double q = fma(r, l4 / 24, l3 / 6);
+    q = fma(r, q, l2 / 2);
+    q = fma(r, q, l) * r;
+    q = fma(power, q, power);                  // 2^-1000 times it is no subnormal: the exponent alone changes
+    return __hiloint2double(__double2hiint(q) + (int)((unsigned)(n & -kPowers) << 14), __double2loint(q));
+  }
+};
+static_assert(kPowers == 64, "n / 64 into the exponent: six places down, twenty up");
+
+// 16 bytes of scores as they lie in memory, rows that begin at any element
+template <typename V>
+struct Raw {
+  typedef typename V::elem elem;
+  static constexpr int kPer = 16 / (int)sizeof(elem);
+  typedef uint32_t loose __attribute__((ext_vector_type(4), aligned(2)));
+  loose w;
+  __device__ __forceinline__ float operator[](int k) const {
+    if constexpr (kPer == 4) return __uint_as_float(w[k]);
+    else return V::get_of(w[k / 2], k % 2);
+  }
+  __device__ __forceinline__ void none() {     // -infinity
+    w = (loose){V::kNone, V::kNone, V::kNone, V::kNone};
+  }
+};
+
+constexpr int kDumped = 32;                    // lanes whose scores are looked through together
+template <int LOADS, int TEAM>
 struct PartShared {
-  double powers[kPowers];
+  Powers powers;
+  uint4 dump[TEAM == 64 ? 64 : kDumped][LOADS];      // of a wave: a quarter
+  uint8_t dumper[TEAM == 64 ? 64 : kDumped];
+  uint32_t dumped[kPartThreads / 64];
   float wave_top[kPartThreads / 64];
   double wave_sum[kPartThreads / 64];
   uint32_t lane_top[kPartThreads];
-  uint32_t bound;
-  uint32_t listed;
+  uint32_t listed[kPartThreads / 64];
   uint64_t list[kPartList];
   uint64_t wave_best[2][kPartThreads / 64];
 };
 
-template <typename V, int LOADS>
-__global__ __launch_bounds__(kPartThreads) void part_kernel(SelectArgs a) {
+// Parts of rows, TEAM lanes each: a workgroup, or a wave, which then needs no barrier but the table's.
+constexpr int waves_of(int scores, int team) { return scores >= 64 ? (team == 64 ? 2 : 3) : scores >= 32 ? 3 : 4; }      // on a SIMD
+template <typename V, int LOADS, int TEAM>
+__global__ __launch_bounds__(kPartThreads, waves_of(LOADS * Raw<V>::kPer, TEAM)) void part_kernel(SelectArgs a, int64_t slots) {
   typedef typename V::elem elem;
-  constexpr int kPer = 16 / (int)sizeof(elem);
-  __shared__ PartShared sh;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const uint32_t row = blockIdx.x / (uint32_t)a.parts, part = blockIdx.x - row * (uint32_t)a.parts;
-  const int64_t slot = (int64_t)blockIdx.x;
-  if (!(a.logp[row] > -INFINITY) || (a.ended && a.ended[row])) {      // not looked at
-    if (tid == 0) a.counts[slot] = 0, a.tops[slot] = -INFINITY, a.sums[slot] = 0.0;
-    return;
-  }
-  fill_powers(sh.powers);
-  if (tid == 0) sh.listed = 0;
+  constexpr int kPer = Raw<V>::kPer, kWaves = kPartThreads / 64, kList = TEAM == 64 ? kPartList / kWaves : kPartList;
+  __shared__ PartShared<LOADS, TEAM> sh;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = TEAM == 64 ? lane : (int)threadIdx.x;
+  const int64_t slot = TEAM == 64 ? (int64_t)blockIdx.x * kWaves + wave : (int64_t)blockIdx.x;
+  auto meet = [&]() {                          // of the team
+    if (TEAM == 64) wave_fence();
+    else __syncthreads();
+  };
+  const bool last_few = TEAM == 64 && slot >= slots;      // waves without a part
+  const uint32_t row = last_few ? 0 : (uint32_t)slot / (uint32_t)a.parts, part = (uint32_t)slot - row * (uint32_t)a.parts;
+  const bool looked_at = !last_few && a.logp[row] > -INFINITY && !(a.ended && a.ended[row]);
+  uint64_t* const keys = a.keys + slot * a.width;
+  auto none = [&]() {
+    if (last_few) return;
+    if (tid == 0) a.tops[slot] = -INFINITY, a.sums[slot] = 0.0;
+    for (int c = tid; c < a.width; c += TEAM) keys[c] = 0;
+  };
+  if (TEAM != 64 && !looked_at) return none();
+  uint32_t* const listed_at = &sh.listed[TEAM == 64 ? wave : 0];
+  uint64_t* const list = sh.list + (TEAM == 64 ? wave * kList : 0);
+
   const int64_t from = (int64_t)part * a.part_len;
-  const int len = (int)min(a.n - from, a.part_len), whole = len / kPer;      // of 16 bytes
+  const int len = looked_at ? (int)min(a.n - from, a.part_len) : 0, whole = len / kPer;      // of 16 bytes
   const elem* base = static_cast<const elem*>(a.scores) + (int64_t)row * a.n + from;
-  float s[LOADS][kPer];
-  {
-    uint4 w[LOADS];
+  Raw<V> s[LOADS];
+  const double power = Powers::mine();
 #pragma unroll
-    for (int e = 0; e < LOADS; ++e) {
-      const int p = e * kPartThreads + tid;
-      if (p < whole) __builtin_memcpy(&w[e], base + (int64_t)p * kPer, 16);
-    }
-#pragma unroll
-    for (int e = 0; e < LOADS; ++e) {
-      const int p = e * kPartThreads + tid;
-      elem x[kPer];
-      __builtin_memcpy(x, &w[e], 16);
-#pragma unroll
-      for (int k = 0; k < kPer; ++k) {
-        const float v = V::get(x[k]);
-        s[e][k] = p < whole && v > -INFINITY ? v : -INFINITY;
-      }
-      if (p == whole)
-#pragma unroll
-        for (int k = 0; k < kPer; ++k) {
-          if (p * kPer + k >= len) break;
-          const float v = V::get(base[(int64_t)p * kPer + k]);
-          s[e][k] = v > -INFINITY ? v : -INFINITY;
-        }
-    }
+  for (int e = 0; e < LOADS; ++e) {
+    if (whole > 0) s[e].w = *reinterpret_cast<const typename Raw<V>::loose*>(base + (int64_t)min(e * TEAM + tid, whole - 1) * kPer);
+    else s[e].none();
   }
+  uint32_t* const dumped_at = &sh.dumped[TEAM == 64 ? wave : 0];
+  if (tid == 0) *listed_at = 0, *dumped_at = 0;
+  sh.powers.fill(power);                       // while the scores are under way
+  if (len < LOADS * TEAM * kPer)               // a part that ends before
+#pragma unroll
+    for (int e = 0; e < LOADS; ++e) {
+      const int p = e * TEAM + tid;
+      if (p >= whole) s[e].none();
+      if (p == whole && p * kPer < len) {      // the last few
+        elem x[kPer];
+        __builtin_memcpy(x, &s[e].w, 16);
+#pragma unroll
+        for (int k = 0; k < kPer; ++k)
+          if (p * kPer + k < len) x[k] = base[(int64_t)p * kPer + k];
+        __builtin_memcpy(&s[e].w, x, 16);
+      }
+    }
   float own = -INFINITY;
 #pragma unroll
   for (int e = 0; e < LOADS; ++e)
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) own = fmaxf(own, s[e][k]);
+    for (int k = 0; k < kPer; ++k) own = s[e][k] > own ? s[e][k] : own;
   float top = own;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-  if (lane == 0) sh.wave_top[wave] = top;
-  __syncthreads();
+  uint32_t bound;
+  if constexpr (TEAM == 64) {
+    bound = wave_bound(key_of(own), a.width);
+    __syncthreads();                           // the table's
+    if (!looked_at) return none();
+  } else {
+    if (lane == 0) sh.wave_top[wave] = top;
+    bound = bound_of<kPartThreads>(key_of(own), a.width, sh.lane_top);      // the barrier inside is also that of tops, table and count
 #pragma unroll
-  for (int w = 0; w < kPartThreads / 64; ++w) top = fmaxf(top, sh.wave_top[w]);
-  if (!(top > -INFINITY)) {                      // nothing there
-    if (tid == 0) a.counts[slot] = 0, a.tops[slot] = -INFINITY, a.sums[slot] = 0.0;
-    return;
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sh.wave_top[w]);
   }
+  if (!(top > -INFINITY)) return none();       // nothing there
 
-  const Weigh weigh(top, 1.0f, sh.powers);
   double sum = 0.0;
+  if (top < INFINITY) {
+    const WeighBelow weigh(top, sh.powers);
 #pragma unroll
-  for (int e = 0; e < LOADS; ++e)
+    for (int e = 0; e < LOADS; ++e)
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) sum += weigh(s[e][k]);
+      for (int k = 0; k < kPer; ++k) sum += weigh(s[e][k]);
+  } else {                                     // those that share the row's probability
+#pragma unroll
+    for (int e = 0; e < LOADS; ++e)
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) sum += s[e][k] == INFINITY ? 1.0 : 0.0;
+  }
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d, 64);
-  if (lane == 0) sh.wave_sum[wave] = sum;
+  if (TEAM != 64 && lane == 0) sh.wave_sum[wave] = sum;
 
-  const uint32_t bound = bound_of<kPartThreads>(key_of(own), a.width, sh.lane_top, &sh.bound);
-  const float least = bound ? score_of(bound) : -INFINITY;
-  int reach = 0;
+  const float least = bound ? score_of(bound) : -3.4028234663852886e38f;      // neither -infinity nor NaN reaches it
+  auto place_at = [&](int e, int k) { return place_of(key_of(s[e][k]), (uint32_t)(from + (e * TEAM + tid) * kPer + k)); };
+  auto take = [&](uint64_t place) {
+    const uint32_t to = atomicAdd(listed_at, 1u);
+    if (to < (uint32_t)kList) list[to] = place;
+  };
+  // About `width` lanes have a score that reaches the bound.  These put all of theirs into LDS, and the team looks through them: a
+  // branch for each score of each lane would take as long as the weights.
+  constexpr int kMost = TEAM == 64 ? 64 / kWaves : kDumped;
+  uint4 (*const dump)[LOADS] = sh.dump + (TEAM == 64 ? wave * kMost : 0);
+  uint8_t* const dumper = sh.dumper + (TEAM == 64 ? wave * kMost : 0);
+  if (own >= least) {
+    const uint32_t to = atomicAdd(dumped_at, 1u);
+    if (to < (uint32_t)kMost) {
 #pragma unroll
-  for (int e = 0; e < LOADS; ++e)
+      for (int e = 0; e < LOADS; ++e) dump[to][e] = make_uint4(s[e].w.x, s[e].w.y, s[e].w.z, s[e].w.w);
+      dumper[to] = (uint8_t)tid;
+    }
+  }
+  meet();
+  const int dumped = (int)*dumped_at;
+  if (dumped <= kMost) {
+    for (int i = tid; i < dumped * LOADS; i += TEAM) {
+      const int d = i / LOADS, e = i % LOADS;
+      const uint4 w = dump[d][e];
+      Raw<V> x;
+      x.w = (typename Raw<V>::loose){w.x, w.y, w.z, w.w};
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) reach += s[e][k] >= least && s[e][k] > -INFINITY;
-  if (reach > 0) {
-    uint32_t to = atomicAdd(&sh.listed, (uint32_t)reach);
+      for (int k = 0; k < kPer; ++k)
+        if (x[k] >= least) take(place_of(key_of(x[k]), (uint32_t)(from + (e * TEAM + dumper[d]) * kPer + k)));
+    }
+  } else {
 #pragma unroll
     for (int e = 0; e < LOADS; ++e)
 #pragma unroll
       for (int k = 0; k < kPer; ++k)
-        if (s[e][k] >= least && s[e][k] > -INFINITY) {
-          if (to < kPartList) sh.list[to] = place_of(key_of(s[e][k]), (uint32_t)(from + (e * kPartThreads + tid) * kPer + k));
-          ++to;
-        }
+        if (s[e][k] >= least) take(place_at(e, k));
   }
-  __syncthreads();
-  const int listed = (int)sh.listed;
-  uint64_t* keys = a.keys + slot * a.width;
-  if (listed <= kPartList) {
-    for (int c = tid; c < listed; c += kPartThreads) {
-      const uint64_t place = sh.list[c];
+  meet();
+  const int listed = (int)*listed_at;
+  for (int c = listed + tid; c < a.width; c += TEAM) keys[c] = 0;
+  if (listed <= (TEAM == 64 ? kList : kCounted)) {
+    for (int c = tid; c < listed; c += TEAM) {
+      const uint64_t place = list[c];
       int before = 0;
-      for (int o = 0; o < listed; ++o) before += sh.list[o] > place;
+#pragma unroll 4
+      for (int o = 0; o < listed; ++o) before += list[o] > place;
       if (before < a.width) keys[before] = place;
     }
+  } else if (TEAM != 64 && listed <= kList) {
+    const int n = power_of_two(listed);
+    for (int c = listed + tid; c < n; c += TEAM) list[c] = 0;
+    __syncthreads();
+    sort_list<TEAM>(n, [&](int i, int j) { return list[i] > list[j]; },
+                    [&](int i, int j) {
+                      const uint64_t x = list[i];
+                      list[i] = list[j], list[j] = x;
+                    });
+    if (tid < a.width) keys[tid] = list[tid];  // listed > width
   } else {
     uint64_t last = ~0ull, best = ~0ull;
     for (int taken = 0; taken < a.width; ++taken) {         // listed > width: there are as many
@@ -193,26 +364,28 @@ __global__ __launch_bounds__(kPartThreads) void part_kernel(SelectArgs a) {
 #pragma unroll
           for (int k = 0; k < kPer; ++k)
             if (s[e][k] > -INFINITY) {
-              const uint64_t place = place_of(key_of(s[e][k]), (uint32_t)(from + (e * kPartThreads + tid) * kPer + k));
+              const uint64_t place = place_at(e, k);
               if (place < last) best = max(best, place);
             }
       }
-      const uint64_t most = wave_most(best);
-      if (lane == 0) sh.wave_best[taken & 1][wave] = most;
-      __syncthreads();
-      last = 0;
+      last = wave_most(best);
+      if constexpr (TEAM != 64) {
+        if (lane == 0) sh.wave_best[taken & 1][wave] = last;
+        __syncthreads();
 #pragma unroll
-      for (int w = 0; w < kPartThreads / 64; ++w) last = max(last, sh.wave_best[taken & 1][w]);
+        for (int w = 0; w < kWaves; ++w) last = max(last, sh.wave_best[taken & 1][w]);
+      }
       if (tid == 0) keys[taken] = last;
     }
   }
   if (tid == 0) {
-    double all = 0.0;
+    if constexpr (TEAM != 64) {
+      sum = 0.0;
 #pragma unroll
-    for (int w = 0; w < kPartThreads / 64; ++w) all += sh.wave_sum[w];
-    a.counts[slot] = min(listed, a.width);
+      for (int w = 0; w < kWaves; ++w) sum += sh.wave_sum[w];
+    }
     a.tops[slot] = top;
-    a.sums[slot] = all;
+    a.sums[slot] = sum;
   }
 }
 
@@ -225,35 +398,41 @@ struct Place {
   }
 };
 
+template <int THREADS>
 struct JoinShared {
   float top[kMostWidth];                       // by walk of the group
   float logp[kMostWidth];
   double log_sum[kMostWidth];                  // log sum exp(s - top)
   uint8_t state[kMostWidth];                   // 0: no walk, 1: one, 2: one that has ended
-  uint64_t lane_top[kJoinThreads];
-  uint64_t bound;
+  uint64_t lane_top[THREADS];
+  uint64_t most;
+  uint32_t bins[kBins];
   uint32_t listed;
+  int cut;
   uint64_t p[kJoinList], in_row[kJoinList];
   uint32_t row[kJoinList];
-  Place wave_best[2][kJoinThreads / 64];
+  Place wave_best[2][THREADS / 64];
 };
 
-__global__ __launch_bounds__(kJoinThreads) void join_kernel(SelectArgs a) {
-  __shared__ JoinShared sh;
+// A workgroup a group: the parts' sums, then the first of all lists.  Of many candidates, first those above the width-th largest of the
+// lists' heads, then those from the step up, of a thousand equal ones between that and the largest, where the width-th lies.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void join_kernel(SelectArgs a) {
+  __shared__ JoinShared<THREADS> sh;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t group = blockIdx.x, first_row = group * a.beams;
-  if (tid == 0) sh.listed = 0;
-  for (int b = wave; b < a.beams; b += kJoinThreads / 64) {        // a wave adds a row's parts, in a fixed order
+  if (tid == 0) sh.listed = 0, sh.cut = 0;
+  for (int b = wave; b < a.beams; b += THREADS / 64) {            // a wave adds a row's parts, in a fixed order
     const int64_t slot = (first_row + b) * a.parts;
-    float top = -INFINITY;
-    for (int part = lane; part < a.parts; part += 64) top = fmaxf(top, a.tops[slot + part]);
+    const float own = lane < a.parts ? a.tops[slot + lane] : -INFINITY;      // both at once: most rows have no more parts
+    const double own_sum = lane < a.parts ? a.sums[slot + lane] : 0.0;
+    float top = own;
+    for (int part = 64 + lane; part < a.parts; part += 64) top = fmaxf(top, a.tops[slot + part]);
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-    double sum = 0.0;
-    for (int part = lane; part < a.parts; part += 64) {
-      const float t = a.tops[slot + part];
-      if (t > -INFINITY) sum += a.sums[slot + part] * (t == top ? 1.0 : exp((double)t - (double)top));
-    }
+    auto share = [&](double sum, float t) { return t > -INFINITY ? sum * (t == top ? 1.0 : exp((double)t - (double)top)) : 0.0; };
+    double sum = share(own_sum, own);
+    for (int part = 64 + lane; part < a.parts; part += 64) sum += share(a.sums[slot + part], a.tops[slot + part]);
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d, 64);
     if (lane == 0) {
@@ -266,36 +445,85 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(SelectArgs a) {
   }
   __syncthreads();
 
-  const int64_t lists = (int64_t)a.beams * a.parts;
-  auto size_of = [&](int b, int part) {        // candidates of a list
-    return sh.state[b] == 1 ? a.counts[(first_row + b) * a.parts + part] : sh.state[b] == 2 && part == 0 ? 1 : 0;
-  };
-  auto place_at = [&](int b, int part, int t) {
-    Place c{0, 0, (uint32_t)b};
-    if (sh.state[b] == 2) {
-      c.p = key64_of((double)sh.logp[b]);
-    } else {
-      c.in_row = a.keys[((first_row + b) * a.parts + part) * a.width + t];
-      const float s = score_of((uint32_t)(c.in_row >> 32));
+  const int64_t lists = (int64_t)a.beams * a.parts, candidates = lists * a.width;
+  const uint64_t* const keys = a.keys + first_row * a.parts * a.width;      // of the group: a candidate each, 0 where there is none
+  auto place_of_key = [&](int b, uint64_t key, bool first_of_row) {
+    Place c{0, key, (uint32_t)b};
+    if (sh.state[b] == 1 && key != 0) {
+      const float s = score_of((uint32_t)(key >> 32));
       c.p = key64_of((double)sh.logp[b] + ((s == sh.top[b] ? 0.0 : (double)s - (double)sh.top[b]) - sh.log_sum[b]));
+    } else if (sh.state[b] == 2 && first_of_row) {
+      c.p = key64_of((double)sh.logp[b]), c.in_row = 0;
     }
     return c;
   };
-
-  uint64_t own = 0;
-  for (int64_t l = tid; l < lists; l += kJoinThreads) {
-    const int b = (int)(l / a.parts), part = (int)(l - (int64_t)b * a.parts);
-    if (size_of(b, part) > 0) own = max(own, place_at(b, part, 0).p);
-  }
-  const uint64_t bound = max(bound_of<kJoinThreads>(own, a.width, sh.lane_top, &sh.bound), (uint64_t)1);
-  for (int64_t l = tid; l < lists; l += kJoinThreads) {
-    const int b = (int)(l / a.parts), part = (int)(l - (int64_t)b * a.parts), size = size_of(b, part);
-    for (int t = 0; t < size; ++t) {
-      const Place c = place_at(b, part, t);
-      if (c.p < bound) break;
-      const uint32_t to = atomicAdd(&sh.listed, 1u);
-      if (to < kJoinList) sh.p[to] = c.p, sh.in_row[to] = c.in_row, sh.row[to] = c.row;
+  auto place_at = [&](int b, int part, int t) {
+    return place_of_key(b, keys[((int64_t)b * a.parts + part) * a.width + t], part == 0 && t == 0);
+  };
+  // visit(candidate) for those of p >= least: a candidate each, or, of very many, a list each, most of which end at once
+  auto for_all = [&](uint64_t least, auto visit) {
+    if (candidates <= 64 * THREADS) {
+      const int per_row = a.parts * a.width;
+#pragma unroll 4
+      for (int c = tid; c < (int)candidates; c += THREADS) {
+        const int b = c / per_row;
+        const Place place = place_of_key(b, keys[c], c == b * per_row);
+        if (place.p >= least) visit(place);
+      }
+    } else {
+      for (int64_t l = tid; l < lists; l += THREADS) {
+        const int b = (int)(l / a.parts), part = (int)(l - (int64_t)b * a.parts);
+        for (int t = 0; t < a.width; ++t) {
+          const Place place = place_at(b, part, t);
+          if (place.p < least) break;
+          visit(place);
+        }
+      }
     }
+  };
+  auto take = [&](const Place& c) {
+    const uint32_t to = atomicAdd(&sh.listed, 1u);
+    if (to < (uint32_t)kJoinList) sh.p[to] = c.p, sh.in_row[to] = c.in_row, sh.row[to] = c.row;
+  };
+  if (candidates <= kCounted) {
+    for_all(1, take);
+  } else {
+    uint64_t own = 0;
+    for (int64_t l = tid; l < lists; l += THREADS) {
+      const int b = (int)(l / a.parts), part = (int)(l - (int64_t)b * a.parts);
+      own = max(own, place_at(b, part, 0).p);
+    }
+    for (int i = tid; i < kBins; i += THREADS) sh.bins[i] = 0;
+    const uint64_t most = wave_most(own);
+    if (lane == 0) sh.wave_best[0][wave].p = most;
+    const uint64_t least = max(bound_of<THREADS>(own, a.width, sh.lane_top), (uint64_t)1);
+    uint64_t largest = 0;
+    for (int w = 0; w < THREADS / 64; ++w) largest = max(largest, sh.wave_best[0][w].p);
+    // steps between least and largest: every operation is monotone, which is all that a cut needs
+    const double low = least > 1 ? value_of(least) : largest ? value_of(largest) - 100.0 : 0.0, range = (largest ? value_of(largest) : 0.0) - low;
+    const double per_step = range > 0.0 && range < 1e300 ? (double)(kBins - 1) / range : 0.0;
+    auto bin_of = [&](const Place& c) { return (int)fmax(0.0, fmin((value_of(c.p) - low) * per_step, (double)(kBins - 1))); };
+    for_all(least, [&](const Place& c) { atomicAdd(&sh.bins[bin_of(c)], 1u); });
+    __syncthreads();
+    if (wave == 0) {                           // the last bin from which on there are `width`, or the first
+      constexpr int kEach = kBins / 64;
+      uint32_t mine = 0;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) mine += sh.bins[(63 - lane) * kEach + i];      // lane 0: the highest bins
+      const uint32_t upto = wave_inclusive(mine, lane);
+      const uint64_t enough = __ballot(upto >= (uint32_t)a.width);
+      if (enough != 0 && lane == (int)__builtin_ctzll(enough)) {
+        uint32_t count = upto - mine;
+        int bin = (63 - lane) * kEach + kEach;
+        while (count < (uint32_t)a.width) count += sh.bins[--bin];
+        sh.cut = bin;
+      }
+    }
+    __syncthreads();
+    const int cut = sh.cut;
+    for_all(least, [&](const Place& c) {
+      if (bin_of(c) >= cut) take(c);
+    });
   }
   __syncthreads();
 
@@ -307,14 +535,33 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(SelectArgs a) {
     a.logp_out[to] = there ? (float)value_of(c.p) : -INFINITY;
   };
   const int listed = (int)sh.listed;
-  if (listed <= kJoinList) {
-    for (int c = tid; c < listed; c += kJoinThreads) {
-      const Place own{sh.p[c], sh.in_row[c], sh.row[c]};
+  auto at = [&](int i) { return Place{sh.p[i], sh.in_row[i], sh.row[i]}; };
+  if (listed <= kCounted) {
+    for (int c = tid; c < listed; c += THREADS) {
+      const Place own = at(c);
       int before = 0;
-      for (int o = 0; o < listed; ++o) before += Place{sh.p[o], sh.in_row[o], sh.row[o]}.before(own);
+#pragma unroll 4
+      for (int o = 0; o < listed; ++o) {       // without branches: equal ones are common among 16-bit scores
+        const uint64_t p = sh.p[o], in_row = sh.in_row[o];
+        const uint32_t row = sh.row[o];
+        before += (p > own.p) | ((p == own.p) & ((row < own.row) | ((row == own.row) & (in_row > own.in_row))));
+      }
       if (before < a.width) write(before, own);
     }
-    for (int at = listed + tid; at < a.width; at += kJoinThreads) write(at, Place{0, 0, 0});
+    for (int c = listed + tid; c < a.width; c += THREADS) write(c, Place{0, 0, 0});
+    return;
+  }
+  if (listed <= kJoinList) {
+    const int n = power_of_two(listed);
+    for (int c = listed + tid; c < n; c += THREADS) sh.p[c] = 0, sh.in_row[c] = 0, sh.row[c] = 0;
+    __syncthreads();
+    sort_list<THREADS>(n, [&](int i, int j) { return sh.p[i] > sh.p[j] || (sh.p[i] == sh.p[j] && at(i).before(at(j))); },
+                       [&](int i, int j) {
+                         const Place x = at(i);
+                         sh.p[i] = sh.p[j], sh.in_row[i] = sh.in_row[j], sh.row[i] = sh.row[j];
+                         sh.p[j] = x.p, sh.in_row[j] = x.in_row, sh.row[j] = x.row;
+                       });
+    for (int c = tid; c < a.width; c += THREADS) write(c, c < listed ? at(c) : Place{0, 0, 0});
     return;
   }
   // The best is taken out `width` times; a lane looks again through its own lists only where it was its own.
@@ -322,11 +569,12 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(SelectArgs a) {
   for (int taken = 0; taken < a.width; ++taken) {
     if (!last.before(best)) {
       best = Place{0, 0, 0};
-      for (int64_t l = tid; l < lists; l += kJoinThreads) {
-        const int b = (int)(l / a.parts), part = (int)(l - (int64_t)b * a.parts), size = size_of(b, part);
-        for (int t = 0; t < size; ++t) {
+      for (int64_t l = tid; l < lists; l += THREADS) {
+        const int b = (int)(l / a.parts), part = (int)(l - (int64_t)b * a.parts);
+        for (int t = 0; t < a.width; ++t) {
           const Place c = place_at(b, part, t);
-          if (c.p == 0 || !last.before(c)) continue;
+          if (c.p == 0) break;
+          if (!last.before(c)) continue;
           if (c.before(best)) best = c;
           break;
         }
@@ -344,18 +592,17 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(SelectArgs a) {
     if (lane == 0) sh.wave_best[taken & 1][wave] = most;
     __syncthreads();
     last = sh.wave_best[taken & 1][0];
-    for (int w = 1; w < kJoinThreads / 64; ++w)
+    for (int w = 1; w < THREADS / 64; ++w)
       if (sh.wave_best[taken & 1][w].before(last)) last = sh.wave_best[taken & 1][w];
     if (tid == 0) write(taken, last);
   }
 }
 
 struct SelectPlan {
-  int loads;
+  int loads, team;
   int32_t parts;
   int64_t part_len;
   uint64_t* keys;
-  int32_t* counts;
   float* tops;
   double* sums;
   size_t bytes;
@@ -365,13 +612,18 @@ SelectPlan plan_select(void* ws, int64_t groups, int32_t beams, int64_t n, int32
   SelectPlan p{};
   const int64_t per = dtype == GS_F32 ? 4 : 8, rows = groups * beams;
   // Few rows: parts small enough that every compute unit has one.
-  p.loads = dtype == GS_F32 ? 16 : 8;
-  while (p.loads > 2 && rows * ceil_div(n, per * kPartThreads * p.loads) < 512) p.loads /= 2;
-  p.part_len = per * kPartThreads * p.loads;
+  const int most = dtype == GS_F32 ? 16 : 8;                      // 64 scores a lane
+  p.team = n <= 64 * per * most && width <= 32 && rows >= 256 ? 64 : kPartThreads;      // short rows: a wave each
+  p.loads = most;
+  if (p.team == 64) {
+    while (p.loads > 2 && n <= 64 * per * p.loads / 2) p.loads /= 2;
+  } else {
+    while (p.loads > 2 && rows * ceil_div(n, per * kPartThreads * p.loads) < 512) p.loads /= 2;
+  }
+  p.part_len = per * p.team * p.loads;
   p.parts = (int32_t)ceil_div(n, p.part_len);
   Carver carve(ws);
   p.keys = carve.take<uint64_t>((size_t)rows * p.parts * width);
-  p.counts = carve.take<int32_t>((size_t)rows * p.parts);
   p.tops = carve.take<float>((size_t)rows * p.parts);
   p.sums = carve.take<double>((size_t)rows * p.parts);
   p.bytes = carve.used;
@@ -386,12 +638,18 @@ bool select_shape_ok(int64_t groups, int32_t beams, int64_t n, int32_t width, in
          n <= (int64_t)INT32_MAX && dtype_known(dtype);
 }
 
+template <typename V, int TEAM>
+void launch_parts(const SelectArgs& a, int loads, int64_t slots, hipStream_t s) {
+  const dim3 grid((unsigned)ceil_div(slots, kPartThreads / TEAM));
+  if (sizeof(typename V::elem) == 4 && loads == 16) part_kernel<V, sizeof(typename V::elem) == 4 ? 16 : 8, TEAM><<<grid, kPartThreads, 0, s>>>(a, slots);
+  if (loads == 8) part_kernel<V, 8, TEAM><<<grid, kPartThreads, 0, s>>>(a, slots);
+  if (loads == 4) part_kernel<V, 4, TEAM><<<grid, kPartThreads, 0, s>>>(a, slots);
+  if (loads == 2) part_kernel<V, 2, TEAM><<<grid, kPartThreads, 0, s>>>(a, slots);
+}
 template <typename V>
-void launch_parts(const SelectArgs& a, int loads, unsigned grid, hipStream_t s) {
-  if (loads == 16) part_kernel<V, 16><<<dim3(grid), kPartThreads, 0, s>>>(a);
-  if (loads == 8) part_kernel<V, 8><<<dim3(grid), kPartThreads, 0, s>>>(a);
-  if (loads == 4) part_kernel<V, 4><<<dim3(grid), kPartThreads, 0, s>>>(a);
-  if (loads == 2) part_kernel<V, 2><<<dim3(grid), kPartThreads, 0, s>>>(a);
+void launch_parts(const SelectArgs& a, const SelectPlan& p, int64_t slots, hipStream_t s) {
+  if (p.team == 64) launch_parts<V, 64>(a, p.loads, slots, s);
+  else launch_parts<V, kPartThreads>(a, p.loads, slots, s);
 }
 
 }  // namespace
@@ -542,14 +800,15 @@ extern "C" int32_t gs_beam_select(const void* scores, int64_t groups, int32_t be
   if (ws_bytes < p.bytes) return GS_EWORKSPACE;
   const int64_t grid = groups * beams * p.parts;
   if (grid > (int64_t)INT32_MAX) return GS_EOVERFLOW;
-  const SelectArgs a{scores, groups, groups * beams, n, beams, width, logp, ended, p.parts, p.part_len, p.keys, p.counts, p.tops, p.sums, parents_out,
+  const SelectArgs a{scores, groups, groups * beams, n, beams, width, logp, ended, p.parts, p.part_len, p.keys, p.tops, p.sums, parents_out,
                      nodes_out, logp_out};
   const hipStream_t s = (hipStream_t)stream;
-  if (dtype == GS_F32) launch_parts<ScoreF32>(a, p.loads, (unsigned)grid, s);
-  if (dtype == GS_BF16) launch_parts<ScoreHalf<bf16_t>>(a, p.loads, (unsigned)grid, s);
-  if (dtype == GS_F16) launch_parts<ScoreHalf<f16_t>>(a, p.loads, (unsigned)grid, s);
+  if (dtype == GS_F32) launch_parts<ScoreF32>(a, p, grid, s);
+  if (dtype == GS_BF16) launch_parts<ScoreHalf<bf16_t>>(a, p, grid, s);
+  if (dtype == GS_F16) launch_parts<ScoreHalf<f16_t>>(a, p, grid, s);
   GS_LAUNCH_CHECK();
-  join_kernel<<<dim3((unsigned)groups), kJoinThreads, 0, s>>>(a);
+  if ((int64_t)beams * p.parts * width > 4096) join_kernel<1024><<<dim3((unsigned)groups), 1024, 0, s>>>(a);
+  else join_kernel<256><<<dim3((unsigned)groups), 256, 0, s>>>(a);
   GS_LAUNCH_CHECK();
   return GS_OK;
 }

@@ -132,6 +132,7 @@ __device__ __forceinline__ void wave_fence() {
 // 32-bit word exactly; round() gives the 16 bits nearest to an fp32 value (ties to even).
 struct bf16_t {
   uint16_t bits;
+  static constexpr uint32_t kNone = 0xff80ff80u;                    // -infinity in both halves
   static __device__ __forceinline__ float lo(uint32_t w) { return __uint_as_float(w << 16); }
   static __device__ __forceinline__ float hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
   static __device__ __forceinline__ uint32_t round(float f) {      // finite inputs
@@ -141,6 +142,7 @@ struct bf16_t {
 };
 struct f16_t {                                                      // IEEE binary16
   uint16_t bits;
+  static constexpr uint32_t kNone = 0xfc00fc00u;
   static __device__ __forceinline__ float lo(uint32_t w) {
     return __half2float(__ushort_as_half((unsigned short)(w & 0xffffu)));
   }

@@ -8,12 +8,15 @@ namespace {
 
 struct ScoreF32 {
   typedef float elem;
+  static constexpr uint32_t kNone = 0xff800000u;      // -infinity
   static __device__ __forceinline__ float get(float x) { return x; }
 };
 template <typename H>
 struct ScoreHalf {
   typedef uint16_t elem;
+  static constexpr uint32_t kNone = H::kNone;         // -infinity, twice
   static __device__ __forceinline__ float get(uint16_t x) { return H::lo(x); }
+  static __device__ __forceinline__ float get_of(uint32_t word, int which) { return which ? H::hi(word) : H::lo(word); }
 };
 
 // 0: left out (-infinity or NaN); otherwise larger keys for larger scores, one key for both zeros
