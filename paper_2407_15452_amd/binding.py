@@ -70,6 +70,13 @@ class StateStruct(C.Structure):
     _fields_ = [("data", C.c_void_p), ("out", C.c_void_p), ("row_bytes", C.c_int64), ("append_at", C.c_int64)]
 
 
+# Arguments of the calls that are made once for every token or walk: p pointer, q int64, i int32, f float, z size.
+SIGNATURES = {
+    "gs_quantize_rows": "pqiipqpppp", "gs_scores_q8_workspace_bytes": "qqi", "gs_scores_q8": "ppqppqipqpfpipzp",
+    "gs_beam_select_workspace_bytes": "qiqii", "gs_beam_select": "pqiqippippppzp", "gs_beam_reorder": "piqiippp",
+}
+_TYPES = {"p": C.c_void_p, "q": C.c_int64, "i": C.c_int32, "f": C.c_float, "z": C.c_size_t}
+
 _lib = None
 
 
@@ -85,6 +92,8 @@ def lib() -> C.CDLL:
         for name in EXPORTS:
             fn = getattr(l, name)
             fn.restype = C.c_size_t if name.endswith("_workspace_bytes") else C.c_int32
+            if name in SIGNATURES:
+                fn.argtypes = [_TYPES[t] for t in SIGNATURES[name]]
         _lib = l
     return _lib
 
@@ -714,13 +723,30 @@ def _one_device(dev, **tensors):
         raise ValueError(f"{dev} must be the current device")
 
 
+def _at(t, dtype, name):
+    """The address of a tensor, or None; its type is checked where one is given."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _stream_of(dev):
+    return torch._C._cuda_getCurrentRawStream(dev.index)     # torch.cuda.current_stream takes as long as a launch
+
+
 class Table8:
     """Rows of 8-bit values for answers: data float8_e4m3fn [rows, pitch], scales float8_e8m0fnu [rows, scale pitch], a scale for
     each block of 128 of the `dim` columns (see gs.h).  ``Table8.empty`` makes room for one."""
 
     def __init__(self, data: torch.Tensor, scales: torch.Tensor, dim: int):
-        _dev(data, torch.float8_e4m3fn, "data")
-        _dev(scales, torch.float8_e8m0fnu, "scales")
+        _at(data, torch.float8_e4m3fn, "data")
+        _at(scales, torch.float8_e8m0fnu, "scales")
         pitch, scale_pitch = self.pitches(dim)
         if data.dim() != 2 or data.shape[1] != pitch or tuple(scales.shape) != (data.shape[0], scale_pitch):
             raise ValueError(f"rows of {dim} columns are data [rows, {pitch}] and scales [rows, {scale_pitch}]")
@@ -756,15 +782,14 @@ def gs_quantize_rows(table, ids=None, count=None, out=None) -> Table8:
     if out.num_nodes != num_nodes or out.dim != dim:
         raise ValueError(f"out must have {num_nodes} rows of {dim} columns")
     n = num_nodes if ids is None else int(ids.numel())
-    rc = lib().gs_quantize_rows(_dev(table, None, "table"), C.c_int64(num_nodes), C.c_int32(dim), C.c_int32(dtype),
-                                _dev(ids, torch.int32, "ids"), C.c_int64(n), _dev(count, torch.int64, "count"), _dev(out.data),
-                                _dev(out.scales), _stream())
+    rc = lib().gs_quantize_rows(_at(table, None, "table"), num_nodes, dim, dtype, _at(ids, torch.int32, "ids"), n, _at(count, torch.int64, "count"),
+                                out.data.data_ptr(), out.scales.data_ptr(), _stream_of(table.device))
     _check(rc, "gs_quantize_rows")
     return out
 
 
 def gs_scores_q8_workspace_bytes(num_centers: int, num_nodes: int, dim: int) -> int:
-    return int(lib().gs_scores_q8_workspace_bytes(C.c_int64(num_centers), C.c_int64(num_nodes), C.c_int32(dim)))
+    return int(lib().gs_scores_q8_workspace_bytes(num_centers, num_nodes, dim))
 
 
 def gs_scores_q8(t_in: Table8, t_out: Table8, centers, bias=None, scale: float = 1.0, dtype=torch.float32, out=None, ws=None):
@@ -779,15 +804,15 @@ def gs_scores_q8(t_in: Table8, t_out: Table8, centers, bias=None, scale: float =
     if ws is None:
         ws = _workspace(gs_scores_q8_workspace_bytes(n, t_out.num_nodes, t_out.dim), dev)
     rc = lib().gs_scores_q8(
-        _dev(t_in.data), _dev(t_in.scales), C.c_int64(t_in.num_nodes), _dev(t_out.data), _dev(t_out.scales), C.c_int64(t_out.num_nodes),
-        C.c_int32(t_out.dim), _dev(centers, torch.int32, "centers"), C.c_int64(n), _dev(bias, torch.float32, "bias"), C.c_float(scale),
-        _dev(out, None, "out"), C.c_int32(_table_dtype(out)), _dev(ws), C.c_size_t(ws.numel()), _stream())
+        t_in.data.data_ptr(), t_in.scales.data_ptr(), t_in.num_nodes, t_out.data.data_ptr(), t_out.scales.data_ptr(), t_out.num_nodes, t_out.dim,
+        _at(centers, torch.int32, "centers"), n, _at(bias, torch.float32, "bias"), scale, _at(out, None, "out"), _table_dtype(out),
+        _at(ws, torch.uint8, "ws"), ws.numel(), _stream_of(dev))
     _check(rc, "gs_scores_q8")
     return out
 
 
 def gs_beam_select_workspace_bytes(groups: int, beams: int, n: int, width: int, dtype: int = GS_F32) -> int:
-    return int(lib().gs_beam_select_workspace_bytes(C.c_int64(groups), C.c_int32(beams), C.c_int64(n), C.c_int32(width), C.c_int32(dtype)))
+    return int(lib().gs_beam_select_workspace_bytes(groups, beams, n, width, dtype))
 
 
 def gs_beam_select(scores, logp, beams: int, width: int, ended=None, parents_out=None, nodes_out=None, logp_out=None, ws=None):
@@ -810,9 +835,9 @@ def gs_beam_select(scores, logp, beams: int, width: int, ended=None, parents_out
     if ws is None:
         ws = _workspace(gs_beam_select_workspace_bytes(groups, beams, n, width, dtype), dev)
     rc = lib().gs_beam_select(
-        _dev(scores, None, "scores"), C.c_int64(groups), C.c_int32(beams), C.c_int64(n), C.c_int32(dtype), _dev(logp, torch.float32, "logp"),
-        _dev(ended, torch.uint8, "ended"), C.c_int32(width), _dev(parents_out), _dev(nodes_out), _dev(logp_out), _dev(ws),
-        C.c_size_t(ws.numel()), _stream())
+        _at(scores, None, "scores"), groups, beams, n, dtype, _at(logp, torch.float32, "logp"), _at(ended, torch.uint8, "ended"), width,
+        _at(parents_out, None, "parents_out"), _at(nodes_out, None, "nodes_out"), _at(logp_out, None, "logp_out"), _at(ws, torch.uint8, "ws"),
+        ws.numel(), _stream_of(dev))
     _check(rc, "gs_beam_select")
     return parents_out, nodes_out, logp_out
 
@@ -833,17 +858,17 @@ def gs_beam_reorder(states, parents, beams: int, outs=None, nodes=None, columns=
     _one_device(parents.device, nodes=nodes, **{f"states[{i}]": x for i, x in enumerate(states)}, **{f"outs[{i}]": x for i, x in enumerate(outs)})
     array = (StateStruct * len(states))()
     for i, (x, out, column) in enumerate(zip(states, outs, columns)):
-        data = _dev(x, None, "state")
+        data = _at(x, None, "state")
         if x.dim() < 1 or x.shape[0] != groups * beams:
             raise ValueError(f"a state must have {groups * beams} rows")
         if out is not None and (out.dtype != x.dtype or tuple(out.shape) != (groups * width, *x.shape[1:])):
             raise ValueError("an output must have its state's type and rows")
         if out is None and beams != width:
             raise ValueError("in place there are as many walks as before: pass outs")
-        row_bytes = x[0].numel() * x.element_size() if groups else 0
+        row_bytes = x.numel() // x.shape[0] * x.element_size() if groups else 0
         if column is not None and (x.dim() != 2 or x.dtype != torch.int32 or not 0 <= column < x.shape[1] or nodes is None):
             raise ValueError("nodes are written to a column of an int32 state [rows, columns]")
-        array[i] = StateStruct(data, None if out is None else _dev(out, None, "output"), row_bytes, -1 if column is None else 4 * column)
-    rc = lib().gs_beam_reorder(array, C.c_int32(len(states)), C.c_int64(groups), C.c_int32(beams), C.c_int32(width),
-                               _dev(parents, torch.int32, "parents"), _dev(nodes, torch.int32, "nodes"), _stream())
+        array[i] = StateStruct(data, _at(out, None, "output"), row_bytes, -1 if column is None else 4 * column)
+    rc = lib().gs_beam_reorder(C.addressof(array), len(states), groups, beams, width, _at(parents, torch.int32, "parents"),
+                               _at(nodes, torch.int32, "nodes"), _stream_of(parents.device))
     _check(rc, "gs_beam_reorder")

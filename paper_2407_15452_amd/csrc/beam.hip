@@ -205,9 +205,10 @@ struct PartShared {
 };
 
 // Parts of rows, TEAM lanes each: a workgroup, or a wave, which then needs no barrier but the table's.
-constexpr int waves_of(int scores, int team) { return scores >= 64 ? (team == 64 ? 2 : 3) : scores >= 32 ? 3 : 4; }      // on a SIMD
+template <int SCORES, int TEAM>
+constexpr int kWavesOf = SCORES >= 64 ? (TEAM == 64 ? 2 : 3) : SCORES >= 32 ? 3 : 4;      // on a SIMD
 template <typename V, int LOADS, int TEAM>
-__global__ __launch_bounds__(kPartThreads, waves_of(LOADS * Raw<V>::kPer, TEAM)) void part_kernel(SelectArgs a, int64_t slots) {
+__global__ __launch_bounds__(kPartThreads, (kWavesOf<LOADS * Raw<V>::kPer, TEAM>)) void part_kernel(SelectArgs a, int64_t slots) {
   typedef typename V::elem elem;
   constexpr int kPer = Raw<V>::kPer, kWaves = kPartThreads / 64, kList = TEAM == 64 ? kPartList / kWaves : kPartList;
   __shared__ PartShared<LOADS, TEAM> sh;

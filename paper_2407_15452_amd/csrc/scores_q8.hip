@@ -527,8 +527,10 @@ __global__ __launch_bounds__(320, 2) void strip_kernel(ScoresArgs a, int64_t gro
 
   if (wave == S::kWaves) {                     // the wave that loads
     const int row = (lane >> 3) * a.pitch, piece = ((lane & 7) ^ (lane >> 4)) * 16;
+    int next = 0;                              // slot
     auto issue = [&](int64_t t) {
-      uint8_t* slot = slots[(t - first) / every % S::kSlots];
+      uint8_t* slot = slots[next];
+      next = next + 1 == S::kSlots ? 0 : next + 1;
       const int64_t n0 = t * S::kNodes;
       const int nodes = (int)max((int64_t)0, min((int64_t)S::kNodes, a.num_nodes - n0));
       const int64_t from = t < last ? n0 : 0;  // beyond the range: nothing, but as many loads
@@ -601,9 +603,11 @@ __global__ __launch_bounds__(320, 2) void strip_kernel(ScoresArgs a, int64_t gro
   int at_n[4];
 #pragma unroll
   for (int c = 0; c < 4; ++c) at_n[c] = at * kBlock + (((4 * (c >> 1) + 2 * half + (c & 1)) ^ ((at >> 1) & 7)) * 16);
+  int at_slot = 0;
   for (int64_t t = first; t < last; t += every) {
     meet();
-    const uint8_t* slot = slots[(t - first) / every % S::kSlots];
+    const uint8_t* slot = slots[at_slot];
+    at_slot = at_slot + 1 == S::kSlots ? 0 : at_slot + 1;
     const uint8_t* side = slot + S::kRows;
     const int64_t n0 = t * S::kNodes;
     const int nodes = (int)min((int64_t)S::kNodes, a.num_nodes - n0);
