@@ -591,8 +591,11 @@ int32_t gs_clip_grads(const gs_tensor* list, int32_t num_tensors, double max_nor
  *
  * gs_scores_q8 -- gs_scores from 8-bit tables: scores_out[i][j] = scale * <row centers[i] of
  *   the one table, row j of the other> + bias[j], of the values that their bytes stand for.
- *   Sums are fp32.  scores_out [num_centers][num_nodes] of dtype GS_F32 | GS_BF16 | GS_F16
- *   (one rounding, from fp32), aligned to its element.  bias, masked nodes and centres that
+ *   scores_out [num_centers][num_nodes] of dtype GS_F32 | GS_BF16 | GS_F16 (one rounding, from
+ *   fp32), aligned to its element.  Sums are fp32.  For fp32 scores products are exact; for 16-bit
+ *   ones the products of eight neighbouring columns keep what lies within 2^-13 of the largest of
+ *   them: at most 7 * 2^-13 of the sum of all products' sizes is lost, some 2^-16 of it for Gaussian
+ *   rows.  bias, masked nodes and centres that
  *   are no row as for gs_scores; a scale NaN makes the scores of its row NaN.
  *   Same bits on every run.  Errors: GS_EINVAL, GS_EOVERFLOW for 2^21 centres and
  *   more, or more tiles of 128 x 128 scores than a launch takes (2^31).
@@ -620,9 +623,10 @@ int32_t gs_scores_q8(const void* q_in, const void* scales_in, int64_t num_in, co
  *   ended  uint8[groups * beams] or NULL: a walk that has ended (not 0) is one candidate, itself:
  *   node -1 and p = logp[r]; its scores are not looked at.
  *   parents_out, nodes_out int32[groups][width], logp_out float[groups][width] (p, rounded
- *   once): b, j and p.  Where a group has fewer candidates: -1, -1 and -infinity.
- *   p is that of the definition to 2e-14 (1 + |p| + log n): candidates of different walks nearer
- *   than that may change places.  Same answer on every run, and for equal rows.
+ *   once): b, j and p.  Where a group has fewer candidates: -1, -1 and -infinity.  logp_out may be
+ *   logp itself where width == beams; outputs overlap no input otherwise.
+ *   p is that of the definition to 6e-14 (1 + |p| + |logp| + log n): candidates of different walks
+ *   nearer than that may change places.  Same answer on every run, and for equal rows.
  *   1 <= n < 2^31, 1 <= beams, width <= 256, groups * beams < 2^22.  Errors: GS_EINVAL,
  *   GS_EOVERFLOW for more rows.
  *
@@ -634,7 +638,7 @@ int32_t gs_scores_q8(const void* q_in, const void* scales_in, int64_t num_in, co
  *   int32[len]: 4 * position; -1, behind a walk that has ended, as gs_random_walk writes it);
  *   a multiple of 4, as row_bytes and both addresses are then.  -1: nothing is.
  *   data [groups * beams][row_bytes], out [groups * width][row_bytes]; no state may overlap
- *   another's out, nor its own out its data otherwise.  beams, width at most 256,
+ *   another's out, nor its own out its data otherwise, nor any out parents or nodes.  beams, width at most 256,
  *   groups * max(beams, width) < 2^22 (GS_EOVERFLOW), row_bytes >= 0 below 2^40.
  * ------------------------------------------------------------------------ */
 size_t gs_beam_select_workspace_bytes(int64_t groups, int32_t beams, int64_t n, int32_t width, int32_t dtype);

@@ -631,6 +631,10 @@ SelectPlan plan_select(void* ws, int64_t groups, int32_t beams, int64_t n, int32
   return p;
 }
 
+bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return a_bytes > 0 && b_bytes > 0 && x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
+}
 bool dtype_known(int32_t dtype) { return dtype == GS_F32 || dtype == GS_BF16 || dtype == GS_F16; }
 constexpr int64_t kMostRows = ((int64_t)1 << 22) - 1;
 // before the products that they bound
@@ -773,11 +777,6 @@ int64_t move_blocks(int64_t pieces, int64_t groups, int32_t beams) {
   return groups * ceil_div(pieces, wide);
 }
 
-bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
-  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  return a_bytes > 0 && b_bytes > 0 && x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
-}
-
 }  // namespace
 }  // namespace gs
 
@@ -801,6 +800,8 @@ extern "C" int32_t gs_beam_select(const void* scores, int64_t groups, int32_t be
   if (ws_bytes < p.bytes) return GS_EWORKSPACE;
   const int64_t grid = groups * beams * p.parts;
   if (grid > (int64_t)INT32_MAX) return GS_EOVERFLOW;
+  // a group's workgroup reads its walks before it writes: those alone where both begin alike
+  if (!(logp_out == logp && width == beams) && overlap(logp_out, groups * width * 4, logp, groups * beams * 4)) return GS_EINVAL;
   const SelectArgs a{scores, groups, groups * beams, n, beams, width, logp, ended, p.parts, p.part_len, p.keys, p.tops, p.sums, parents_out,
                      nodes_out, logp_out};
   const hipStream_t s = (hipStream_t)stream;
@@ -836,6 +837,8 @@ extern "C" int32_t gs_beam_reorder(const gs_state* list, int32_t num_states, int
       const gs_state &x = list[i], &y = list[j];
       const bool in_place = !x.out || x.out == x.data, other_in_place = !y.out || y.out == y.data;
       const void* out = in_place ? x.data : x.out;
+      if (j == 0 && (overlap(out, rows_out * x.row_bytes, parents, rows_out * 4) || overlap(out, rows_out * x.row_bytes, nodes, nodes ? rows_out * 4 : 0)))
+        return GS_EINVAL;
       if (!(i == j && in_place) && overlap(out, rows_out * x.row_bytes, y.data, rows_in * y.row_bytes)) return GS_EINVAL;
       if (i != j && !other_in_place && overlap(out, rows_out * x.row_bytes, y.out, rows_out * y.row_bytes)) return GS_EINVAL;
     }

@@ -113,6 +113,12 @@ def test_select_refuses(lib, bad):
     assert select(lib, **bad) == EINVAL
 
 
+@pytest.mark.parametrize("more", [dict(out=at(1 << 20), logp=at(1 << 20), width=5), dict(out=at((1 << 20) + 44), logp=at(1 << 20)),
+                                  dict(out=at((1 << 20) - 56), logp=at(1 << 20)), dict(out=at((1 << 20) + 4), logp=at(1 << 20), width=4)], ids=str)
+def test_select_refuses_overlaps(lib, more):
+    assert select(lib, **more) == EINVAL
+
+
 def test_select_sizes(lib):
     assert select(lib, groups=0) == 0
     assert select(lib, groups=1 << 22, beams=1) == EOVERFLOW and select(lib, groups=1 << 14, beams=256) == EOVERFLOW
@@ -147,7 +153,9 @@ A, B = 1 << 30, 1 << 31
     # overlaps: an output and its state, an output and another state, two outputs, a state moved in place and another's output
     ([(A, A + 8, 8, -1)], {}), ([(A, A - 8, 8, -1)], {}), ([(A, A + 47, 8, -1)], {}), ([(A, B, 8, -1), (B + 40, None, 8, -1)], {}),
     ([(A, B, 8, -1), (A + 4096, B + 47, 8, -1)], {}), ([(A, None, 8, -1), (B, A + 8, 8, -1)], {}), ([(A, None, 8, -1), (A, None, 8, -1)], {}),
-    ([(A, None, 8, -1), (A + 40, None, 8, -1)], {}), ([(A, B, 8, -1)] * 2, {})], ids=str)
+    ([(A, None, 8, -1), (A + 40, None, 8, -1)], {}), ([(A, B, 8, -1)] * 2, {}),
+    # an output and the choice itself
+    ([(A, B, 8, -1)], dict(parents=at(B + 44))), ([(A, B, 8, -1)], dict(nodes=at(B - 20))), ([(A, None, 8, 4)], dict(parents=at(A)))], ids=str)
 def test_reorder_refuses(lib, states, more):
     assert reorder(lib, states, **more) == EINVAL
 

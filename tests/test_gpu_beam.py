@@ -1,7 +1,9 @@
 """gs_beam_select and gs_beam_reorder against their definitions, in 64 bits.
 
 Parents and nodes are equal.  logp is fp64 rounded to fp32 once: half a step, 2^-24 of it, and what the definition leaves to p,
-2e-14 (1 + |p| + log n)."""
+6e-14 (1 + |p| + |logp| + log n): weights 2^r, |r| <= 1/128, end with the fourth term of their series, and the fifth is
+(log 2 / 128)^5 / 120 = 3.9e-14 of a weight, so of the sum at most, and of its logarithm; the exponents' roundings take 2^-52 |x| exp(x),
+x <= 0, of the largest weight, less than 2^-53, and the handful of operations on p half a step of their numbers each, 2^-53."""
 import math
 
 import numpy as np
@@ -60,8 +62,8 @@ def check(gs, scores, logp, beams, width, ended=None):
     assert np.array_equal(nodes, want[1])
     fine = np.isfinite(want[2])
     assert np.array_equal(p[~fine], want[2][~fine].astype(np.float32))
-    size = np.abs(want[2][fine])
-    assert (np.abs(p[fine].astype(np.float64) - want[2][fine]) <= 2.0 ** -24 * size + 2e-14 * (1 + size + math.log(scores.shape[1])) + 2.0 ** -150).all()
+    size, before = np.abs(want[2][fine]), float(logp[torch.isfinite(logp)].abs().max()) if bool(torch.isfinite(logp).any()) else 0.0
+    assert (np.abs(p[fine].astype(np.float64) - want[2][fine]) <= 2.0 ** -24 * size + 6e-14 * (1 + size + before + math.log(scores.shape[1])) + 2.0 ** -150).all()
     return got
 
 
@@ -337,3 +339,86 @@ def test_a_search(gs):
         logp = new
     assert torch.equal(rows, gs.gs_get_rows(w_in, walks[:, 0].contiguous()))
     assert bool((walks[:, 0].view(groups, beams) == starts[:, None]).all()) and bool((logp[:, :-1] >= logp[:, 1:]).all())
+
+
+@pytest.mark.parametrize("dtype", list(TORCH))
+@pytest.mark.parametrize("n", [1, 63, 64, 1000, 2049, 4096])
+@pytest.mark.parametrize("width", [1, 20, 32])
+def test_many_short_rows(gs, n, width, dtype):
+    """Rows that a wave each takes: all different, few values, all equal, rising; walks that ended or are none in between."""
+    groups, beams = 43, 6
+    rows = groups * beams
+    z, logp = some(rows, n, dtype, n + width)
+    gen = torch.Generator().manual_seed(n)
+    z[::4] = torch.randint(-2, 2, (z[::4].shape[0], n), generator=gen).to(TORCH[dtype]).to(DEV)
+    z[1::8] = 0.5
+    z[5::8] = torch.linspace(-3, 3, n).to(TORCH[dtype]).to(DEV)
+    z[7::16] = torch.nan
+    z[9::32, n // 2] = INF
+    logp[::11], logp[3::17] = -INF, -1.0
+    ended = (torch.rand(rows, generator=gen) < 0.1).to(DEV)
+    check(gs, z, logp, beams, width, ended)
+
+
+@pytest.mark.parametrize("dtype", list(TORCH))
+@pytest.mark.parametrize("groups,beams,n,width", [(1, 256, 20, 256), (2, 256, 9000, 40), (3, 130, 2, 200), (1, 64, 40_000, 250)])
+def test_more_equal_candidates_than_a_list_takes(gs, groups, beams, n, width, dtype):
+    logp = torch.full((groups * beams,), -3.0, device=DEV)
+    logp[beams // 2] = -4.0
+    check(gs, torch.zeros(groups * beams, n, dtype=TORCH[dtype], device=DEV), logp, beams, width)
+    step = torch.zeros(groups * beams, n)
+    step[:, 1::2] = 0.25
+    check(gs, step.to(TORCH[dtype]).to(DEV), logp, beams, width)
+
+
+@pytest.mark.parametrize("n", [10, 20_000])
+def test_certain_walks(gs, n):
+    """log-probabilities of +infinity, and above 0: nothing but an order."""
+    z, logp = some(10, n, "f32", 2)
+    logp[3], logp[7], logp[8] = INF, 5.0, 5.0
+    parents, nodes, p = gs.gs_beam_select(z, logp, 5, 8)
+    best = torch.sort(z[3], descending=True, stable=True)[1][:8].int()
+    count = min(8, int((z[3] > -INF).sum()))
+    assert parents[0, :count].tolist() == [3] * count and bool((p[0, :count] == INF).all()) and torch.equal(nodes[0, :count], best[:count])
+    assert bool((p[1] <= 5).all()) and set(parents[1].tolist()) <= {2, 3}
+
+
+def test_log_probabilities_in_place(gs):
+    for groups, beams, n in ((3, 5, 40_000), (70, 8, 900)):
+        z, logp = some(groups * beams, n, "bf16", n)
+        want = check(gs, z, logp, beams, beams)
+        got = gs.gs_beam_select(z, logp, beams, beams, logp_out=logp.view(groups, beams))
+        assert all(torch.equal(x, y) for x, y in zip(got, want)) and torch.equal(logp.view(groups, beams), want[2])
+
+
+def test_two_graphs_of_one_workspace_and_another_stream(gs):
+    shapes = [(3, 5, 30_001, 6), (2, 8, 9000, 8)]
+    ws = torch.empty(max(gs.gs_beam_select_workspace_bytes(g, b, n, w, gs.GS_F32) for g, b, n, w in shapes), dtype=torch.uint8, device=DEV)
+    work, graphs = [], []
+    stream = torch.cuda.Stream()
+    for g, b, n, w in shapes:
+        z, logp = some(g * b, n, "f32", n)
+        state = torch.arange(g * b * 7, dtype=torch.int32, device=DEV).view(g * b, 7)
+        out = torch.zeros(g * w, 7, dtype=torch.int32, device=DEV)
+        with torch.cuda.stream(stream):
+            stream.wait_stream(torch.cuda.default_stream())
+            outs = gs.gs_beam_select(z, logp, b, w, ws=ws)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            gs.gs_beam_select(z, logp, b, w, parents_out=outs[0], nodes_out=outs[1], logp_out=outs[2], ws=ws)
+            gs.gs_beam_reorder([state], outs[0], b, outs=[out], nodes=outs[1], columns=[6])
+        work.append((z, logp, b, w, state, outs, out))
+        graphs.append(graph)
+    for turn in range(3):
+        for z, logp, *_ in work:
+            z.copy_(z.roll(turn + 1, 1))
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for z, logp, b, w, state, outs, out in work:
+            want = check(gs, z, logp, b, w)
+            assert all(torch.equal(x, y) for x, y in zip(outs, want))
+            rows = moved(state.cpu(), want[0].cpu(), b, out.cpu())
+            rows[:, 6] = want[1].reshape(-1).cpu()
+            assert torch.equal(out.cpu(), rows)
