@@ -254,19 +254,29 @@ __global__ __launch_bounds__(256, 4) void few_kernel(ScoresArgs a, int64_t turns
 }
 
 // ---- many centres: tiles of both through LDS ---------------------------------
-// Centres are copied first: rows of whole blocks, zeros behind, so that no load looks at an id; a centre that is no row has the scale
-// NaN.  A workgroup computes TN x TC scores in steps of 64 columns, half a block: the loads write rows' 64 bytes to LDS themselves,
-// three steps ahead.  Such a load puts lane l's 16 bytes at base + 16 l, so rows cannot be padded: the four pieces of a row are exchanged
-// among each other by a quarter of the row's number instead, so that 16 rows' pieces of a read lie in different banks (four rows
-// make 256 bytes, all 64 banks).  One barrier a step.
+// A workgroup computes 128 x TC scores in steps of 64 columns, half a block: the loads write rows' 64 bytes to LDS themselves, two
+// steps ahead, one barrier a step.  Such a load puts lane l's 16 bytes at base + 16 l, so rows cannot be padded: the four pieces of a
+// row are exchanged among each other by a quarter of the row's number instead, so that 16 rows' pieces of a read lie in different
+// banks (four rows make 256 bytes, all 64 banks).  Centres are copied first, in the order in which a tile reads them: its rows' 64
+// bytes of a step side by side, whole lines (loads of 64 bytes each of rows reach 31 to 39 bytes a clock and compute unit, whole
+// lines 54 to 60), zeros behind the rows, so that no load looks at an id; a centre that is no row has the scale NaN.
+// Two workgroups of four waves share a compute unit: where one waits at its barrier, begins or writes its scores, the other multiplies.
+// One of 256 x 256 with eight waves reads a third fewer bytes, but everything in it stops together: 8192 centres on 32,768 nodes of
+// 2048 columns (bf16 scores) 595 us, here 582; 4096 on 50,000 of 1024 columns 301, here 270; fp32 scores of the first 1040, here 995.
+// What bounds it: products and loads together.  2048 columns more cost the first case 490 us (2.24 PFLOP/s).  With one workgroup (495)
+// products alone took 333 of that, with their LDS reads 390, loads alone 279, and loads and products that wait for no data 501: a load's
+// way into LDS and the matrix instructions hinder each other.  Reads a step ahead, loads between products, halves of a workgroup in
+// opposite phases and centres straight into registers gave 479 to 611.  Beginnings and ends of tiles are the other 90 us.
 // The scores go out through LDS as well, as pieces of 16 bytes of whole rows.
 
 struct Copied {                                // of the centres, in the workspace
-  uint8_t* q;                                  // [padded centres][128 * blocks]
+  uint8_t* q;                                  // [tiles][steps][centres of a tile][64]
   uint8_t* scales;                             // [padded centres][scale pitch]: blocks up to a multiple of 4
   int32_t* top;                                // [padded centres]: largest power, as its byte
-  int32_t pitch, scale_pitch;
+  int32_t pitch, scale_pitch;                  // pitch: 128 * blocks
+  int32_t tile;                                // centres
 };
+constexpr int kStep = 64;                      // columns
 
 // A workgroup of 64 lanes a row.
 __global__ __launch_bounds__(64) void copy_centers_kernel(ScoresArgs a, Copied to) {
@@ -277,7 +287,7 @@ __global__ __launch_bounds__(64) void copy_centers_kernel(ScoresArgs a, Copied t
   for (int col = lane * 16; col < to.pitch; col += 64 * 16) {
     uint4 w = make_uint4(0, 0, 0, 0);
     if (there && col < a.pitch) w = *reinterpret_cast<const uint4*>(a.q_in + id * a.pitch + col);
-    *reinterpret_cast<uint4*>(to.q + i * to.pitch + col) = w;
+    *reinterpret_cast<uint4*>(to.q + i / to.tile * to.tile * to.pitch + (col / kStep * to.tile + i % to.tile) * kStep + col % kStep) = w;
   }
   int top = 0;
   if (lane < to.scale_pitch) {                 // 64 at most
@@ -297,17 +307,16 @@ __device__ __forceinline__ uint4 read_loose(const uint8_t* from) {
   const of_halves w = *reinterpret_cast<const of_halves*>(from);
   return make_uint4(w.x, w.y, w.z, w.w);
 }
-constexpr int kStep = 64;                      // columns
-constexpr int kStages = 4;                     // steps in LDS
+constexpr int kStages = 3;                     // steps in LDS
 
 template <typename O, int NA, int NC, int WA, int WC>
 __global__ __launch_bounds__(64 * WA * WC, 2) void tile_kernel(ScoresArgs a, Copied in, int64_t tiles_c, int64_t tiles_n) {
   typedef typename O::elem elem;
   constexpr int S = kStages, TN = 32 * NA * WA, TC = 32 * NC * WC, kWaves = WA * WC;
-  constexpr int kLoads = (TN + TC) / 16 / kWaves;                        // of 1 KB: sixteen rows
+  constexpr int kLoadsN = TN / 16 / kWaves, kLoadsC = TC / 16 / kWaves, kLoads = kLoadsN + kLoadsC;       // of 1 KB: sixteen rows
   constexpr int kPer = 16 / (int)sizeof(elem), kRowBytes = TN * (int)sizeof(elem) + 16, kRound = 32 * WC;   // of scores in LDS
   constexpr int kStageBytes = S * (TN + TC) * kStep, kBytes = kStageBytes > kRound * kRowBytes ? kStageBytes : kRound * kRowBytes;
-  static_assert((TN / 16) % kLoads == 0 && kLoads * 16 * kWaves == TN + TC, "a wave's loads are of one operand");
+  static_assert(kLoads * 16 * kWaves == TN + TC, "whole loads");
   __shared__ __attribute__((aligned(16))) uint8_t lds[kBytes];
   __shared__ __attribute__((aligned(16))) int32_t side_top[TN];
   __shared__ __attribute__((aligned(16))) float side_bias[TN];
@@ -315,30 +324,36 @@ __global__ __launch_bounds__(64 * WA * WC, 2) void tile_kernel(ScoresArgs a, Cop
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), at = lane & 31, half = lane >> 5;
   const int wa = wave % WA, wc = wave / WA;
 
-  // Consecutive workgroups go round the eight XCDs: each of them gets neighbouring tiles, eight of nodes at a time, so that what 32
-  // compute units read at once is in their L2.
+  // Consecutive workgroups go round the eight XCDs: each of them gets neighbouring tiles, 2048 nodes at a time, so that what 32 compute
+  // units read at once is in their L2 (1024 nodes: 4096 centres on 50,000 of 1024 columns 283 us instead of 270; 4096: 8192 on 32,768
+  // of 2048 columns 620 instead of 582).
   const int64_t tiles = tiles_c * tiles_n, per = (tiles + 7) / 8;
   const int64_t t = (int64_t)(blockIdx.x % 8) * per + blockIdx.x / 8;
   if (blockIdx.x / 8 >= per || t >= tiles) return;
-  const int64_t group = t / (8 * tiles_c), left = min((int64_t)8, tiles_n - 8 * group), in_group = t - group * 8 * tiles_c;
-  const int64_t c0 = in_group / left * TC, n0 = (8 * group + in_group % left) * TN;
+  constexpr int kGroup = 2048 / TN;
+  const int64_t group = t / (kGroup * tiles_c), left = min((int64_t)kGroup, tiles_n - kGroup * group), in_group = t - group * kGroup * tiles_c;
+  const int64_t c0 = in_group / left * TC, n0 = (kGroup * group + in_group % left) * TN;
   const int nodes = (int)min((int64_t)TN, a.num_nodes - n0);
 
-  const bool of_nodes = wave * kLoads < TN / 16;
-  const int first_row = wave * kLoads * 16 - (of_nodes ? 0 : TN), pitch = of_nodes ? a.pitch : in.pitch;
-  const __amdgpu_buffer_rsrc_t range = range_of(of_nodes ? a.q_out + n0 * a.pitch : in.q + c0 * in.pitch, (of_nodes ? nodes : TC) * pitch);
-  uint8_t* const to = (of_nodes ? lds : lds_c) + first_row * kStep;
-  const int to_next = (of_nodes ? TN : TC) * kStep;
-  const int piece = ((lane & 3) ^ (lane >> 4)) * 16, row_at = (first_row + (lane >> 2)) * pitch;
-  auto issue = [&](int step, int buf, int n) {
-    const int col = step * kStep + piece;
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(range, (__attribute__((address_space(3))) void*)(to + buf * to_next + n * 1024), 16,
-                                             col < pitch ? row_at + col + n * 16 * pitch : kOutside, 0, 0, 0);
+  const int row_n = wave * kLoadsN * 16, row_c = wave * kLoadsC * 16;
+  const __amdgpu_buffer_rsrc_t range_n = range_of(a.q_out + n0 * a.pitch, nodes * a.pitch), range_c = range_of(in.q + c0 * in.pitch, TC * in.pitch);
+  // as a number: where the compiler sees that loads and reads are of one array, it lets every read wait for all loads
+  const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds);
+  const int piece = ((lane & 3) ^ (lane >> 4)) * 16;
+  const int at_row = (row_n + (lane >> 2)) * a.pitch + piece, at_piece = (row_c + (lane >> 2)) * kStep + piece;
+  auto load = [&](const __amdgpu_buffer_rsrc_t& range, uint32_t place, int from) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(range, (__attribute__((address_space(3))) void*)(uintptr_t)(to + place), 16, from, 0, 0, 0);
+  };
+  auto issue = [&](int step, int buf) {
+#pragma unroll
+    for (int n = 0; n < kLoadsN; ++n)
+      load(range_n, (buf * TN + row_n + n * 16) * kStep, step * kStep + piece < a.pitch ? at_row + step * kStep + n * 16 * a.pitch : kOutside);
+#pragma unroll
+    for (int n = 0; n < kLoadsC; ++n)
+      load(range_c, (S * TN + buf * TC + row_c + n * 16) * kStep, step < 2 * a.blocks ? at_piece + (step * TC + n * 16) * kStep : kOutside);
   };
 #pragma unroll
-  for (int s = 0; s < S - 1; ++s)
-#pragma unroll
-    for (int n = 0; n < kLoads; ++n) issue(s, s, n);
+  for (int s = 0; s < S - 1; ++s) issue(s, s);
 
   // ---- scales: of a lane's rows, four blocks at a time
   const uint8_t *scales_c = in.scales + c0 * in.scale_pitch, *scales_n = a.scales_out + n0 * a.scale_pitch;
@@ -393,17 +408,17 @@ __global__ __launch_bounds__(64 * WA * WC, 2) void tile_kernel(ScoresArgs a, Cop
     const uint4 p = *reinterpret_cast<const uint4*>(base + place[0] + more), q = *reinterpret_cast<const uint4*>(base + place[1] + more);
     return int8v{(int)p.x, (int)p.y, (int)p.z, (int)p.w, (int)q.x, (int)q.y, (int)q.z, (int)q.w};
   };
+  int buf = 0;
   auto step = [&](int k) {
-    const int buf = k % S;
     wait_loads<(S - 2) * kLoads>();            // this step's rows; those of later ones may be under way
     meet();
-#pragma unroll
-    for (int n = 0; n < kLoads; ++n) issue(k + S - 1, (k + S - 1) % S, n);      // where the step before was read
+    issue(k + S - 1, buf == 0 ? S - 1 : buf - 1);      // where the step before was read
     int8v x[NA], y[NC];
 #pragma unroll
     for (int n = 0; n < NC; ++n) y[n] = pair(lds_c + buf * TC * kStep, at_c, n * 32 * kStep);
 #pragma unroll
     for (int m = 0; m < NA; ++m) x[m] = pair(lds + buf * TN * kStep, at_n, m * 32 * kStep);
+    buf = buf == S - 1 ? 0 : buf + 1;
     if (O::kExact) {
       float fx[NA], fy[NC];
 #pragma unroll
@@ -788,6 +803,7 @@ namespace gs {
 namespace {
 
 constexpr int kFew = 32;                       // centres at most that take no tiles
+constexpr int kNarrow = 128;                   // that take tiles of 128
 struct ScoresPlan {
   bool few;
   int64_t padded;
@@ -801,7 +817,7 @@ ScoresPlan plan_scores(void* ws, int64_t num_centers, int32_t dim) {
   if (p.few || dim <= 2 * kBlock) return p;
   p.padded = ceil_div(num_centers, 256) * 256;
   const int blocks = (int)ceil_div(dim, kBlock);
-  p.in.pitch = blocks * kBlock, p.in.scale_pitch = (blocks + 3) / 4 * 4;
+  p.in.pitch = blocks * kBlock, p.in.scale_pitch = (blocks + 3) / 4 * 4, p.in.tile = num_centers <= kNarrow ? 128 : 256;
   Carver carve(ws);
   p.in.q = carve.take<uint8_t>((size_t)p.padded * p.in.pitch);
   p.in.scales = carve.take<uint8_t>((size_t)p.padded * p.in.scale_pitch);
@@ -865,8 +881,8 @@ int32_t run_scores(const ScoresArgs& a, const ScoresPlan& p, hipStream_t s) {
   if (a.blocks <= 2) return run_strips<O>(a, s);
   copy_centers_kernel<<<dim3((unsigned)p.padded), 64, 0, s>>>(a, p.in);
   GS_LAUNCH_CHECK();
-  if (a.num_centers <= 128) return run_tiles<O, 2, 2, 2, 2>(a, p.in, s);
-  return run_tiles<O, 4, 2, 2, 4>(a, p.in, s);
+  if (a.num_centers <= kNarrow) return run_tiles<O, 2, 2, 2, 2>(a, p.in, s);
+  return run_tiles<O, 4, 2, 1, 4>(a, p.in, s);
 }
 
 }  // namespace
