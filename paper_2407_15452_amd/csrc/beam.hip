@@ -11,6 +11,17 @@
 // The width best without a sort: of the largest score of each lane, the width-th largest is a lower bound of what can be taken,
 // and little more than `width` scores reach it.  Those go to a list, where each one's place is the number of larger ones.  Where too
 // many reach it (equal scores), the best is taken out `width` times instead.
+//
+// Bound: the weights' arithmetic.  A score costs 26 vector instructions, 18 of them the fp64 weight (a sum in fp32 would be off by more
+// than neighbours of different walks are apart): 64 rows of 1,000,000 fp32 scores take 64 us, 4.0 TB/s, 49 of them instructions; reading
+// alone takes 42.  256 rows of 100,003 bf16 scores 35 us.  The join is a chain of small steps in one workgroup a group, 6 us for one
+// group of four walks on 10,000 nodes (the parts before it 6), 9 to 20 us for many lists.  Rows of up to 4096 scores take a wave each
+// where there are 256 rows and more: no barriers in between (4096 rows of 64 fp32 scores 25 us, with a workgroup a row 81; of 1000 scores
+// 18 and 72).
+//
+// gs_beam_reorder: memory.  64 groups of 8 walks with six rows of 32,768 fp32 values each: 131 us, 6.1 TB/s counted as every row read and
+// written once (parents repeat, and such rows come from the caches).  Sixteen bytes a lane, four of them in flight, one launch for all
+// states; in place a workgroup holds a stripe of all rows of a group in LDS between reading and writing.
 
 #include "weigh.h"
 
@@ -809,7 +820,8 @@ extern "C" int32_t gs_beam_select(const void* scores, int64_t groups, int32_t be
   if (dtype == GS_BF16) launch_parts<ScoreHalf<bf16_t>>(a, p, grid, s);
   if (dtype == GS_F16) launch_parts<ScoreHalf<f16_t>>(a, p, grid, s);
   GS_LAUNCH_CHECK();
-  if ((int64_t)beams * p.parts * width > 4096) join_kernel<1024><<<dim3((unsigned)groups), 1024, 0, s>>>(a);
+  // of many candidates a group's lists take a large workgroup less time (8 groups of 8 walks on 1,000,000 nodes, width 8: 85 -> 80 us)
+  if ((int64_t)beams * p.parts * width > 2048) join_kernel<1024><<<dim3((unsigned)groups), 1024, 0, s>>>(a);
   else join_kernel<256><<<dim3((unsigned)groups), 256, 0, s>>>(a);
   GS_LAUNCH_CHECK();
   return GS_OK;

