@@ -216,3 +216,31 @@ def test_tables_beyond_32_bits(gs, centers):
     assert int((got != 0).sum()) == 0
     far = gs.gs_scores_q8(t_out, small, rows.to(torch.int32))
     check(gs, small, small, torch.arange(6, dtype=torch.int32, device=DEV), got=far)
+
+
+@pytest.mark.parametrize("dtype", list(TORCH))
+@pytest.mark.parametrize("centers,nodes,dim", [(128, 4097, 260), (129, 6200, 384), (300, 5001, 300), (1025, 4100, 640), (513, 2176, 1100)])
+def test_tiles_over_groups_of_nodes(gs, centers, nodes, dim, dtype):
+    """Several groups of 2048 nodes, the last one ragged; masked nodes and centres that are no row among them."""
+    t_in, t_out = table(gs, 400, dim, 5), table(gs, nodes, dim, 6)
+    gen = torch.Generator().manual_seed(nodes)
+    ids = torch.randint(-1, 401, (centers,), generator=gen, dtype=torch.int32).to(DEV)
+    bias = torch.randn(nodes, generator=gen)
+    bias[::13] = -INF
+    check(gs, t_in, t_out, ids, bias=bias.to(DEV), scale=0.5, dtype=dtype)
+
+
+def test_on_two_streams_at_once(gs):
+    """Calls with workspaces of their own on two streams; each waits for its inputs alone."""
+    t_in, t_out = table(gs, 200, 700, 7), table(gs, 9000, 700, 8)
+    ids = [torch.randint(0, 200, (n,), generator=torch.Generator().manual_seed(n), dtype=torch.int32).to(DEV) for n in (200, 600)]
+    want = [gs.gs_scores_q8(t_in, t_out, i, dtype=torch.bfloat16) for i in ids]
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [None, None]
+    for turn in range(3):
+        for s in streams:
+            s.wait_stream(torch.cuda.current_stream())
+        for k in (0, 1):
+            with torch.cuda.stream(streams[k]):
+                got[k] = gs.gs_scores_q8(t_in, t_out, ids[k], dtype=torch.bfloat16)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
