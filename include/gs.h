@@ -598,7 +598,7 @@ int32_t gs_clip_grads(const gs_tensor* list, int32_t num_tensors, double max_nor
  *   rows.  bias, masked nodes and centres that
  *   are no row as for gs_scores; a scale NaN makes the scores of its row NaN.
  *   Same bits on every run.  Errors: GS_EINVAL, GS_EOVERFLOW for 2^21 centres and
- *   more, or more tiles of 128 x 128 scores than a launch takes (2^31).
+ *   more, or more tiles of scores (128 x 128 or larger) than a launch takes (2^31).
  * ------------------------------------------------------------------------ */
 enum { GS_Q8_MAX_DIM = 8192 };
 int32_t gs_q8_pitch(int32_t dim);
