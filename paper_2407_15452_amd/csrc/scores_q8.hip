@@ -4,8 +4,8 @@
 //
 // a, c: e4m3 values; e, f: the powers of two of their blocks of 128 columns.  Two kinds of products:
 //   fp32 scores: the values go through v_cvt_scalef32_pk_bf16_fp8 into the bf16 matrix instruction, whose products of them are exact
-//     and whose sums are fp32.  The conversion multiplies by powers of two as well: by a block's relative to its row's largest, so
-//     that nothing leaves bf16's range; the rows' largest ones multiply the sum.
+//     and whose sums are fp32.  The conversion multiplies by powers of two as well, by the block's own; those that bf16 has no room
+//     for are looked for, and multiply sums of the block alone.
 //   16-bit scores: v_mfma_scale_f32_32x32x64 on the bytes themselves, which multiplies by the powers of the blocks and runs at twice
 //     the rate.  Of eight neighbouring products it drops what lies 2^13 below the largest of them (measured, and so do the 8-bit
 //     instructions without scales): at most 7 * 2^-13 of the sum of the products' sizes, some 2^-16 of it for Gaussian rows; fp32
@@ -96,10 +96,15 @@ __device__ __forceinline__ int8v load32(__amdgpu_buffer_rsrc_t range, int row, i
   return int8v{(int)a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, (int)b.y, (int)b.z, (int)b.w};
 }
 
-// 2^(byte - top) for the conversion, which looks at the exponent alone; NaN stays
-__device__ __forceinline__ float relative(int byte, int top) {
-  return __uint_as_float((uint32_t)(byte == 255 ? 255 : max(byte - top + 127, 1)) << 23);
-}
+// 1 for the conversion, which looks at the exponent alone, or NaN
+__device__ __forceinline__ float plain_or_nan(int byte) { return __uint_as_float((uint32_t)(byte == 255 ? 255 : 127) << 23); }
+// With its power a block's values are multiples of 2^-9 times that, up to 448 times, and bf16 holds multiples of 2^-133 (conversion and
+// matrix instruction keep subnormal numbers) up to 2^128.  Nodes' are taken 8 times as large and centres' an eighth, so that blocks of
+// zeros, which have the least power, 2^-127, need no look at their values: exact for nodes' powers up to 2^116, and for centres' from 2^-121
+// to 2^122.  Beyond are blocks of values above 4e37 and centres' blocks that lie below 1e-34, but for zeros.
+constexpr int kLift = 3, kMostNode = 246 - kLift, kLeastCenter = 3 + kLift, kMostCenter = 246 + kLift;      // powers, as their bytes
+__device__ __forceinline__ float node_factor(int byte) { return __uint_as_float((uint32_t)(byte == 255 ? 255 : min(byte + kLift, 254)) << 23); }
+__device__ __forceinline__ float center_factor(int byte) { return __uint_as_float((uint32_t)(byte == 255 ? 255 : max(byte - kLift, 1)) << 23); }
 // eight values of two words
 __device__ __forceinline__ bf8 widen(int lo, int hi, float scale) {
   union {
@@ -223,8 +228,8 @@ __global__ __launch_bounds__(256, 4) void few_kernel(ScoresArgs a, int64_t turns
     if (O::kExact) {
       auto easy = [](int byte) { return byte == 255 || (unsigned)(byte - 10) <= 236u; };
       const bool by_values = __ballot(easy(now.node_power) && easy(now.center_power)) == ~0ull;
-      const float fx = by_values ? __uint_as_float((uint32_t)now.node_power << 23) : relative(now.node_power, now.node_power);
-      const float fy = by_values ? __uint_as_float((uint32_t)now.center_power << 23) : relative(now.center_power, now.center_power);
+      const float fx = by_values ? __uint_as_float((uint32_t)now.node_power << 23) : plain_or_nan(now.node_power);
+      const float fy = by_values ? __uint_as_float((uint32_t)now.center_power << 23) : plain_or_nan(now.center_power);
       acc16 sum = {};
       if (by_values) sum = acc;
 #pragma unroll
@@ -269,11 +274,14 @@ __global__ __launch_bounds__(256, 4) void few_kernel(ScoresArgs a, int64_t turns
 // way into LDS and the matrix instructions hinder each other.  Reads a step ahead, loads between products, halves of a workgroup in
 // opposite phases and centres straight into registers gave 479 to 611.  Beginnings and ends of tiles are the other 90 us.
 // The scores go out through LDS as well, as pieces of 16 bytes of whole rows.
+// fp32 scores: both sides' values go in with their powers, nodes' lifted.  Scores of rows with a block beyond what that is exact for
+// are computed once more at the end, block by block, which few tables need: 4096 centres on
+// 50,000 nodes of 1024 columns take 0.45 ms, with ten such nodes 0.61 and where all are 1.7.
 
 struct Copied {                                // of the centres, in the workspace
   uint8_t* q;                                  // [tiles][steps][centres of a tile][64]
   uint8_t* scales;                             // [padded centres][scale pitch]: blocks up to a multiple of 4
-  int32_t* top;                                // [padded centres]: largest power, as its byte
+  int32_t* beyond;                             // [padded centres]: whether a block's power is
   int32_t pitch, scale_pitch;                  // pitch: 128 * blocks
   int32_t tile;                                // centres
 };
@@ -285,20 +293,24 @@ __global__ __launch_bounds__(64) void copy_centers_kernel(ScoresArgs a, Copied t
   const int lane = threadIdx.x;
   const int64_t id = i < a.num_centers ? (int64_t)a.centers[i] : -1;
   const bool there = id >= 0 && id < a.num_in;
-  for (int col = lane * 16; col < to.pitch; col += 64 * 16) {
+  bool zeros = true;                           // block `lane`
+  for (int first = 0; first < to.pitch; first += 64 * 16) {
+    const int col = first + lane * 16;
     uint4 w = make_uint4(0, 0, 0, 0);
     if (there && col < a.pitch) w = *reinterpret_cast<const uint4*>(a.q_in + id * a.pitch + col);
-    *reinterpret_cast<uint4*>(to.q + i / to.tile * to.tile * to.pitch + (col / kStep * to.tile + i % to.tile) * kStep + col % kStep) = w;
+    if (col < to.pitch)
+      *reinterpret_cast<uint4*>(to.q + i / to.tile * to.tile * to.pitch + (col / kStep * to.tile + i % to.tile) * kStep + col % kStep) = w;
+    const uint64_t some = __ballot(((w.x | w.y | w.z | w.w) & 0x7f7f7f7fu) != 0);      // eight lanes a block
+    if (lane / 8 == first / (64 * 16)) zeros = (some >> (lane % 8 * 8) & 255u) == 0;
   }
-  int top = 0;
+  bool beyond = false;
   if (lane < to.scale_pitch) {                 // 64 at most
     const int byte = !there ? 255 : lane < a.blocks ? (int)a.scales_in[id * a.scale_pitch + lane] : 0;
     to.scales[i * to.scale_pitch + lane] = (uint8_t)byte;
-    if (byte != 255) top = byte;
+    beyond = !zeros && byte != 255 && (byte < kLeastCenter || byte > kMostCenter);
   }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) top = max(top, __shfl_xor(top, d, 64));
-  if (lane == 0) to.top[i] = top;
+  const bool any = __ballot(beyond) != 0;
+  if (lane == 0) to.beyond[i] = any;
 }
 
 __device__ __forceinline__ void put_piece(float* to, const uint4& w) { *reinterpret_cast<of_words*>(to) = (of_words){w.x, w.y, w.z, w.w}; }
@@ -319,7 +331,8 @@ __global__ __launch_bounds__(64 * WA * WC, 2) void tile_kernel(ScoresArgs a, Cop
   constexpr int kStageBytes = S * (TN + TC) * kStep, kBytes = kStageBytes > kRound * kRowBytes ? kStageBytes : kRound * kRowBytes;
   static_assert(kLoads * 16 * kWaves == TN + TC, "whole loads");
   __shared__ __attribute__((aligned(16))) uint8_t lds[kBytes];
-  __shared__ __attribute__((aligned(16))) int32_t side_top[TN];
+  __shared__ uint8_t beyond_n[TN];             // whether a block's power is
+  __shared__ bool any_beyond[kWaves];
   __shared__ __attribute__((aligned(16))) float side_bias[TN];
   uint8_t* const lds_c = lds + S * TN * kStep;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), at = lane & 31, half = lane >> 5;
@@ -367,23 +380,26 @@ __global__ __launch_bounds__(64 * WA * WC, 2) void tile_kernel(ScoresArgs a, Cop
     if (a.scale_pitch >= 4) return *reinterpret_cast<const uint32_t*>(p + block);
     return (uint32_t)p[0] | (a.scale_pitch == 2 ? (uint32_t)p[1] << 8 : 0u);
   };
-  int top_n[NA], top_c[NC];
   if (O::kExact) {
+    bool any = false;
 #pragma unroll
-    for (int n = 0; n < NC; ++n) top_c[n] = in.top[c0 + (wc * NC + n) * 32 + at];
+    for (int n = 0; n < NC; ++n) any |= in.beyond[c0 + (wc * NC + n) * 32 + at] != 0;
 #pragma unroll
     for (int m = 0; m < NA; ++m) {
-      top_n[m] = 0;
+      int top = 0;
       for (int b = 0; b < a.blocks; b += 4) {
         const uint32_t w = four(m, b);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int byte = (int)((w >> (8 * k)) & 255u);
-          top_n[m] = max(top_n[m], byte == 255 ? 0 : byte);
+          top = max(top, byte == 255 ? 0 : byte);
         }
       }
-      if (wc == 0 && half == 0) side_top[(wa * NA + m) * 32 + at] = top_n[m];
+      any |= top > kMostNode;
+      if (wc == 0 && half == 0) beyond_n[(wa * NA + m) * 32 + at] = top > kMostNode;
     }
+    any = __ballot(any) != 0;
+    if (lane == 0) any_beyond[wave] = any;
   }
   if (a.bias)
     for (int i = tid; i < nodes; i += 64 * kWaves) side_bias[i] = a.bias[n0 + i];
@@ -423,9 +439,9 @@ __global__ __launch_bounds__(64 * WA * WC, 2) void tile_kernel(ScoresArgs a, Cop
     if (O::kExact) {
       float fx[NA], fy[NC];
 #pragma unroll
-      for (int m = 0; m < NA; ++m) fx[m] = relative((int)(sn[m] & 255u), top_n[m]);
+      for (int m = 0; m < NA; ++m) fx[m] = node_factor((int)(sn[m] & 255u));
 #pragma unroll
-      for (int n = 0; n < NC; ++n) fy[n] = relative((int)(sc[n] & 255u), top_c[n]);
+      for (int n = 0; n < NC; ++n) fy[n] = center_factor((int)(sc[n] & 255u));
 #pragma unroll
       for (int w = 0; w < 8; w += 2) {
         bf8 u[NA], v[NC];
@@ -475,14 +491,10 @@ __global__ __launch_bounds__(64 * WA * WC, 2) void tile_kernel(ScoresArgs a, Cop
       for (int g = 0; g < 4; ++g) {
         const int j = (wa * NA + m) * 32 + 8 * g + 4 * half;
         float v[4], bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        int top[4] = {0, 0, 0, 0};
-        if (O::kExact) __builtin_memcpy(top, &side_top[j], 16);
         if (a.bias) __builtin_memcpy(bias, &side_bias[j], 16);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          float z = acc[m][n][4 * g + k];
-          if (O::kExact) z = ldexpf(z, top[k] + top_c[n] - 254);
-          z = a.scale * z + bias[k];
+          const float z = a.scale * acc[m][n][4 * g + k] + bias[k];
           v[k] = bias[k] == -INFINITY ? -INFINITY : z;
         }
         O::put4(reinterpret_cast<elem*>(lds + (wc * 32 + at) * kRowBytes) + j, v);
@@ -502,6 +514,43 @@ __global__ __launch_bounds__(64 * WA * WC, 2) void tile_kernel(ScoresArgs a, Cop
         const int r = p / TN, j = p - r * TN;
         const int64_t i = c0 + (r / 32 * NC + n) * 32 + r % 32;
         if (i < a.num_centers && j < nodes) out[i * a.num_nodes + n0 + j] = reinterpret_cast<const elem*>(lds + r * kRowBytes)[j];
+      }
+    }
+  }
+  if constexpr (O::kExact) {
+    bool any = false;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) any |= any_beyond[w];
+    if (!any) return;
+    wait_loads<0>();                           // the stores of all waves: some of them are replaced
+    meet();
+    for (int sub = wave; sub < TN / 32 * (TC / 32); sub += kWaves) {         // 32 x 32 scores
+      const int j0 = sub % (TN / 32) * 32, r = sub / (TN / 32) * 32 + at;
+      const int64_t i = c0 + r;
+      const bool beyond_c = in.beyond[i] != 0;
+      if (__ballot(beyond_c || beyond_n[j0 + at]) == 0) continue;
+      const uint8_t* row_c = in.q + c0 * in.pitch + r * kStep;
+      acc16 z = {};
+      for (int block = 0; block < a.blocks; ++block) {
+        const int power = scales_n[min(j0 + at, nodes - 1) * a.scale_pitch + block], power_c = in.scales[i * in.scale_pitch + block];
+        acc16 sum = {};
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const int col = block * kBlock + half * kStep + s * 32;
+          const int8v x = load32(range_n, (j0 + at) * a.pitch, col, a.pitch), y = load32(row_c + (2 * block + half) * TC * kStep, s * 32, kStep);
+#pragma unroll
+          for (int w = 0; w < 8; w += 2)
+            sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(x[w], x[w + 1], plain_or_nan(power)), widen(y[w], y[w + 1], plain_or_nan(power_c)), sum, 0, 0, 0);
+        }
+#pragma unroll
+        for (int t = 0; t < 16; ++t) z[t] += ldexpf(sum[t], power_c - 254 + __shfl(power, 8 * (t / 4) + 4 * half + t % 4, 64));
+      }
+#pragma unroll
+      for (int t = 0; t < 16; ++t) {
+        const int j = j0 + 8 * (t / 4) + 4 * half + t % 4;
+        if (i >= a.num_centers || j >= nodes || !(beyond_c || beyond_n[j])) continue;
+        const float bias = a.bias ? side_bias[j] : 0.0f;
+        out[i * a.num_nodes + n0 + j] = bias == -INFINITY ? -INFINITY : a.scale * z[t] + bias;
       }
     }
   }
@@ -581,37 +630,40 @@ __global__ __launch_bounds__(320, 2) void strip_kernel(ScoresArgs a, int64_t gro
   const int64_t c0 = (group * S::kWaves + wave) * 32 * KC;
   int8v kept[O::kExact ? 1 : KC][BL * 2];
   bf8 wide[O::kExact ? KC : 1][BL * 8];
-  int top_c[KC], scale_c[KC][BL];
+  int scale_c[KC][BL];
+  bool zeros[KC][BL];                          // what the lane holds of a block
 #pragma unroll
   for (int n = 0; n < KC; ++n) {
     const int64_t i = c0 + n * 32 + at, id = i < a.num_centers ? (int64_t)a.centers[i] : -1;
     const bool there = id >= 0 && id < a.num_in;
     const uint8_t *h = a.q_in + (there ? id : 0) * a.pitch, *e = a.scales_in + (there ? id : 0) * BL;
-    top_c[n] = 0;
 #pragma unroll
-    for (int b = 0; b < BL; ++b) {
-      scale_c[n][b] = there ? e[b] : 255;
-      top_c[n] = max(top_c[n], scale_c[n][b] == 255 ? 0 : scale_c[n][b]);
-    }
+    for (int b = 0; b < BL; ++b) scale_c[n][b] = there ? e[b] : 255, zeros[n][b] = there;
 #pragma unroll
     for (int k = 0; k < BL * 2; ++k) {
       const int8v x = load32(h, (k >> 1) * kBlock + (k & 1) * 64 + half * 32, a.pitch);
       if (O::kExact) {
 #pragma unroll
-        for (int w = 0; w < 8; w += 2) wide[n][k * 4 + w / 2] = widen(x[w], x[w + 1], relative(scale_c[n][k >> 1], top_c[n]));
+        for (int w = 0; w < 8; ++w) zeros[n][k >> 1] = zeros[n][k >> 1] && (x[w] & 0x7f7f7f7f) == 0;
+#pragma unroll
+        for (int w = 0; w < 8; w += 2) wide[n][k * 4 + w / 2] = widen(x[w], x[w + 1], plain_or_nan(scale_c[n][k >> 1]));
       } else {
         kept[n][k] = x;
       }
     }
   }
 
-  float factor_c[KC];
+  float factor_c[KC][BL];
   bool near_c = true;
 #pragma unroll
-  for (int n = 0; n < KC; ++n) {
-    factor_c[n] = __uint_as_float((uint32_t)top_c[n] << 23) * a.scale;
-    near_c = near_c && top_c[n] - 27u <= 173u && factor_c[n] >= 0x1p-126f && factor_c[n] <= 0x1p126f;
-  }
+  for (int n = 0; n < KC; ++n)
+#pragma unroll
+    for (int b = 0; b < BL; ++b) {
+      factor_c[n][b] = center_factor(scale_c[n][b]) * a.scale;
+      const bool fits = scale_c[n][b] - 27u <= 173u && factor_c[n][b] >= 0x1p-126f && factor_c[n][b] <= 0x1p126f;
+      if (!fits) factor_c[n][b] = 0.0f;        // of zeros, where it is used
+      near_c = near_c && (fits || zeros[n][b]);
+    }
   near_c = __ballot(near_c) == ~0ull;
   uint8_t* const mine = turn[wave];
   const int rows = (int)min((int64_t)32 * KC, a.num_centers - c0);      // may be none, or fewer
@@ -628,21 +680,32 @@ __global__ __launch_bounds__(320, 2) void strip_kernel(ScoresArgs a, int64_t gro
     const uint8_t* side = slot + S::kRows;
     const int64_t n0 = t * S::kNodes;
     const int nodes = (int)min((int64_t)S::kNodes, a.num_nodes - n0);
-    acc16 acc[2][KC];
-    int byte[2][BL], top[2];
+    // fp32 scores: a sum for each block, times the centre's power, so that no block's size matters to another's.  The node's power goes in
+    // with its values, which is exact and leaves sums below 2^121, but for blocks of values above 4e30 and of NaN; and the centre's is a
+    // factor, but for blocks of NaN, and those below 3e-28 or above 4e24 that are no zeros.  Otherwise both multiply the sums of the
+    // plain values.
+    constexpr int kSums = O::kExact ? BL : 1;
+    acc16 acc[kSums][2][KC];
+    int byte[2][BL];
     bool near = true;
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
 #pragma unroll
-      for (int n = 0; n < KC; ++n) acc[m][n] = acc16{};
-      top[m] = 0;
+      for (int b = 0; b < kSums; ++b)
+#pragma unroll
+        for (int n = 0; n < KC; ++n) acc[b][m][n] = acc16{};
 #pragma unroll
       for (int b = 0; b < BL; ++b) {
         byte[m][b] = side[(m * 32 + at) * BL + b];
-        top[m] = max(top[m], byte[m][b]);
+        near = near && byte[m][b] <= 220;
       }
-      near = near && top[m] - 27u <= 173u;
     }
+    const bool factors = !O::kExact || (__ballot(near) == ~0ull && near_c);
+    float factor_n[2][BL];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int b = 0; b < BL; ++b) factor_n[m][b] = factors ? node_factor(byte[m][b]) : plain_or_nan(byte[m][b]);
 #pragma unroll
     for (int k = 0; k < BL * 2; ++k) {
       int8v x[2];
@@ -657,21 +720,20 @@ __global__ __launch_bounds__(320, 2) void strip_kernel(ScoresArgs a, int64_t gro
         for (int w = 0; w < 8; w += 2)
 #pragma unroll
           for (int m = 0; m < 2; ++m) {
-            const bf8 u = widen(x[m][w], x[m][w + 1], relative(byte[m][k >> 1], top[m]));
+            const bf8 u = widen(x[m][w], x[m][w + 1], factor_n[m][k >> 1]);
 #pragma unroll
-            for (int n = 0; n < KC; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u, wide[n][k * 4 + w / 2], acc[m][n], 0, 0, 0);
+            for (int n = 0; n < KC; ++n)
+              acc[O::kExact ? k >> 1 : 0][m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u, wide[n][k * 4 + w / 2], acc[O::kExact ? k >> 1 : 0][m][n], 0, 0, 0);
           }
       } else {
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
           for (int n = 0; n < KC; ++n)
-            acc[m][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x[m], kept[n][k], acc[m][n], 0, 0, 0, byte[m][k >> 1], 0, scale_c[n][k >> 1]);
+            acc[0][m][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x[m], kept[n][k], acc[0][m][n], 0, 0, 0, byte[m][k >> 1], 0, scale_c[n][k >> 1]);
       }
     }
-    // Register 4 g + k of a block is node 8 g + 4 half + k, a lane's centre is ... + at.  The powers are factors where no product leaves
-    // the normal numbers (the sums lie within 2^-18 and 2^27), which is always but for rows of 1e-30 or 1e21, and rows of NaN.
-    const bool factors = !O::kExact || (__ballot(near) == ~0ull && near_c);
+    // Register 4 g + k of a block is node 8 g + 4 half + k, a lane's centre is ... + at.
     auto finish = [&](auto by_factors, auto with_bias) {
 #pragma unroll
       for (int m = 0; m < 2; ++m)
@@ -679,29 +741,34 @@ __global__ __launch_bounds__(320, 2) void strip_kernel(ScoresArgs a, int64_t gro
         for (int g = 0; g < 4; ++g) {
           const int j = m * 32 + 8 * g + 4 * half;
           float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-          uint32_t power[4] = {0, 0, 0, 0};
+          uint32_t power[4][BL];
           if constexpr (decltype(with_bias)::value) __builtin_memcpy(bias, side + 256 + 4 * j, 16);
-          if constexpr (O::kExact) {
+          if constexpr (O::kExact && !decltype(by_factors)::value) {
             uint32_t w[BL];
             __builtin_memcpy(w, side + j * BL, 4 * BL);
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              power[k] = BL == 1 ? (w[0] >> (8 * k)) & 255u : max((w[k * BL / 4] >> (8 * (k * BL % 4))) & 255u, (w[k * BL / 4] >> (8 * (k * BL % 4 + 1))) & 255u);
+#pragma unroll
+              for (int b = 0; b < BL; ++b) power[k][b] = (w[(k * BL + b) / 4] >> (8 * ((k * BL + b) % 4))) & 255u;
           }
 #pragma unroll
           for (int n = 0; n < KC; ++n)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              float z = acc[m][n][4 * g + k];
+              float z = 0.0f;
               if constexpr (!O::kExact) {
-                z = fmaf(z, a.scale, bias[k]);
+                z = fmaf(acc[0][m][n][4 * g + k], a.scale, bias[k]);
               } else if constexpr (decltype(by_factors)::value) {
-                z = fmaf(z * __uint_as_float(power[k] << 23), factor_c[n], bias[k]);
+                z = bias[k];
+#pragma unroll
+                for (int b = 0; b < BL; ++b) z = fmaf(acc[b][m][n][4 * g + k], factor_c[n][b], z);
               } else {
-                z = fmaf(ldexpf(z, (int)power[k] + top_c[n] - 254), a.scale, bias[k]);
+#pragma unroll
+                for (int b = 0; b < BL; ++b) z += ldexpf(acc[b][m][n][4 * g + k], (int)power[k][b] + scale_c[n][b] - 254);
+                z = fmaf(z, a.scale, bias[k]);
               }
               if constexpr (decltype(with_bias)::value) z = bias[k] == -INFINITY ? -INFINITY : z;
-              acc[m][n][4 * g + k] = z;
+              acc[0][m][n][4 * g + k] = z;
             }
         }
     };
@@ -723,7 +790,7 @@ __global__ __launch_bounds__(320, 2) void strip_kernel(ScoresArgs a, int64_t gro
           for (int m = 0; m < 2; ++m)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-              const float v[4] = {acc[m][n][4 * g], acc[m][n][4 * g + 1], acc[m][n][4 * g + 2], acc[m][n][4 * g + 3]};
+              const float v[4] = {acc[0][m][n][4 * g], acc[0][m][n][4 * g + 1], acc[0][m][n][4 * g + 2], acc[0][m][n][4 * g + 3]};
               O::put4(to + m * 32 + 8 * g + 4 * half, v);
             }
         }
@@ -823,7 +890,7 @@ ScoresPlan plan_scores(void* ws, int64_t num_centers, int32_t dim) {
   Carver carve(ws);
   p.in.q = carve.take<uint8_t>((size_t)p.padded * p.in.pitch);
   p.in.scales = carve.take<uint8_t>((size_t)p.padded * p.in.scale_pitch);
-  p.in.top = carve.take<int32_t>((size_t)p.padded);
+  p.in.beyond = carve.take<int32_t>((size_t)p.padded);
   p.bytes = carve.used;
   return p;
 }
