@@ -677,6 +677,7 @@ namespace {
 
 constexpr int kCopyThreads = 256;
 constexpr int kStates = 64;                    // of one launch
+constexpr int64_t kMostBlocks = (((int64_t)1 << 32) - 1) / kCopyThreads;       // of one launch: fewer than 2^32 lanes
 constexpr int kAhead = 4;                      // pieces of a lane in flight
 constexpr int kStripe = 4096;                  // pieces of a group that a workgroup holds, in place
 
@@ -686,7 +687,8 @@ struct ReorderArgs {
     char* out;
     int64_t row_bytes, append_at;
     int32_t piece;                             // bytes: 16, 4 or 1
-    int32_t first;                             // workgroup
+    int32_t first;                             // workgroup of the launch
+    int64_t before;                            // workgroups of the state in earlier launches
   };
   State state[kStates];
   int32_t num_states, beams, width;
@@ -766,7 +768,7 @@ __global__ __launch_bounds__(kCopyThreads) void reorder_kernel(ReorderArgs a) {
   int s = 0;
   while (s + 1 < a.num_states && (int)blockIdx.x >= a.state[s + 1].first) ++s;
   const ReorderArgs::State& st = a.state[s];
-  const int64_t at = (int64_t)blockIdx.x - st.first;
+  const int64_t at = (int64_t)blockIdx.x - st.first + st.before;
   if (IN_PLACE) {
     if (st.piece == 16) move_rows<uint4>(a, st, at, lds);
     else if (st.piece == 4) move_rows<uint32_t>(a, st, at, lds);
@@ -876,14 +878,17 @@ extern "C" int32_t gs_beam_reorder(const gs_state* list, int32_t num_states, int
       int piece = 1;
       for (int size : {4, 16})
         if (aligned(x.data, size) && aligned(out, size) && x.row_bytes % size == 0) piece = size;
-      const int64_t pieces = x.row_bytes / piece, more = in_place ? move_blocks(pieces, groups, beams) : copy_blocks(pieces, rows_out);
-      if (more > (int64_t)INT32_MAX) return GS_EOVERFLOW;
-      if (a.num_states == kStates || blocks + more > (int64_t)INT32_MAX) {
-        const int32_t rc = launch();
-        if (rc != GS_OK) return rc;
+      const int64_t pieces = x.row_bytes / piece, all = in_place ? move_blocks(pieces, groups, beams) : copy_blocks(pieces, rows_out);
+      for (int64_t done = 0; done < all;) {    // what a launch has no room for goes to the next: workgroups share nothing
+        if (a.num_states == kStates || blocks == kMostBlocks) {
+          const int32_t rc = launch();
+          if (rc != GS_OK) return rc;
+        }
+        const int64_t now = std::min(all - done, kMostBlocks - blocks);
+        a.state[a.num_states++] =
+            ReorderArgs::State{static_cast<const char*>(x.data), static_cast<char*>(out), x.row_bytes, x.append_at, piece, (int32_t)blocks, done};
+        blocks += now, done += now;
       }
-      a.state[a.num_states++] = ReorderArgs::State{static_cast<const char*>(x.data), static_cast<char*>(out), x.row_bytes, x.append_at, piece, (int32_t)blocks};
-      blocks += more;
     }
     const int32_t rc = launch();
     if (rc != GS_OK) return rc;
