@@ -36,7 +36,7 @@ def search(t_in, t_out, w_in, starts, goals, beams, length, scale=1.0):
         ended = (new < 0) | is_goal[new]
         rows = gs.gs_get_rows(w_in, nodes.reshape(-1).clamp(min=0))
         sums += torch.where((new >= 0)[:, None], rows, 0.0)
-    return walks.view(groups, beams, length), logp, sums.view(groups, beams, -1)
+    return walks.view(groups, beams, length), logp, sums.view(groups, beams, w_in.shape[1])
 
 
 def main(beams=8, num_starts=4, length=12):

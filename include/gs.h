@@ -639,7 +639,7 @@ int32_t gs_scores_q8(const void* q_in, const void* scales_in, int64_t num_in, co
  *   a multiple of 4, as row_bytes and both addresses are then.  -1: nothing is.
  *   data [groups * beams][row_bytes], out [groups * width][row_bytes]; no state may overlap
  *   another's out, nor its own out its data otherwise, nor any out parents or nodes.  beams, width at most 256,
- *   groups * max(beams, width) < 2^22 (GS_EOVERFLOW), row_bytes >= 0 below 2^40.
+ *   groups * max(beams, width) < 2^22 (GS_EOVERFLOW), row_bytes >= 0 below 2^40.  With groups == 0 no address is looked at.
  * ------------------------------------------------------------------------ */
 size_t gs_beam_select_workspace_bytes(int64_t groups, int32_t beams, int64_t n, int32_t width, int32_t dtype);
 int32_t gs_beam_select(const void* scores, int64_t groups, int32_t beams, int64_t n, int32_t dtype, const float* logp,

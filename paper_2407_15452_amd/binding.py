@@ -8,6 +8,7 @@ library is missing, or a tensor is not on the GPU, the call raises.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 
 import torch
@@ -865,7 +866,7 @@ def gs_beam_reorder(states, parents, beams: int, outs=None, nodes=None, columns=
             raise ValueError("an output must have its state's type and rows")
         if out is None and beams != width:
             raise ValueError("in place there are as many walks as before: pass outs")
-        row_bytes = x.numel() // x.shape[0] * x.element_size() if groups else 0
+        row_bytes = math.prod(x.shape[1:]) * x.element_size()
         if column is not None and (x.dim() != 2 or x.dtype != torch.int32 or not 0 <= column < x.shape[1] or nodes is None):
             raise ValueError("nodes are written to a column of an int32 state [rows, columns]")
         array[i] = StateStruct(data, _at(out, None, "output"), row_bytes, -1 if column is None else 4 * column)

@@ -842,9 +842,10 @@ extern "C" int32_t gs_beam_reorder(const gs_state* list, int32_t num_states, int
   for (int i = 0; i < num_states; ++i) {
     const gs_state& x = list[i];
     const bool in_place = !x.out || x.out == x.data;
-    if (x.row_bytes < 0 || x.row_bytes >= ((int64_t)1 << 40) || (in_place && beams != width && x.row_bytes > 0)) return GS_EINVAL;
+    if (x.row_bytes < 0 || x.row_bytes >= ((int64_t)1 << 40) || (in_place && beams != width && x.row_bytes > 0 && groups > 0))
+      return GS_EINVAL;
     if (x.row_bytes > 0 && groups > 0 && !x.data) return GS_EINVAL;
-    if (x.append_at < -1 || (x.append_at >= 0 && (x.append_at % 4 != 0 || x.append_at + 4 > x.row_bytes || x.row_bytes % 4 != 0 || !nodes ||
+    if (x.append_at < -1 || (x.append_at >= 0 && (x.append_at % 4 != 0 || x.append_at + 4 > x.row_bytes || x.row_bytes % 4 != 0 || (groups > 0 && !nodes) ||
                                                   !aligned(x.data, 4) || !aligned(x.out, 4))))
       return GS_EINVAL;
   }
