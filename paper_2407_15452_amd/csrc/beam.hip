@@ -417,7 +417,6 @@ struct JoinShared {
   double log_sum[kMostWidth];                  // log sum exp(s - top)
   uint8_t state[kMostWidth];                   // 0: no walk, 1: one, 2: one that has ended
   uint64_t lane_top[THREADS];
-  uint64_t most;
   uint32_t bins[kBins];
   uint32_t listed;
   int cut;
@@ -426,10 +425,12 @@ struct JoinShared {
   Place wave_best[2][THREADS / 64];
 };
 
-// A workgroup a group: the parts' sums, then the first of all lists.  Of many candidates, first those above the width-th largest of the
-// lists' heads, then those from the step up, of a thousand equal ones between that and the largest, where the width-th lies.
+// A workgroup a group, of 256 lanes for up to kJoinList candidates and of 1024 beyond: the parts' sums, then the first of all lists.  Of
+// many candidates, first those above the width-th largest of the lists' heads, then those from the step up, of a thousand equal ones
+// between that and the largest, where the width-th lies.
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void join_kernel(SelectArgs a) {
+  constexpr bool kMany = THREADS > 256;        // more than kJoinList candidates
   __shared__ JoinShared<THREADS> sh;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t group = blockIdx.x, first_row = group * a.beams;
@@ -476,7 +477,7 @@ __global__ __launch_bounds__(THREADS) void join_kernel(SelectArgs a) {
   // 1,000,000 nodes, bf16 scores, width 32: 120 -> 94 us; one of 32 walks on 100,000, width 64: 87 -> 46; from 4 candidates a lane on
   // instead of 8, 8 groups of 8 walks on 100,000 nodes, width 64: 49 -> 77, where most of a list is visited)
   auto for_all = [&](uint64_t least, auto visit) {
-    if (candidates <= 8 * THREADS) {
+    if (!kMany || candidates <= 8 * THREADS) {
       const int per_row = a.parts * a.width;
 #pragma unroll 4
       for (int c = tid; c < (int)candidates; c += THREADS) {
@@ -484,7 +485,7 @@ __global__ __launch_bounds__(THREADS) void join_kernel(SelectArgs a) {
         const Place place = place_of_key(b, keys[c], c == b * per_row);
         if (place.p >= least) visit(place);
       }
-    } else {
+    } else if constexpr (kMany) {
       for (int64_t l = tid; l < lists; l += THREADS) {
         const int b = (int)(l / a.parts), part = (int)(l - (int64_t)b * a.parts);
         for (int t = 0; t < a.width; ++t) {
@@ -499,7 +500,7 @@ __global__ __launch_bounds__(THREADS) void join_kernel(SelectArgs a) {
     const uint32_t to = atomicAdd(&sh.listed, 1u);
     if (to < (uint32_t)kJoinList) sh.p[to] = c.p, sh.in_row[to] = c.in_row, sh.row[to] = c.row;
   };
-  if (candidates <= kCounted) {
+  if (!kMany && candidates <= kCounted) {
     for_all(1, take);
   } else {
     uint64_t own = 0;
@@ -565,7 +566,7 @@ __global__ __launch_bounds__(THREADS) void join_kernel(SelectArgs a) {
     for (int c = listed + tid; c < a.width; c += THREADS) write(c, Place{0, 0, 0});
     return;
   }
-  if (listed <= kJoinList) {
+  if (!kMany || listed <= kJoinList) {
     const int n = power_of_two(listed);
     for (int c = listed + tid; c < n; c += THREADS) sh.p[c] = 0, sh.in_row[c] = 0, sh.row[c] = 0;
     __syncthreads();
@@ -578,37 +579,39 @@ __global__ __launch_bounds__(THREADS) void join_kernel(SelectArgs a) {
     for (int c = tid; c < a.width; c += THREADS) write(c, c < listed ? at(c) : Place{0, 0, 0});
     return;
   }
-  // The best is taken out `width` times; a lane looks again through its own lists only where it was its own.
-  Place last{~0ull, ~0ull, 0}, best = last;
-  for (int taken = 0; taken < a.width; ++taken) {
-    if (!last.before(best)) {
-      best = Place{0, 0, 0};
-      for (int64_t l = tid; l < lists; l += THREADS) {
-        const int b = (int)(l / a.parts), part = (int)(l - (int64_t)b * a.parts);
-        for (int t = 0; t < a.width; ++t) {
-          const Place c = place_at(b, part, t);
-          if (c.p == 0) break;
-          if (!last.before(c)) continue;
-          if (c.before(best)) best = c;
-          break;
+  if constexpr (kMany) {
+    // The best is taken out `width` times; a lane looks again through its own lists only where it was its own.
+    Place last{~0ull, ~0ull, 0}, best = last;
+    for (int taken = 0; taken < a.width; ++taken) {
+      if (!last.before(best)) {
+        best = Place{0, 0, 0};
+        for (int64_t l = tid; l < lists; l += THREADS) {
+          const int b = (int)(l / a.parts), part = (int)(l - (int64_t)b * a.parts);
+          for (int t = 0; t < a.width; ++t) {
+            const Place c = place_at(b, part, t);
+            if (c.p == 0) break;
+            if (!last.before(c)) continue;
+            if (c.before(best)) best = c;
+            break;
+          }
         }
       }
-    }
-    Place most = best;
+      Place most = best;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      Place o;
-      o.p = (uint64_t)__shfl_xor((unsigned long long)most.p, d, 64);
-      o.in_row = (uint64_t)__shfl_xor((unsigned long long)most.in_row, d, 64);
-      o.row = (uint32_t)__shfl_xor((int)most.row, d, 64);
-      if (o.before(most)) most = o;
+      for (int d = 1; d < 64; d <<= 1) {
+        Place o;
+        o.p = (uint64_t)__shfl_xor((unsigned long long)most.p, d, 64);
+        o.in_row = (uint64_t)__shfl_xor((unsigned long long)most.in_row, d, 64);
+        o.row = (uint32_t)__shfl_xor((int)most.row, d, 64);
+        if (o.before(most)) most = o;
+      }
+      if (lane == 0) sh.wave_best[taken & 1][wave] = most;
+      __syncthreads();
+      last = sh.wave_best[taken & 1][0];
+      for (int w = 1; w < THREADS / 64; ++w)
+        if (sh.wave_best[taken & 1][w].before(last)) last = sh.wave_best[taken & 1][w];
+      if (tid == 0) write(taken, last);
     }
-    if (lane == 0) sh.wave_best[taken & 1][wave] = most;
-    __syncthreads();
-    last = sh.wave_best[taken & 1][0];
-    for (int w = 1; w < THREADS / 64; ++w)
-      if (sh.wave_best[taken & 1][w].before(last)) last = sh.wave_best[taken & 1][w];
-    if (tid == 0) write(taken, last);
   }
 }
 
@@ -825,7 +828,7 @@ extern "C" int32_t gs_beam_select(const void* scores, int64_t groups, int32_t be
   if (dtype == GS_F16) launch_parts<ScoreHalf<f16_t>>(a, p, grid, s);
   GS_LAUNCH_CHECK();
   // of many candidates a group's lists take a large workgroup less time (8 groups of 8 walks on 1,000,000 nodes, width 8: 85 -> 80 us)
-  if ((int64_t)beams * p.parts * width > 2048) join_kernel<1024><<<dim3((unsigned)groups), 1024, 0, s>>>(a);
+  if ((int64_t)beams * p.parts * width > kJoinList) join_kernel<1024><<<dim3((unsigned)groups), 1024, 0, s>>>(a);
   else join_kernel<256><<<dim3((unsigned)groups), 256, 0, s>>>(a);
   GS_LAUNCH_CHECK();
   return GS_OK;
