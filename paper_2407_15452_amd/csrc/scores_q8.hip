@@ -375,11 +375,7 @@ __global__ __launch_bounds__(64 * WA * WC, 2) void tile_kernel(ScoresArgs a, Cop
   const int scale_c = (wc * NC * 32 + at) * in.scale_pitch;
 #pragma unroll
   for (int m = 0; m < NA; ++m) scale_n[m] = min((wa * NA + m) * 32 + at, nodes - 1) * a.scale_pitch;
-  auto four = [&](int m, int block) {
-    const uint8_t* p = scales_n + scale_n[m];
-    if (a.scale_pitch >= 4) return *reinterpret_cast<const uint32_t*>(p + block);
-    return (uint32_t)p[0] | (a.scale_pitch == 2 ? (uint32_t)p[1] << 8 : 0u);
-  };
+  auto four = [&](int m, int block) { return *reinterpret_cast<const uint32_t*>(scales_n + scale_n[m] + block); };      // three blocks and more
   if (O::kExact) {
     bool any = false;
 #pragma unroll
