@@ -598,7 +598,7 @@ int32_t gs_clip_grads(const gs_tensor* list, int32_t num_tensors, double max_nor
  *   rows.  bias, masked nodes and centres that
  *   are no row as for gs_scores; a scale NaN makes the scores of its row NaN.
  *   Same bits on every run.  Errors: GS_EINVAL, GS_EOVERFLOW for 2^21 centres and
- *   more, or more tiles of scores (128 x 128 or larger) than a launch takes (2^31).
+ *   more, or more tiles of scores (128 x 128 or larger) than a launch takes (2^24).
  * ------------------------------------------------------------------------ */
 enum { GS_Q8_MAX_DIM = 8192 };
 int32_t gs_q8_pitch(int32_t dim);
@@ -628,7 +628,8 @@ int32_t gs_scores_q8(const void* q_in, const void* scales_in, int64_t num_in, co
  *   p is that of the definition to 6e-14 (1 + |p| + |logp| + log n): candidates of different walks
  *   nearer than that may change places.  Same answer on every run, and for equal rows.
  *   1 <= n < 2^31, 1 <= beams, width <= 256, groups * beams < 2^22.  Errors: GS_EINVAL,
- *   GS_EOVERFLOW for more rows.
+ *   GS_EOVERFLOW for more rows, or more parts of them, of up to 16,384 scores, than a launch
+ *   takes (2^24).
  *
  * gs_beam_reorder -- what is kept for each walk follows the choice: row g * width + k of
  *   `out` becomes row g * beams + parents[g][k] of `data`, for each state of the list, a HOST

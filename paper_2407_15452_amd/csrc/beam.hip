@@ -816,16 +816,16 @@ extern "C" int32_t gs_beam_select(const void* scores, int64_t groups, int32_t be
   if (groups == 0) return GS_OK;
   const SelectPlan p = plan_select(ws, groups, beams, n, width, dtype);
   if (ws_bytes < p.bytes) return GS_EWORKSPACE;
-  const int64_t grid = groups * beams * p.parts;
-  if (grid > (int64_t)INT32_MAX) return GS_EOVERFLOW;
+  const int64_t slots = groups * beams * p.parts;
+  if (ceil_div(slots, kPartThreads / p.team) * kPartThreads >= (int64_t)1 << 32) return GS_EOVERFLOW;      // a launch takes fewer lanes
   // a group's workgroup reads its walks before it writes: those alone where both begin alike
   if (!(logp_out == logp && width == beams) && overlap(logp_out, groups * width * 4, logp, groups * beams * 4)) return GS_EINVAL;
   const SelectArgs a{scores, groups, groups * beams, n, beams, width, logp, ended, p.parts, p.part_len, p.keys, p.tops, p.sums, parents_out,
                      nodes_out, logp_out};
   const hipStream_t s = (hipStream_t)stream;
-  if (dtype == GS_F32) launch_parts<ScoreF32>(a, p, grid, s);
-  if (dtype == GS_BF16) launch_parts<ScoreHalf<bf16_t>>(a, p, grid, s);
-  if (dtype == GS_F16) launch_parts<ScoreHalf<f16_t>>(a, p, grid, s);
+  if (dtype == GS_F32) launch_parts<ScoreF32>(a, p, slots, s);
+  if (dtype == GS_BF16) launch_parts<ScoreHalf<bf16_t>>(a, p, slots, s);
+  if (dtype == GS_F16) launch_parts<ScoreHalf<f16_t>>(a, p, slots, s);
   GS_LAUNCH_CHECK();
   // of many candidates a group's lists take a large workgroup less time (8 groups of 8 walks on 1,000,000 nodes, width 8: 85 -> 80 us)
   if ((int64_t)beams * p.parts * width > kJoinList) join_kernel<1024><<<dim3((unsigned)groups), 1024, 0, s>>>(a);

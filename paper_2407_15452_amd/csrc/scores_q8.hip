@@ -892,10 +892,12 @@ ScoresPlan plan_scores(void* ws, int64_t num_centers, int32_t dim) {
 }
 
 template <typename O, int NA, int NC, int WA, int WC>
-int32_t run_tiles(const ScoresArgs& a, const Copied& in, hipStream_t s) {
+int32_t run_tiles(const ScoresArgs& a, const ScoresPlan& p, hipStream_t s) {
   const int64_t c = ceil_div(a.num_centers, 32 * NC * WC), n = ceil_div(a.num_nodes, 32 * NA * WA);
-  if (ceil_div(c * n, 8) * 8 > (int64_t)INT32_MAX) return GS_EOVERFLOW;
-  tile_kernel<O, NA, NC, WA, WC><<<dim3((unsigned)(ceil_div(c * n, 8) * 8)), 64 * WA * WC, 0, s>>>(a, in, c, n);
+  if (ceil_div(c * n, 8) * 8 * (64 * WA * WC) >= (int64_t)1 << 32) return GS_EOVERFLOW;      // a launch takes fewer lanes
+  copy_centers_kernel<<<dim3((unsigned)p.padded), 64, 0, s>>>(a, p.in);
+  GS_LAUNCH_CHECK();
+  tile_kernel<O, NA, NC, WA, WC><<<dim3((unsigned)(ceil_div(c * n, 8) * 8)), 64 * WA * WC, 0, s>>>(a, p.in, c, n);
   GS_LAUNCH_CHECK();
   return GS_OK;
 }
@@ -944,10 +946,8 @@ int32_t run_scores(const ScoresArgs& a, const ScoresPlan& p, hipStream_t s) {
     return GS_OK;
   }
   if (a.blocks <= 2) return run_strips<O>(a, s);
-  copy_centers_kernel<<<dim3((unsigned)p.padded), 64, 0, s>>>(a, p.in);
-  GS_LAUNCH_CHECK();
-  if (a.num_centers <= kNarrow) return run_tiles<O, 2, 2, 2, 2>(a, p.in, s);
-  return run_tiles<O, 4, 2, 1, 4>(a, p.in, s);
+  if (a.num_centers <= kNarrow) return run_tiles<O, 2, 2, 2, 2>(a, p, s);
+  return run_tiles<O, 4, 2, 1, 4>(a, p, s);
 }
 
 }  // namespace

@@ -111,3 +111,27 @@ def test_what_a_launch_takes_stays_one(launches):
     """2^24 - 1 workgroups are one launch, 2^24 are two."""
     assert check(launches, [(A, None, ((1 << 24) - 1) * 1024, -1)], 1, 1, 1) == 1
     assert check(launches, [(A, None, (1 << 24) * 1024, -1)], 1, 1, 1) == 2
+
+
+ANSWERS = """
+p = [C.c_void_p(1 << (40 + i)) for i in range(9)]
+def scores(centers, nodes, dim, dtype):
+    return lib.gs_scores_q8(p[0], p[1], C.c_int64(1000), p[2], p[3], C.c_int64(nodes), C.c_int32(dim), p[4], C.c_int64(centers), None, C.c_float(1.0), p[5],
+                            C.c_int32(dtype), p[6], C.c_size_t(1 << 50), None)
+def select(groups, beams, n, width, dtype):
+    return lib.gs_beam_select(p[0], C.c_int64(groups), C.c_int32(beams), C.c_int64(n), C.c_int32(dtype), p[1], None, C.c_int32(width), p[2], p[3], p[4], p[6],
+                              C.c_size_t(1 << 60), None)
+"""
+
+
+@pytest.mark.parametrize("call,fits", [
+    # 2^24 - 1 tiles go out in eights: 2^24 workgroups of 256 are 2^32 lanes; eight tiles fewer fit
+    ("scores(128, 2147483520, 300, 1)", False), ("scores(128, 2147483520 - 8 * 128, 300, 1)", True),
+    ("scores(1 << 20, 16777216 // 4096 * 128 - 1024, 300, 1)", True), ("scores(1 << 20, 16777216 // 4096 * 128, 300, 0)", False),
+    ("scores((1 << 21) - 1, 1 << 20, 300, 2)", False), ("scores(100_000, (1 << 31) - 1, 8192, 1)", False),
+    ("scores(2_000_000, 2_000_000_000, 256, 1)", True), ("scores(32, (1 << 31) - 1, 8192, 0)", True),
+    ("select(4_000_000, 1, 4096, 4, 0)", True), ("select(4_000_000, 1, 60_000, 33, 0)", True), ("select(4_000_000, 1, 90_000, 33, 0)", False),
+    ("select(4_000_000, 1, 1_000_000, 4, 1)", False), ("select(128, 1, (1 << 31) - 1, 4, 1)", False), ("select(127, 1, (1 << 31) - 1, 4, 1)", True)])
+def test_what_no_launch_takes_is_refused_at_once(launches, call, fits):
+    got, rc = launches(ANSWERS + "print(json.dumps({'rc': %s}))\n" % call)
+    assert rc == [0 if fits else -3] and (len(got) > 0) == fits
