@@ -713,6 +713,7 @@ def gs_clip_grads(grads, max_norm: float, norm_out=None, ws=None):
 
 
 GS_Q8_MAX_DIM = 8192
+MOST_BEAMS = 256                 # and the most places of a selection; checked here, since what is passed on has 32 bits
 
 
 def _one_device(dev, **tensors):
@@ -790,7 +791,7 @@ def gs_quantize_rows(table, ids=None, count=None, out=None) -> Table8:
 
 
 def gs_scores_q8_workspace_bytes(num_centers: int, num_nodes: int, dim: int) -> int:
-    return int(lib().gs_scores_q8_workspace_bytes(num_centers, num_nodes, dim))
+    return int(lib().gs_scores_q8_workspace_bytes(num_centers, num_nodes, dim)) if 1 <= dim <= GS_Q8_MAX_DIM else 0
 
 
 def gs_scores_q8(t_in: Table8, t_out: Table8, centers, bias=None, scale: float = 1.0, dtype=torch.float32, out=None, ws=None):
@@ -813,6 +814,8 @@ def gs_scores_q8(t_in: Table8, t_out: Table8, centers, bias=None, scale: float =
 
 
 def gs_beam_select_workspace_bytes(groups: int, beams: int, n: int, width: int, dtype: int = GS_F32) -> int:
+    if not (1 <= beams <= MOST_BEAMS and 1 <= width <= MOST_BEAMS):
+        return 0
     return int(lib().gs_beam_select_workspace_bytes(groups, beams, n, width, dtype))
 
 
@@ -821,6 +824,8 @@ def gs_beam_select(scores, logp, beams: int, width: int, ended=None, parents_out
     [groups * beams]; ended: bool or uint8 [groups * beams].  Returns (parents, nodes int32, logp float32), [groups, width] each."""
     if scores.dim() != 2 or beams < 1 or scores.shape[0] % beams != 0:
         raise ValueError("scores must be [groups * beams, n]")
+    if not 1 <= width <= MOST_BEAMS:
+        raise ValueError(f"width must be from 1 to {MOST_BEAMS}")
     dtype = _table_dtype(scores)
     rows, n, dev = int(scores.shape[0]), int(scores.shape[1]), scores.device
     groups = rows // beams
