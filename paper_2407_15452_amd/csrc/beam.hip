@@ -10,7 +10,8 @@
 //
 // The width best without a sort: of the largest score of each lane, the width-th largest is a lower bound of what can be taken,
 // and little more than `width` scores reach it.  Those go to a list, where each one's place is the number of larger ones.  Where too
-// many reach it (equal scores), the best is taken out `width` times instead.
+// many reach it (equal scores), the best is taken out `width` times instead, step after step: four walks on 10,000 nodes of equal scores,
+// width 4, take 63 us where random ones take 15, 32 walks on 100,000, width 64, 0.9 ms instead of 47 us, and 256 walks on 5000, width 256, 9.8 ms.
 //
 // Bound: the weights' arithmetic.  A score costs 26 vector instructions, 18 of them the fp64 weight (a sum in fp32 would be off by more
 // than neighbours of different walks are apart): 64 rows of 1,000,000 fp32 scores take 64 us, 4.0 TB/s, 49 of them instructions; reading
@@ -20,8 +21,9 @@
 // 18 and 72).
 //
 // gs_beam_reorder: memory.  64 groups of 8 walks with six rows of 32,768 fp32 values each: 131 us, 6.1 TB/s counted as every row read and
-// written once (parents repeat, and such rows come from the caches).  Sixteen bytes a lane, four of them in flight, one launch for all
-// states; in place a workgroup holds a stripe of all rows of a group in LDS between reading and writing.
+// written once (parents repeat, and such rows come from the caches).  A lane moves four pieces of sixteen bytes one after the other (the
+// compiler keeps them in LDS between reading and writing, and waits for each); one launch for all states that fit one.  In place a workgroup
+// holds a stripe of all rows of a group in LDS between reading and writing: the same case 334 us.
 
 #include "weigh.h"
 
